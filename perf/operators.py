@@ -1,0 +1,357 @@
+"""The operators of the 8-bit paged KV cache, as measured cases, with their plain forms.
+
+A row (token, kv head) of such a cache is d codes in e4m3 and one exponent byte E, the values being code * 2^(E - 127); E - 127 is the smallest e
+>= -126 with max|x| <= 448 * 2^e.
+
+kind "write"   new rows of a layer: bias, rotary embedding, quantising and write; the rows just written read back
+kind "attend"  tree attention over a layer's cache (one node: plain decoding)
+kind "read"    a range of committed rows of every sequence read back
+kind "commit"  the accepted path of every sequence kept, all layers; the kept rows read back
+kind "step"    one layer's part of a step: write, attention, commit; the kept rows read back
+
+Head shapes are those of synth/inputs.py: "tiny" 4 / 2 of 64 in fp32, "7b" 28 / 4, "32b" 40 / 8 and "70b" 64 / 8 of 128 in bf16.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+HEADS = {"tiny": (4, 2, 64), "7b": (28, 4, 128), "32b": (40, 8, 128), "70b": (64, 8, 128)}   # query heads, kv heads, head_dim
+PAGE, THETA = 16, 1e6
+
+
+def listed():
+    return [
+        # the smallest calls: a tiny fp32 decoder's step with a chain of drafts; launches and latency are everything
+        dict(name="tiny step 2 x 5", kind="step", heads="tiny", batch=2, nodes=5, ctx=128, spread=0.0, layers=1),
+        # speculation off: the last sequence of a rollout, a middling batch, a rollout's first phase with lengths of all kinds
+        dict(name="attend 1 x 1 of 8192", kind="attend", heads="7b", batch=1, nodes=1, ctx=8192, spread=0.0, layers=1),
+        dict(name="attend 16 x 1 of 8192", kind="attend", heads="7b", batch=16, nodes=1, ctx=8192, spread=0.0, layers=1),
+        dict(name="attend 64 x 1 of ~8192", kind="attend", heads="32b", batch=64, nodes=1, ctx=8192, spread=0.6, layers=1),
+        # a small tree behind a very long context, a small tree for many sequences, the benchmark's tree
+        dict(name="attend 1 x 8 of 30000", kind="attend", heads="7b", batch=1, nodes=8, ctx=30000, spread=0.0, layers=1),
+        dict(name="attend 16 x 16 of 8192", kind="attend", heads="7b", batch=16, nodes=16, ctx=8192, spread=0.0, layers=1),
+        dict(name="attend 32 x 48 of ~4096", kind="attend", heads="7b", batch=32, nodes=48, ctx=4096, spread=0.8, layers=1),
+        # one new row, and a verification's rows
+        dict(name="write 1 x 1", kind="write", heads="7b", batch=1, nodes=1, ctx=8191, spread=0.0, layers=1),
+        dict(name="write 32 x 48", kind="write", heads="7b", batch=32, nodes=48, ctx=4096, spread=0.8, layers=1),
+        # prefixes of a few layers taken out of the cache; a batch's accepted paths kept in all layers
+        dict(name="read 7 x 4001", kind="read", heads="7b", batch=7, nodes=4001, ctx=5000, spread=0.3, layers=4),
+        dict(name="commit 32 x 28 layers", kind="commit", heads="7b", batch=32, nodes=48, ctx=700, spread=0.5, layers=28),
+        # the tail of a rollout: few sequences of 24k-32k tokens with the largest trees
+        dict(name="step 4 x 64 of ~28000", kind="step", heads="7b", batch=4, nodes=64, ctx=28000, spread=0.1, layers=1),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(["attend", "attend", "attend", "step", "step", "write", "read", "commit"])
+    heads = rng.choice(["7b", "7b", "32b", "70b", "tiny"])
+    spread = rng.choice([0.0, 0.3, 0.8])
+    if heads == "tiny":
+        kind = rng.choice(["attend", "step"])
+        return dict(kind=kind, heads=heads, batch=_log(rng, 1, 8), nodes=_log(rng, 1, 16), ctx=_log(rng, 20, 600), spread=spread, layers=1)
+    if kind == "write":
+        batch = _log(rng, 1, 64)
+        return dict(kind=kind, heads=heads, batch=batch, nodes=_log(rng, 1, min(64, 1536 // batch)), ctx=_log(rng, 50, 8000), spread=spread, layers=1)
+    if kind == "read":
+        batch = _log(rng, 1, 16)
+        n = _log(rng, 1, 12000 // batch)
+        return dict(kind=kind, heads=heads, batch=batch, nodes=n, ctx=n + _log(rng, 1, 500), spread=spread, layers=_log(rng, 1, 4))
+    if kind == "commit":
+        batch = _log(rng, 1, 32)
+        return dict(kind=kind, heads=heads, batch=batch, nodes=_log(rng, 8, 64), ctx=_log(rng, 30, 700), spread=spread, layers=_log(rng, 1, 28))
+    batch, nodes = _log(rng, 1, 32), rng.choice([1, 1, 2, _log(rng, 2, 64), _log(rng, 2, 64)])
+    # (the work of the largest listed case: some 160000 keys times 48 nodes, and lengths that stay inside 32768 when spread)
+    return dict(kind=kind, heads=heads, batch=batch, nodes=nodes, ctx=_log(rng, 60, min(20000, 200000 // batch, 4000000 // (batch * nodes))), spread=spread, layers=1)
+
+
+# ---- inputs
+
+def _contexts(case, rng):
+    """Committed tokens of every sequence: ctx, or lognormal lengths whose mean it is."""
+    ctx = case["ctx"] * np.exp(rng.normal(-case["spread"] / 2, 1.0, case["batch"]) * case["spread"])
+    low = case["nodes"] if case["kind"] == "read" else 1
+    return np.clip(np.rint(ctx), low, max(4 * case["ctx"] if case["ctx"] < 8192 else 32768, low)).astype(np.int32)
+
+
+def _quantised(shape, std, g):
+    """Codes and exponents of rows drawn from a normal distribution."""
+    codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device="cuda")
+    exps = torch.empty(shape[:-1], dtype=torch.uint8, device="cuda")
+    flat, flat_e = codes.view(-1, shape[-1]), exps.view(-1)
+    for o in range(0, flat.shape[0], 1 << 21):
+        x = torch.randn((min(1 << 21, flat.shape[0] - o), shape[-1]), generator=g, device="cuda") * std
+        flat[o:o + x.shape[0]], flat_e[o:o + x.shape[0]] = _codes(x)
+    return codes, exps
+
+
+def _tree(rng, batch, n):
+    """Parents and ancestor masks of random trees."""
+    depth, mask = np.zeros((batch, n), np.int32), np.zeros((batch, n), np.uint64)
+    for b in range(batch):
+        for i in range(n):
+            p = int(rng.integers(max(0, i - 6), i)) if i else -1
+            depth[b, i] = depth[b, p] + 1 if i else 0
+            mask[b, i] = (mask[b, p] if i else np.uint64(0)) | (np.uint64(1) << np.uint64(i))
+    return depth, mask
+
+
+def prepare(case, seed):
+    rng = np.random.default_rng(seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    Hq, Hkv, d = HEADS[case["heads"]]
+    B, L, kind = case["batch"], case["layers"], case["kind"]
+    n = case["nodes"]
+    ctx = _contexts(case, rng)
+    room = n if kind != "read" else 0
+    pages = (ctx + room + PAGE - 1) // PAGE
+    order = rng.permutation(int(pages.sum()) + 3).astype(np.int32)
+    table = np.full((B, int(pages.max())), -1, np.int32)
+    for b, o in enumerate(np.cumsum(pages) - pages):
+        table[b, :pages[b]] = order[o:o + pages[b]]
+    cuda = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    s = dict(kind=kind, Hq=Hq, Hkv=Hkv, d=d, B=B, n=n, L=L, bound=int(ctx.max()), dtype=torch.float32 if case["heads"] == "tiny" else torch.bfloat16,
+             table=cuda(table), seq_len=cuda(ctx), seq_len0=cuda(ctx))
+    shape = (L, len(order), Hkv, PAGE, d)
+    s["k"], s["k_exp"] = _quantised(shape, 1.0, g)
+    s["v"], s["v_exp"] = _quantised(shape, 1.0, g)
+    if kind in ("write", "attend", "step"):
+        depth, mask = _tree(rng, B, n)
+        s["depth"], s["mask"] = cuda(depth), cuda(mask.view(np.int64))
+        s["qkv"] = (torch.randn((B, n, (Hq + 2 * Hkv) * d), generator=g, device="cuda") * 1.5).to(s["dtype"])
+        s["bias"] = (torch.randn(((Hq + 2 * Hkv) * d,), generator=g, device="cuda") * 0.5).to(s["dtype"])
+        s["q"] = s["qkv"][..., :Hq * d].contiguous()
+        s["out"] = torch.empty_like(s["q"])
+    if kind in ("commit", "step"):
+        # an accepted path: the root, then nodes of rising index (sources behind the places they go to)
+        width = min(7, n)
+        acc, path = np.zeros(B, np.int32), np.full((B, width), -1, np.int32)
+        for b in range(B):
+            a = int(rng.integers(0, min(width - 1, (n - 1) // 2) + 1))
+            acc[b] = a
+            path[b, 0], path[b, 1:a + 1] = 0, np.sort(rng.permutation(np.arange(a + 1, n))[:a])
+        s["accept_len"], s["path"], s["stride"], s["count"] = cuda(acc), cuda(path), width, cuda(acc + 1)
+    if kind == "read":
+        s["first"] = cuda(np.array([rng.integers(0, c - n + 1) for c in ctx], np.int32))
+    rows = s["stride"] if kind in ("commit", "step") else n
+    if kind != "attend":
+        s["k_rows"], s["v_rows"] = (torch.zeros((L, B, rows, Hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    return s
+
+
+# ---- the plain forms
+
+def _codes(x):
+    """(e4m3 codes, exponent bytes) of finite fp32 rows."""
+    m, e = torch.frexp(x.abs().amax(-1))
+    e = torch.where(m > 0, (e - 9 + (m > 0.875).to(e.dtype)).clamp(min=-126), -126)
+    return (x * torch.exp2(-e.float())[..., None]).to(torch.float8_e4m3fn), (e + 127).to(torch.uint8)
+
+
+def _slots(s, first, n):
+    """(page, row) of slots first[b] .. first[b] + n - 1; slots behind the table's end stand for its last one."""
+    slot = first[:, None].long() + torch.arange(n, device="cuda")
+    return s["table"].gather(1, (slot // PAGE).clamp(max=s["table"].shape[1] - 1)).long().clamp(min=0), slot % PAGE
+
+
+def _values(codes, exps, pg, row):
+    """[L, B, n, Hkv, d] in fp32."""
+    return (codes.view(torch.uint8)[:, pg, :, row].view(torch.float8_e4m3fn).float() * torch.exp2(exps[:, pg, :, row].float() - 127.0)[..., None]).permute(2, 0, 1, 3, 4)
+
+
+def _plain_write(s):
+    Hq, Hkv, d, B, n = s["Hq"], s["Hkv"], s["d"], s["B"], s["n"]
+    x = (s["qkv"].float() + s["bias"].float()).view(B, n, Hq + 2 * Hkv, d)
+    pos = (s["seq_len"][:, None] + s["depth"]).double()
+    angle = pos[..., None] * torch.pow(torch.tensor(THETA, dtype=torch.float64, device="cuda"), -2.0 * torch.arange(d // 2, device="cuda", dtype=torch.float64) / d)
+    c, sn = torch.cos(angle).float()[:, :, None], torch.sin(angle).float()[:, :, None]
+    lo, hi = x[:, :, :Hq + Hkv, :d // 2], x[:, :, :Hq + Hkv, d // 2:]
+    rot = torch.cat([lo * c - hi * sn, hi * c + lo * sn], -1)
+    pg, row = _slots(s, s["seq_len"], n)
+    s["k"][0].view(torch.uint8)[pg, :, row], s["k_exp"][0][pg, :, row] = (t.view(torch.uint8) for t in _codes(rot[:, :, Hq:]))
+    s["v"][0].view(torch.uint8)[pg, :, row], s["v_exp"][0][pg, :, row] = (t.view(torch.uint8) for t in _codes(x[:, :, Hq + Hkv:]))
+    return rot[:, :, :Hq].reshape(B, n, Hq * d).to(s["dtype"])
+
+
+def _plain_attend(s, q):
+    Hq, Hkv, d, B, n = s["Hq"], s["Hkv"], s["d"], s["B"], s["n"]
+    T, G = s["bound"] + n, Hq // Hkv
+    pg, row = _slots(s, torch.zeros_like(s["seq_len"]), T)
+    at = torch.arange(T, device="cuda")[None, None] - s["seq_len"][:, None, None]          # place in the tree, negative: context
+    seen = (at < 0) | ((at < n) & (((s["mask"][:, :, None] >> at.clamp(0, 63)) & 1) != 0))   # [B, n, T]
+    q = q.float().view(B, n, Hkv, G, d).permute(0, 2, 1, 3, 4).reshape(B, Hkv, n * G, d)
+    k = _values(s["k"], s["k_exp"], pg, row)[0].permute(0, 2, 3, 1).contiguous()   # [B, Hkv, d, T]
+    score = (torch.matmul(q, k) / math.sqrt(d)).view(B, Hkv, n, G, T).masked_fill_(~seen[:, None, :, None], -math.inf).view(B, Hkv, n * G, T)
+    p = torch.exp(score - score.amax(-1, keepdim=True))
+    v = _values(s["v"], s["v_exp"], pg, row)[0].permute(0, 2, 1, 3).contiguous()
+    o = torch.matmul(p, v) / p.sum(-1, keepdim=True)
+    return o.view(B, Hkv, n, G, d).permute(0, 2, 1, 3, 4).reshape(B, n, Hq * d).to(s["dtype"])
+
+
+def _plain_read(s, first, n, count=None):
+    k, v = (_values(s[x], s[x + "_exp"], *_slots(s, first, n)) for x in ("k", "v"))
+    if count is not None:
+        keep = (torch.arange(n, device="cuda")[None] < count[:, None])[None, :, :, None, None]
+        k, v = torch.where(keep, k, s["k_rows"].float()), torch.where(keep, v, s["v_rows"].float())
+    return k.to(torch.bfloat16), v.to(torch.bfloat16)
+
+
+def _plain_commit(s):
+    j = torch.arange(s["stride"], device="cuda")[None].expand(s["B"], -1)
+    moves = (j >= 1) & (j <= s["accept_len"][:, None])
+    src = torch.where(moves, s["path"], j) + s["seq_len"][:, None]
+    dst = j + s["seq_len"][:, None]
+    place = lambda slot: (s["table"].gather(1, (slot // PAGE).clamp(max=s["table"].shape[1] - 1)).long().clamp(min=0)[moves], (slot % PAGE)[moves])
+    (ps, rs), (pd, rd) = place(src.long()), place(dst.long())
+    for x in ("k", "v", "k_exp", "v_exp"):
+        t = s[x].view(torch.uint8)
+        t[:, pd, :, rd] = t[:, ps, :, rs]
+    s["seq_len"] += s["accept_len"] + 1
+
+
+def _plain(s):
+    kind, start = s["kind"], s["seq_len0"]
+    if kind == "attend":
+        return _plain_attend(s, s["q"])
+    if kind == "read":
+        return _plain_read(s, s["first"], s["n"])
+    s["seq_len"].copy_(start)
+    if kind == "write":
+        q = _plain_write(s)
+        return (q, *_plain_read(s, start, s["n"]))
+    out = _plain_attend(s, _plain_write(s)) if kind == "step" else None
+    _plain_commit(s)
+    rows = _plain_read(s, start, s["stride"], s["count"])
+    return (s["seq_len"], *rows) if out is None else (out, s["seq_len"], *rows)
+
+
+# ---- the framework's calls
+
+def _own(s):
+    from paper_2511_16665_amd import binding as tlt
+    code = tlt.TLT_F32 if s["dtype"] == torch.float32 else tlt.TLT_BF16
+    kind, Hq = s["kind"], s["Hq"]
+    if "kv" not in s:   # what a program keeps: the cache's handle and the attention's workspace
+        s["kv"] = tlt.KV8(s["k"], s["v"], s["k_exp"], s["v_exp"], s["table"], s["seq_len"], s["bound"])
+        if kind in ("attend", "step"):
+            s["ws"] = tlt.kv8_attention_workspace(s["B"], s["n"], Hq, s["Hkv"], s["d"], s["bound"] + s["n"])
+    kv = s["kv"]
+    if kind == "attend":
+        tlt.kv8_attention(code, Hq, s["q"], s["mask"], kv, 0, s["out"], s["ws"])
+        return s["out"]
+    if kind == "read":
+        tlt.kv8_read(tlt.TLT_BF16, kv, s["first"], None, s["k_rows"], s["v_rows"])
+        return s["k_rows"], s["v_rows"]
+    s["seq_len"].copy_(s["seq_len0"])
+    if kind in ("write", "step"):
+        tlt.kv8_write(code, Hq, THETA, s["qkv"], s["bias"], s["depth"], kv, 0, s["q"])
+    if kind == "write":
+        tlt.kv8_read(tlt.TLT_BF16, kv, s["seq_len0"], None, s["k_rows"], s["v_rows"])
+        return s["q"], s["k_rows"], s["v_rows"]
+    if kind == "step":
+        tlt.kv8_attention(code, Hq, s["q"], s["mask"], kv, 0, s["out"], s["ws"])
+    tlt.kv8_commit(kv, s["accept_len"], s["path"])
+    tlt.kv8_read(tlt.TLT_BF16, kv, s["seq_len0"], s["count"], s["k_rows"], s["v_rows"])
+    rows = (s["seq_len"], s["k_rows"], s["v_rows"])
+    return (s["out"], *rows) if kind == "step" else rows
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+# ---- what a pass cannot do without
+
+def work(case):
+    Hq, Hkv, d = HEADS[case["heads"]]
+    B, n, L, kind = case["batch"], case["nodes"], case["layers"], case["kind"]
+    e = 4 if case["heads"] == "tiny" else 2
+    token = 2 * Hkv * (d + 1)                       # a cached token of one layer
+    keys = B * (case["ctx"] + n)
+    attend = (keys * token + 2 * B * n * Hq * d * e, 4.0 * d * Hq * n * keys)
+    write = (B * n * ((2 * Hq + 2 * Hkv) * d * e + token), 3.0 * B * n * (Hq + 2 * Hkv) * d)
+    rows = min(7, n) if kind in ("commit", "step") else n
+    read = (L * B * rows * (token + 2 * Hkv * d * 2), L * B * rows * 2.0 * Hkv * d)
+    commit = (2 * L * B * min(3, (n - 1) // 2) * token, 0.0)
+    parts = {"attend": [attend], "write": [write, read], "read": [read], "commit": [commit, read], "step": [write, attend, commit, read]}[kind]
+    return {"bytes": float(sum(p[0] for p in parts)), "flops": float(sum(p[1] for p in parts))}
+
+
+# ---- the definitions in 64 bits, a sequence and a row at a time
+
+def _decode(byte):
+    """Values of e4m3 codes: sign, four bits of exponent (bias 7), three of fraction."""
+    byte = byte.long()
+    x, f = (byte >> 3) & 15, (byte & 7).double()
+    mag = torch.where(x > 0, (1.0 + f / 8.0) * torch.pow(2.0, (x - 7).double()), f * 2.0 ** -9)
+    return torch.where(byte >= 128, -mag, mag)
+
+
+def _nearest(x):
+    """Rows in 64 bits as the cache keeps them: the nearest of e4m3's values times the row's power of two (halves to the even fraction)."""
+    a = x.abs().amax(-1, keepdim=True)
+    e = torch.ceil(torch.log2(a / 448.0)).clamp(min=-126.0)
+    e = torch.where(448.0 * torch.pow(2.0, e - 1) >= a, e - 1, e)
+    e = torch.where(448.0 * torch.pow(2.0, e) < a, e + 1, e).clamp(min=-126.0)
+    y = x / torch.pow(2.0, e)
+    step = torch.pow(2.0, torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3.0)
+    return torch.round(y / step) * step * torch.pow(2.0, e)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    Hq, Hkv, d, B, n, L, kind = s["Hq"], s["Hkv"], s["d"], s["B"], s["n"], s["L"], s["kind"]
+    G, table, ctx = Hq // Hkv, s["table"].long(), s["seq_len0"].tolist()
+    raw = {x: s[x].view(torch.uint8) for x in ("k", "v")}
+
+    def rows(x, layer, b, lo, hi):          # [hi - lo, Hkv, d]
+        at = torch.arange(lo, hi, device="cuda")
+        pg, r = table[b, at // PAGE], at % PAGE
+        return _decode(raw[x][layer][pg, :, r]) * torch.pow(2.0, s[x + "_exp"][layer][pg, :, r].double() - 127.0)[..., None]
+
+    new, q64 = {}, {}
+    if kind in ("write", "step"):
+        freq = THETA ** (-np.arange(0, d, 2, dtype=np.float64) / d)
+        for b in range(B):
+            x = s["qkv"][b].double() + s["bias"].double()
+            x = x.view(n, Hq + 2 * Hkv, d)
+            turn = (ctx[b] + s["depth"][b].double())[:, None] * torch.from_numpy(freq).cuda()
+            z = torch.complex(x[:, :Hq + Hkv, :d // 2], x[:, :Hq + Hkv, d // 2:]) * torch.polar(torch.ones_like(turn), turn)[:, None]
+            y = torch.cat([z.real, z.imag], -1)
+            q64[b] = y[:, :Hq]
+            new[b] = {"k": _nearest(y[:, Hq:]), "v": _nearest(x[:, Hq + Hkv:])}
+    attended = []
+    if kind in ("attend", "step"):
+        for b in range(B):
+            K, V = (torch.cat([rows(x, 0, b, 0, ctx[b]), new[b][x] if new else rows(x, 0, b, ctx[b], ctx[b] + n)]) for x in ("k", "v"))
+            q = q64[b] if new else s["q"][b].double().view(n, Hq, d)
+            if new:
+                q = q.to(s["dtype"]).double()      # (the rotated query is held in the model's type)
+            tree = ((s["mask"][b][:, None] >> torch.arange(n, device="cuda")) & 1).bool()
+            out = torch.empty((n, Hq, d), dtype=torch.float64, device="cuda")
+            for h in range(Hkv):
+                sc = (q[:, h * G:(h + 1) * G].reshape(n * G, d) @ K[:, h].t()) * d ** -0.5
+                sc = sc.view(n, G, -1)
+                sc[:, :, ctx[b]:] = torch.where(tree[:, None], sc[:, :, ctx[b]:], -math.inf)
+                out[:, h * G:(h + 1) * G] = (torch.softmax(sc, -1).view(n * G, -1) @ V[:, h]).view(n, G, d)
+            attended.append(out.view(n, Hq * d))
+        attended = torch.stack(attended)
+    if kind == "attend":
+        return attended
+    if kind == "write":
+        return (torch.stack([q64[b].reshape(n, Hq * d) for b in range(B)]), *(torch.stack([new[b][x] for b in range(B)])[None] for x in ("k", "v")))
+    if kind == "read":
+        return tuple(torch.stack([torch.stack([rows(x, l, b, f, f + n) for b, f in enumerate(s["first"].tolist())]) for l in range(L)]) for x in ("k", "v"))
+    kept = {x: torch.zeros((L, B, s["stride"], Hkv, d), dtype=torch.float64, device="cuda") for x in ("k", "v")}
+    for b, a in enumerate(s["accept_len"].tolist()):
+        for j, p in enumerate(s["path"][b, :a + 1].tolist()):
+            for x in ("k", "v"):
+                for l in range(L):
+                    kept[x][l, b, j] = new[b][x][p] if new else rows(x, l, b, ctx[b] + p, ctx[b] + p + 1)[0]
+    return (None, kept["k"], kept["v"]) if kind == "commit" else (attended, None, kept["k"], kept["v"])
