@@ -332,6 +332,65 @@ int tlt_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
                   const void *qkv, const uint64_t *anc_mask, const tlt_kv *kv, void *out, void *ws, size_t ws_bytes,
                   int impl);
 
+/* ---- 8-bit paged KV cache -----------------------------------------------------------------------
+ * The cache of tlt_kv in half the memory (a quarter of fp32's): what bounds a step of few rows behind long contexts, and
+ * how many sequences fit, is the cache.  A row (one token of one kv head, d elements) is d codes in e4m3 (the OCP
+ * format: bias 7, largest value 448) and one exponent byte E, its values being code * 2^(E - 127).  E - 127 is the
+ * smallest e >= -126 with max|x| <= 448 * 2^e; codes are rounded to nearest, ties to even.  Scaling is exact and a value has
+ * four significant bits, so reading a row into bf16 or fp32 is exact.  A row with an element that is not finite has E =
+ * 255 and codes of zero: all of it reads as NaN (and poisons exactly the attention rows that see it).  Codes 0x7f and 0xff
+ * and E = 0 are never written and must not be put there.
+ *
+ * k_pool, v_pool: DEVICE [n_layers][n_pages][n_kv_heads][page_size][d] bytes, 16-byte aligned; k_exp, v_exp: DEVICE
+ * [n_layers][n_pages][n_kv_heads][page_size] bytes.  The other fields are those of tlt_kv.  tlt_kv8_write and
+ * tlt_kv8_attention take ONE layer's pools (advance the four pointers), tlt_kv8_commit and tlt_kv8_read those of n_layers.
+ * All of them: head_dim 64, 128, 192 or 256, any page size, any number of query heads per kv head; slots that the block table does not
+ * back are not written, and count as keys and values of zero.  dtype (TLT_F32 / TLT_BF16) is that of the activations.
+ * Sums, softmax and rotations are fp32, angles double.  No memory is kept between calls; calls may be captured into
+ * graphs.  Errors: TLT_EINVAL, TLT_ESHAPE (a workspace that is too small, or an `impl` that does not cover the shape),
+ * TLT_ENOPAGES, TLT_EHIP. */
+typedef struct tlt_kv8 {
+    void *k_pool, *v_pool, *k_exp, *v_exp;
+    int64_t n_pages;
+    const int32_t *block_table;
+    int32_t *seq_len;
+    int32_t max_pages;
+    int32_t seq_len_bound;
+} tlt_kv8;
+
+/* n new rows per sequence, from their projection qkv [B][n][(Hq+2Hkv)*d] (DEVICE, dtype): bqkv [(Hq+2Hkv)*d] is added
+ * (NULL: none), q and k are rotated at position seq_len[b] + depth[b][i] (depth DEVICE [B][n]; NULL: i), and keys and values go to
+ * slot seq_len[b] + i.  The rotated queries go to q_out: rows of Hq*d elements of dtype, q_stride elements apart (a multiple of
+ * 16 bytes, at least Hq*d); q_out may be qkv with q_stride = (Hq+2Hkv)*d.  seq_len is unchanged.  qkv, bqkv and q_out
+ * are 16-byte aligned.  Any n >= 1. */
+int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size,
+                  float rope_theta, const void *qkv, const void *bqkv, const int32_t *depth, const tlt_kv8 *kv, void *q_out,
+                  int64_t q_stride);
+
+/* Attention of the rows that tlt_kv8_write has written (n <= TLT_MAX_TREE per sequence): row (b, i) attends to every slot below
+ * seq_len[b] and to slot seq_len[b] + j (j < n) where bit j of anc_mask[b][i] is set (anc_mask NULL: j <= i, a chain); a row that
+ * sees nothing gives zeros.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
+ * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
+ * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
+ * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).
+ * impl: -1 automatic, 0 a workgroup per row and query head (any shape). */
+size_t tlt_kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int max_ctx);
+int tlt_kv8_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size,
+                      const void *q, int64_t q_stride, const uint64_t *anc_mask, const tlt_kv8 *kv, void *out, void *ws,
+                      size_t ws_bytes, int impl);
+
+/* tlt_kv_commit for this cache: in every layer and kv head row seq_len[b]+path_idx[b][j] moves to row seq_len[b]+j for
+ * j <= accept_len[b] (codes and exponent bytes), then seq_len[b] += accept_len[b]+1.  accept_len is capped at stride - 1
+ * and at 63; entries of path_idx [B][stride] that do not lie behind j (or at 64 and above) move nothing. */
+int tlt_kv8_commit(void *stream, int B, int n_layers, int n_kv_heads, int head_dim, int page_size, const tlt_kv8 *kv,
+                   const int32_t *accept_len, const int32_t *path_idx, int stride);
+
+/* Reads rows back: out_k, out_v [n_layers][B][n][Hkv][d] (DEVICE, dtype, 16-byte aligned), row j of sequence b being slot first[b] + j
+ * (first: DEVICE [B]).  count (DEVICE [B], may be NULL: n): rows j >= count[b] of the outputs are left as they were.  Slots
+ * that the block table does not back read as zeros; whether a slot has been written is the caller's business. */
+int tlt_kv8_read(void *stream, int dtype, int n_layers, int B, int n, int n_kv_heads, int head_dim, int page_size,
+                 const tlt_kv8 *kv, const int32_t *first, const int32_t *count, void *out_k, void *out_v);
+
 /* Attention kernel choice for cross-checks: -1 automatic (default), 0 wave-per-row kernel,
  * 1 MFMA split-KV kernel (bf16, head_dim 128 only; other shapes fall back to 0). */
 int tlt_set_attention_impl(tlt_ctx *ctx, int impl);

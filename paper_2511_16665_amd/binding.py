@@ -28,6 +28,7 @@ EXPORTS = [
     "tlt_mab_median_reward", "tlt_ngram_create", "tlt_ngram_destroy", "tlt_ngram_insert", "tlt_ngram_propose",
     "tlt_template_build", "tlt_draft_sample", "tlt_gemm_argmax", "tlt_gemm_glu", "tlt_gemm_parts", "tlt_draft_pool", "tlt_set_oproj_rounding", "tlt_device_status", "tlt_accept_sample_static", "tlt_attention", "tlt_attention_workspace_bytes",
     "tlt_graph_pool_create", "tlt_graph_pool_destroy", "tlt_graph_pool_step", "tlt_graph_pool_count", "tlt_mfma_stream", "tlt_prefill", "tlt_step_report",
+    "tlt_kv8_write", "tlt_kv8_attention", "tlt_kv8_attention_workspace_bytes", "tlt_kv8_commit", "tlt_kv8_read",
 ]
 
 
@@ -58,6 +59,11 @@ class StrategyC(C.Structure):
 class KVC(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("n_pages", C.c_int64), ("block_table", C.c_void_p),
                 ("seq_len", C.c_void_p), ("max_pages", C.c_int32), ("seq_len_bound", C.c_int32)]
+
+
+class KV8C(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("n_pages", C.c_int64),
+                ("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("max_pages", C.c_int32), ("seq_len_bound", C.c_int32)]
 
 
 class TreeC(C.Structure):
@@ -119,6 +125,13 @@ def load() -> C.CDLL:
     lib.tlt_attention_workspace_bytes.argtypes = [C.c_int] * 6
     lib.tlt_attention.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.c_void_p, C.c_void_p, C.POINTER(KVC), C.c_void_p, C.c_void_p,
                                                                C.c_size_t, C.c_int]
+    lib.tlt_kv8_write.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.c_float] + [C.c_void_p] * 3 + [C.POINTER(KV8C), C.c_void_p, C.c_int64]
+    lib.tlt_kv8_attention_workspace_bytes.restype = C.c_size_t
+    lib.tlt_kv8_attention_workspace_bytes.argtypes = [C.c_int] * 6
+    lib.tlt_kv8_attention.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(KV8C), C.c_void_p, C.c_void_p,
+                                                                   C.c_size_t, C.c_int]
+    lib.tlt_kv8_commit.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.POINTER(KV8C), C.c_void_p, C.c_void_p, C.c_int]
+    lib.tlt_kv8_read.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.POINTER(KV8C)] + [C.c_void_p] * 4
     lib.tlt_set_oproj_rounding.argtypes = [C.c_void_p, C.c_int]
     lib.tlt_device_status.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint32)]
     lib.tlt_step_report.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_uint32)]
@@ -483,6 +496,108 @@ def attention(dtype_code, n_q_heads, page_size, qkv, anc_mask, kv: KV, out, ws, 
               kv.block_table.shape[1], int(kv.seq_len_bound))
     return load().tlt_attention(_stream(), dtype_code, B, n, n_q_heads, n_kv, d, page_size, _ptr(qkv), _ptr(anc_mask),
                                 C.byref(kvc), _ptr(out), _ptr(ws), ws.numel(), impl)
+
+
+@dataclasses.dataclass
+class KV8:
+    """8-bit paged KV cache of one model (tlt_kv8): codes [L, n_pages, Hkv, page, d] and exponent bytes [L, n_pages, Hkv, page] of keys and
+    values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV."""
+    k_pool: torch.Tensor
+    v_pool: torch.Tensor
+    k_exp: torch.Tensor
+    v_exp: torch.Tensor
+    block_table: torch.Tensor
+    seq_len: torch.Tensor
+    seq_len_bound: int
+
+    @staticmethod
+    def empty(n_layers, n_pages, n_kv_heads, page_size, head_dim, block_table, seq_len, seq_len_bound) -> "KV8":
+        """Pools of zeros; block_table [B, max_pages] and seq_len [B]: int32 device tensors."""
+        pool = lambda *s: torch.zeros((n_layers, n_pages, n_kv_heads, page_size, *s), dtype=torch.uint8, device="cuda")
+        return KV8(pool(head_dim), pool(head_dim), pool().fill_(127), pool().fill_(127), block_table, seq_len, seq_len_bound)
+
+    def c(self, layer: int = 0) -> KV8C:
+        """The C handle of the layers from `layer` on."""
+        L, n_pages, n_kv, page, d = self.k_pool.shape
+        assert 0 <= layer < L and self.block_table.dtype == torch.int32 and self.seq_len.dtype == torch.int32
+        assert self.v_pool.shape == self.k_pool.shape and self.k_exp.shape == self.v_exp.shape == self.k_pool.shape[:4]
+        assert all(t.element_size() == 1 for t in (self.k_pool, self.v_pool, self.k_exp, self.v_exp))
+        assert self.block_table.shape[0] == self.seq_len.shape[0]
+        rows = layer * n_pages * n_kv * page
+        at = lambda t, off: C.c_void_p(_ptr(t).value + off)
+        return KV8C(at(self.k_pool, rows * d), at(self.v_pool, rows * d), at(self.k_exp, rows), at(self.v_exp, rows), n_pages, _ptr(self.block_table),
+                    _ptr(self.seq_len), self.block_table.shape[1], int(self.seq_len_bound))
+
+
+def _rows(t: torch.Tensor):
+    """(pointer, elements between rows) of [B, n, width] rows that may lie in wider ones."""
+    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1)), "rows must be evenly spaced"
+    return C.c_void_p(t.data_ptr()), t.stride(1)
+
+
+def _dtype_ok(dtype_code, *tensors):
+    assert all(t is None or t.dtype == torch_dtype(dtype_code) for t in tensors), "tensors must be of the given type"
+
+
+def kv8_write(dtype_code, n_q_heads, rope_theta, qkv, bias, depth, kv: KV8, layer, q_out):
+    """tlt_kv8_write: qkv [B, n, (Hq+2Hkv)*d], bias [(Hq+2Hkv)*d] or None, depth [B, n] int32 or None (a chain), q_out [B, n, Hq*d] (contiguous, or
+    the first Hq*d columns of wider rows: qkv[..., :Hq*d] itself)."""
+    B, n, width = qkv.shape
+    _, _, n_kv, page, d = kv.k_pool.shape
+    _dtype_ok(dtype_code, qkv, bias, q_out)
+    assert width == (n_q_heads + 2 * n_kv) * d and q_out.shape == (B, n, n_q_heads * d) and kv.seq_len.shape[0] == B
+    assert (bias is None or bias.shape == (width,)) and (depth is None or (depth.shape == (B, n) and depth.dtype == torch.int32))
+    q, stride = _rows(q_out)
+    kvc = kv.c(layer)
+    rc = load().tlt_kv8_write(_stream(), dtype_code, B, n, n_q_heads, n_kv, d, page, rope_theta, _ptr(qkv), _ptr(bias), _ptr(depth), C.byref(kvc), q, stride)
+    if rc:
+        raise TltError(rc, "tlt_kv8_write")
+
+
+def kv8_attention_workspace(B, n, n_q_heads, n_kv_heads, head_dim, max_ctx) -> torch.Tensor:
+    nbytes = load().tlt_kv8_attention_workspace_bytes(B, n, n_q_heads, n_kv_heads, head_dim, max_ctx)
+    if nbytes == 0:
+        raise TltError(-1, "tlt_kv8_attention_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
+def kv8_attention(dtype_code, n_q_heads, q, anc_mask, kv: KV8, layer, out, ws, impl=-1):
+    """tlt_kv8_attention: q [B, n, Hq*d] (rows as kv8_write's q_out), anc_mask [B, n] int64 or None (a chain), out [B, n, Hq*d]."""
+    B, n, width = q.shape
+    _, _, n_kv, page, d = kv.k_pool.shape
+    _dtype_ok(dtype_code, q, out)
+    assert width == n_q_heads * d and out.shape == q.shape and kv.seq_len.shape[0] == B
+    assert anc_mask is None or (anc_mask.shape == (B, n) and anc_mask.element_size() == 8)
+    qp, stride = _rows(q)
+    kvc = kv.c(layer)
+    rc = load().tlt_kv8_attention(_stream(), dtype_code, B, n, n_q_heads, n_kv, d, page, qp, stride, _ptr(anc_mask), C.byref(kvc), _ptr(out), _ptr(ws),
+                                  ws.numel() * ws.element_size(), impl)
+    if rc:
+        raise TltError(rc, "tlt_kv8_attention")
+
+
+def kv8_commit(kv: KV8, accept_len, path_idx):
+    """tlt_kv8_commit over all layers: accept_len [B], path_idx [B, stride] int32.  kv.seq_len_bound is left to the caller, as in kv_commit."""
+    L, _, n_kv, page, d = kv.k_pool.shape
+    B, stride = path_idx.shape
+    assert accept_len.shape == (B,) and kv.seq_len.shape[0] == B and accept_len.dtype == path_idx.dtype == torch.int32
+    kvc = kv.c()
+    rc = load().tlt_kv8_commit(_stream(), B, L, n_kv, d, page, C.byref(kvc), _ptr(accept_len), _ptr(path_idx), stride)
+    if rc:
+        raise TltError(rc, "tlt_kv8_commit")
+
+
+def kv8_read(dtype_code, kv: KV8, first, count, out_k, out_v):
+    """tlt_kv8_read over all layers: first [B] int32, count [B] int32 or None, out_k / out_v [L, B, n, Hkv, d] of dtype_code's type."""
+    L, _, n_kv, page, d = kv.k_pool.shape
+    B, n = out_k.shape[1], out_k.shape[2]
+    _dtype_ok(dtype_code, out_k, out_v)
+    assert out_k.shape == out_v.shape == (L, B, n, n_kv, d) and kv.seq_len.shape[0] == B and first.shape == (B,) and first.dtype == torch.int32
+    assert count is None or (count.shape == (B,) and count.dtype == torch.int32)
+    kvc = kv.c()
+    rc = load().tlt_kv8_read(_stream(), dtype_code, L, B, n, n_kv, d, page, C.byref(kvc), _ptr(first), _ptr(count), _ptr(out_k), _ptr(out_v))
+    if rc:
+        raise TltError(rc, "tlt_kv8_read")
 
 
 def gemm_argmax(A, W, ws, out):

@@ -1183,6 +1183,97 @@ int tlt_attention(void* stream, int dtype, int B, int n, int n_q_heads, int n_kv
     return e == hipSuccess ? TLT_OK : (e == hipErrorInvalidValue ? TLT_ESHAPE : TLT_EHIP);
 }
 
+// What the calls on an 8-bit cache ask of their sizes and of its handle; rows_ahead: new rows behind seq_len_bound.
+static int check_kv8(const tlt_kv8* kv, int B, int n_kv_heads, int head_dim, int page_size, int rows_ahead) {
+    if (B < 1 || B > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || head_dim < 64 || head_dim % 64 || head_dim > 256 || page_size < 1) return TLT_EINVAL;
+    if (!kv || !kv->k_pool || !kv->v_pool || !kv->k_exp || !kv->v_exp || !kv->block_table || !kv->seq_len || kv->n_pages < 1 || kv->max_pages < 1 ||
+        kv->seq_len_bound < 0 || (((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool) & 15) != 0)
+        return TLT_EINVAL;
+    return (int64_t)kv->seq_len_bound + rows_ahead > (int64_t)kv->max_pages * page_size ? TLT_ENOPAGES : TLT_OK;
+}
+
+static KV8Layer kv8_layer(const tlt_kv8* kv, int n_kv_heads, int head_dim, int page_size) {
+    KV8Layer k;
+    k.k = (uint8_t*)kv->k_pool;
+    k.v = (uint8_t*)kv->v_pool;
+    k.k_exp = (uint8_t*)kv->k_exp;
+    k.v_exp = (uint8_t*)kv->v_exp;
+    k.n_pages = kv->n_pages;
+    k.block_table = kv->block_table;
+    k.seq_len = kv->seq_len;
+    k.max_pages = kv->max_pages;
+    k.page_size = page_size;
+    k.n_kv = n_kv_heads;
+    k.d = head_dim;
+    k.seq_len_bound = kv->seq_len_bound;
+    return k;
+}
+
+static bool heads_ok(int n_q_heads, int n_kv_heads) { return n_kv_heads >= 1 && n_q_heads >= 1 && n_q_heads <= 65535 && n_q_heads % n_kv_heads == 0; }
+
+// rows of n_q_heads * head_dim elements, `stride` apart, that kernels move in 16-byte pieces
+static bool q_rows_ok(const void* q, int64_t stride, int dtype, int n_q_heads, int head_dim) {
+    return q && ((uintptr_t)q & 15) == 0 && stride >= (int64_t)n_q_heads * head_dim && stride % (dtype == TLT_F32 ? 4 : 8) == 0;
+}
+
+int tlt_kv8_write(void* stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size, float rope_theta, const void* qkv,
+                  const void* bqkv, const int32_t* depth, const tlt_kv8* kv, void* q_out, int64_t q_stride) {
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || n < 1 || !(rope_theta > 0.f) || !heads_ok(n_q_heads, n_kv_heads) || !qkv ||
+        (((uintptr_t)qkv | (uintptr_t)bqkv) & 15) != 0)
+        return TLT_EINVAL;
+    const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, n);
+    if (rc) return rc;
+    if (!q_rows_ok(q_out, q_stride, dtype, n_q_heads, head_dim) || (int64_t)B * n > 0x7fffffff) return TLT_EINVAL;
+    const hipError_t e = kv8_write((hipStream_t)stream, dtype, B, n, kv8_layer(kv, n_kv_heads, head_dim, page_size), qkv, bqkv, depth, n_q_heads, rope_theta,
+                                   q_out, q_stride);
+    return e == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
+size_t tlt_kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int max_ctx) {
+    if (B < 1 || B > 65535 || n < 1 || n > TLT_MAX_TREE || !heads_ok(n_q_heads, n_kv_heads) || head_dim < 64 || head_dim % 64 || head_dim > 256 || max_ctx < 1)
+        return 0;
+    return kv8_attention_workspace_bytes(B, n, n_q_heads, n_kv_heads, head_dim, max_ctx);
+}
+
+int tlt_kv8_attention(void* stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size, const void* q, int64_t q_stride,
+                      const uint64_t* anc_mask, const tlt_kv8* kv, void* out, void* ws, size_t ws_bytes, int impl) {
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || n < 1 || n > TLT_MAX_TREE || !heads_ok(n_q_heads, n_kv_heads) || !out || ((uintptr_t)out & 15) != 0 || !ws ||
+        ((uintptr_t)ws & 255) != 0 || impl < -1 || impl > 0)
+        return TLT_EINVAL;
+    const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, n);
+    if (rc) return rc;
+    if (!q_rows_ok(q, q_stride, dtype, n_q_heads, head_dim)) return TLT_EINVAL;
+    KV8Rows rows;
+    rows.B = B;
+    rows.n = n;
+    rows.mask = anc_mask;
+    const hipError_t e = kv8_attention((hipStream_t)stream, dtype, rows, kv8_layer(kv, n_kv_heads, head_dim, page_size), q, q_stride, out, n_q_heads, ws,
+                                       ws_bytes, impl);
+    return e == hipSuccess ? TLT_OK : (e == hipErrorInvalidValue ? TLT_ESHAPE : TLT_EHIP);
+}
+
+int tlt_kv8_commit(void* stream, int B, int n_layers, int n_kv_heads, int head_dim, int page_size, const tlt_kv8* kv, const int32_t* accept_len,
+                   const int32_t* path_idx, int stride) {
+    if (n_layers < 1 || n_layers > 65535 || !accept_len || !path_idx || stride < 1) return TLT_EINVAL;
+    const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, 0);
+    if (rc) return rc;
+    if ((int64_t)n_layers * n_kv_heads > (1 << 24)) return TLT_EINVAL;
+    const hipError_t e = kv8_commit((hipStream_t)stream, n_layers, B, kv8_layer(kv, n_kv_heads, head_dim, page_size), kv->seq_len, accept_len, path_idx, stride);
+    return e == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
+int tlt_kv8_read(void* stream, int dtype, int n_layers, int B, int n, int n_kv_heads, int head_dim, int page_size, const tlt_kv8* kv, const int32_t* first,
+                 const int32_t* count, void* out_k, void* out_v) {
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || n_layers < 1 || n < 1 || !first || !out_k || !out_v || (((uintptr_t)out_k | (uintptr_t)out_v) & 15) != 0)
+        return TLT_EINVAL;
+    const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, 0);
+    if (rc) return rc;
+    // (a wave per 16 rows, kv head, sequence and layer; the count times 64 threads has to fit a grid)
+    if (n > (1 << 30) || (double)n_layers * B * (n / 16 + 1) * n_kv_heads >= (double)(1 << 25)) return TLT_EINVAL;
+    const hipError_t e = kv8_read((hipStream_t)stream, dtype, n_layers, B, n, kv8_layer(kv, n_kv_heads, head_dim, page_size), first, count, out_k, out_v);
+    return e == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
 int tlt_gemm_glu(void* stream, int M, int N, int K, const void* A, const void* Wg, const void* Wu, void* act) {
     if (M < 1 || N < 1 || K < 1 || !A || !Wg || !Wu || !act) return TLT_EINVAL;
     if (!gemm_glu_supported(TLT_BF16, M, N, K, A, Wg, Wu) || ((uintptr_t)act & 7) != 0) return TLT_ENOTIMPL;   // (8-byte stores)

@@ -157,6 +157,32 @@ bool attention_rope_supported(int dtype, const Rows& rows, const KVLayer& kv, co
 hipError_t attention_rope(hipStream_t s, const Rows& rows, const KVLayer& kv, const void* qkv, void* out, int n_q_heads, float theta, const void* bias,
                           const RopeTable& tab, bool from_table);
 
+// ---- kv8.hip: the 8-bit cache (its format stands there)
+struct KV8Layer {
+    uint8_t *k = nullptr, *v = nullptr;           // one layer's codes [n_pages][n_kv][page][d] (of several layers: the first one's)
+    uint8_t *k_exp = nullptr, *v_exp = nullptr;   // exponent bytes [n_pages][n_kv][page]
+    int64_t n_pages = 0;
+    const int32_t* block_table = nullptr;
+    const int32_t* seq_len = nullptr;
+    int max_pages = 0, page_size = 16, n_kv = 0, d = 0;
+    int seq_len_bound = 0;
+};
+// Rows [B][n]: row (b, i) is slot seq_len[b] + i and attends to every slot < seq_len[b] and to slot seq_len[b] + j (j < n) when bit j of its
+// mask is set; a null mask means j <= i.  n <= 64.
+struct KV8Rows {
+    int B = 0, n = 0;
+    const uint64_t* mask = nullptr;
+};
+// depth null: row i is at position seq_len[b] + i.  q_out: rotated queries, rows q_stride elements apart (may be qkv itself)
+hipError_t kv8_write(hipStream_t s, int dtype, int B, int n, const KV8Layer& kv, const void* qkv, const void* bias, const int32_t* depth, int n_q_heads,
+                     float theta, void* q_out, int64_t q_stride);
+hipError_t kv8_read(hipStream_t s, int dtype, int n_layers, int B, int n, const KV8Layer& kv, const int32_t* first, const int32_t* count, void* out_k,
+                    void* out_v);
+hipError_t kv8_commit(hipStream_t s, int n_layers, int B, const KV8Layer& kv, int32_t* seq_len, const int32_t* accept_len, const int32_t* path_idx, int stride);
+size_t kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int d, int max_ctx);
+hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV8Layer& kv, const void* q, int64_t q_stride, void* out, int n_q_heads, void* ws,
+                         size_t ws_bytes, int impl);
+
 // ---- sample.hip
 // (scratch, may be null: 8-byte aligned device memory the call may use, M * 256 bytes at most, to spread few rows over the chip)
 hipError_t row_argmax(hipStream_t s, int M, int V, const float* logits, int32_t* out, void* scratch = nullptr,
