@@ -241,6 +241,8 @@ def _own(s):
         s["kv"] = tlt.KV8(s["k"], s["v"], s["k_exp"], s["v_exp"], s["table"], s["seq_len"], s["bound"])
         if kind in ("attend", "step"):
             s["ws"] = tlt.kv8_attention_workspace(s["B"], s["n"], Hq, s["Hkv"], s["d"], s["bound"] + s["n"])
+        if kind in ("write", "step"):   # (a buffer of their own: with one row in all, s["q"] lies inside s["qkv"])
+            s["rotated"] = torch.empty((s["B"], s["n"], Hq * s["d"]), dtype=s["dtype"], device="cuda")
     kv = s["kv"]
     if kind == "attend":
         tlt.kv8_attention(code, Hq, s["q"], s["mask"], kv, 0, s["out"], s["ws"])
@@ -250,12 +252,12 @@ def _own(s):
         return s["k_rows"], s["v_rows"]
     s["seq_len"].copy_(s["seq_len0"])
     if kind in ("write", "step"):
-        tlt.kv8_write(code, Hq, THETA, s["qkv"], s["bias"], s["depth"], kv, 0, s["q"])
+        tlt.kv8_write(code, Hq, THETA, s["qkv"], s["bias"], s["depth"], kv, 0, s["rotated"])
     if kind == "write":
         tlt.kv8_read(tlt.TLT_BF16, kv, s["seq_len0"], None, s["k_rows"], s["v_rows"])
-        return s["q"], s["k_rows"], s["v_rows"]
+        return s["rotated"], s["k_rows"], s["v_rows"]
     if kind == "step":
-        tlt.kv8_attention(code, Hq, s["q"], s["mask"], kv, 0, s["out"], s["ws"])
+        tlt.kv8_attention(code, Hq, s["rotated"], s["mask"], kv, 0, s["out"], s["ws"])
     tlt.kv8_commit(kv, s["accept_len"], s["path"])
     tlt.kv8_read(tlt.TLT_BF16, kv, s["seq_len0"], s["count"], s["k_rows"], s["v_rows"])
     rows = (s["seq_len"], s["k_rows"], s["v_rows"])
