@@ -531,8 +531,10 @@ class KV8:
 
 def _rows(t: torch.Tensor):
     """(pointer, elements between rows) of [B, n, width] rows that may lie in wider ones."""
-    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1)), "rows must be evenly spaced"
-    return C.c_void_p(t.data_ptr()), t.stride(1)
+    B, n, width = t.shape
+    step = t.stride(1) if n > 1 else (t.stride(0) if B > 1 else width)   # (a dimension of one element may have any stride)
+    assert t.is_cuda and t.stride(2) == 1 and (B == 1 or t.stride(0) == n * step), "rows must be evenly spaced"
+    return C.c_void_p(t.data_ptr()), step
 
 
 def _dtype_ok(dtype_code, *tensors):

@@ -139,6 +139,23 @@ def test_write_in_place_and_without_pages():
         assert all(torch.equal(c.kv.__dict__[x][0, pg], kept[x][0, pg]) for x in kept)
 
 
+def test_one_row_of_queries_inside_their_projection():
+    """With one node the queries' rows are as far apart as the sequences are."""
+    d, Hq, Hkv = 128, 4, 2
+    for B in (1, 3):
+        c = m.Cache([20 + b for b in range(B)], 1, Hkv, d, 16, seed=2)
+        qkv = np.random.default_rng(0).standard_normal((B, 1, (Hq + 2 * Hkv) * d)).astype(np.float32)
+        print("one row each,", B, flush=True)
+        q, _ = run_write(c, "bf16", Hq, qkv, None, None, 1e6)
+        q2, whole = run_write(c, "bf16", Hq, qkv, None, None, 1e6, in_place=True)
+        np.testing.assert_array_equal(q, q2)
+        out = [torch.zeros((B, 1, Hq * d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        ws = tlt.kv8_attention_workspace(B, 1, Hq, Hkv, d, 30)
+        tlt.kv8_attention(tlt.TLT_BF16, Hq, whole[..., :Hq * d], None, c.kv, 0, out[0], ws)
+        tlt.kv8_attention(tlt.TLT_BF16, Hq, whole[..., :Hq * d].clone(memory_format=torch.contiguous_format), None, c.kv, 0, out[1], ws)
+        assert torch.equal(*out) and out[0].any()
+
+
 # ---- read
 
 @pytest.mark.parametrize("dtype,Hkv,d,page,n,L", [("bf16", 4, 128, 16, 37, 3), ("fp32", 2, 64, 16, 1, 2), ("fp32", 1, 192, 5, 20, 1), ("bf16", 3, 256, 7, 16, 2)])
