@@ -498,60 +498,88 @@ def attention(dtype_code, n_q_heads, page_size, qkv, anc_mask, kv: KV, out, ws, 
                                 C.byref(kvc), _ptr(out), _ptr(ws), ws.numel(), impl)
 
 
-@dataclasses.dataclass
 class KV8:
     """8-bit paged KV cache of one model (tlt_kv8): codes [L, n_pages, Hkv, page, d] and exponent bytes [L, n_pages, Hkv, page] of keys and
-    values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV."""
-    k_pool: torch.Tensor
-    v_pool: torch.Tensor
-    k_exp: torch.Tensor
-    v_exp: torch.Tensor
-    block_table: torch.Tensor
-    seq_len: torch.Tensor
-    seq_len_bound: int
+    values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV.  A field is checked when it is set, the
+    tensors' addresses are taken at every call."""
+    _TENSORS = ("k_pool", "v_pool", "k_exp", "v_exp", "block_table", "seq_len")
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, block_table: torch.Tensor,
+                 seq_len: torch.Tensor, seq_len_bound: int):
+        given = locals()
+        for name in self._TENSORS:
+            object.__setattr__(self, name, given[name])
+        self._check()
+        self.seq_len_bound = int(seq_len_bound)
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name in self._TENSORS:
+            self._check()
+
+    def _check(self):
+        k = self.k_pool
+        assert k.dim() == 5 and self.v_pool.shape == k.shape and self.k_exp.shape == self.v_exp.shape == k.shape[:4], "pools' shapes"
+        assert all(t.element_size() == 1 for t in (k, self.v_pool, self.k_exp, self.v_exp)), "pools hold bytes"
+        assert self.block_table.dtype == self.seq_len.dtype == torch.int32 and self.block_table.dim() == 2
+        assert self.seq_len.shape == self.block_table.shape[:1]
+        tensors = [getattr(self, name) for name in self._TENSORS]
+        assert all(t.is_cuda and t.is_contiguous() and t.device == k.device for t in tensors), "device tensors must be contiguous CUDA/HIP tensors"
+        # (layers, pages, kv heads, page size, head_dim), sequences, entries of the table per sequence
+        object.__setattr__(self, "dims", tuple(k.shape))
+        object.__setattr__(self, "table_dims", tuple(self.block_table.shape))
 
     @staticmethod
     def empty(n_layers, n_pages, n_kv_heads, page_size, head_dim, block_table, seq_len, seq_len_bound) -> "KV8":
         """Pools of zeros; block_table [B, max_pages] and seq_len [B]: int32 device tensors."""
-        pool = lambda *s: torch.zeros((n_layers, n_pages, n_kv_heads, page_size, *s), dtype=torch.uint8, device="cuda")
+        pool = lambda *s: torch.zeros((n_layers, n_pages, n_kv_heads, page_size, *s), dtype=torch.uint8, device=block_table.device)
         return KV8(pool(head_dim), pool(head_dim), pool().fill_(127), pool().fill_(127), block_table, seq_len, seq_len_bound)
 
     def c(self, layer: int = 0) -> KV8C:
         """The C handle of the layers from `layer` on."""
-        L, n_pages, n_kv, page, d = self.k_pool.shape
-        assert 0 <= layer < L and self.block_table.dtype == torch.int32 and self.seq_len.dtype == torch.int32
-        assert self.v_pool.shape == self.k_pool.shape and self.k_exp.shape == self.v_exp.shape == self.k_pool.shape[:4]
-        assert all(t.element_size() == 1 for t in (self.k_pool, self.v_pool, self.k_exp, self.v_exp))
-        assert self.block_table.shape[0] == self.seq_len.shape[0]
+        L, n_pages, n_kv, page, d = self.dims
+        if not 0 <= layer < L:
+            raise IndexError(f"layer {layer} of {L}")
         rows = layer * n_pages * n_kv * page
-        at = lambda t, off: C.c_void_p(_ptr(t).value + off)
-        return KV8C(at(self.k_pool, rows * d), at(self.v_pool, rows * d), at(self.k_exp, rows), at(self.v_exp, rows), n_pages, _ptr(self.block_table),
-                    _ptr(self.seq_len), self.block_table.shape[1], int(self.seq_len_bound))
+        return KV8C(self.k_pool.data_ptr() + rows * d, self.v_pool.data_ptr() + rows * d, self.k_exp.data_ptr() + rows, self.v_exp.data_ptr() + rows, n_pages,
+                    self.block_table.data_ptr(), self.seq_len.data_ptr(), self.table_dims[1], self.seq_len_bound)
 
 
-def _rows(t: torch.Tensor):
-    """(pointer, elements between rows) of [B, n, width] rows that may lie in wider ones."""
-    B, n, width = t.shape
+def _stream_of(kv: KV8):
+    """The current stream of the cache's device, which has to be the current one."""
+    device = kv.k_pool.get_device()
+    assert device == torch.cuda.current_device(), "the cache lies on another device than the current one"
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a tenth of what current_stream()'s object costs, 2.8 us)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _addr(t: Optional[torch.Tensor], kv: KV8, shape, dtype):
+    """The address of a contiguous tensor beside the cache, of this shape and type (a type, or the bytes of an element); None stays None."""
+    if t is None:
+        return None
+    assert t.shape == shape and (t.dtype is dtype or t.element_size() == dtype) and t.is_contiguous() and t.get_device() == kv.k_pool.get_device(), \
+        f"a contiguous tensor {tuple(shape)} of {dtype} on the cache's device"
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, kv: KV8, shape, dtype):
+    """(address, elements between rows) of rows [B, n, width] that may lie in wider ones."""
+    assert t.shape == shape and t.dtype is dtype and t.get_device() == kv.k_pool.get_device(), f"rows {tuple(shape)} of {dtype} on the cache's device"
+    B, n, width = shape
     step = t.stride(1) if n > 1 else (t.stride(0) if B > 1 else width)   # (a dimension of one element may have any stride)
-    assert t.is_cuda and t.stride(2) == 1 and (B == 1 or t.stride(0) == n * step), "rows must be evenly spaced"
-    return C.c_void_p(t.data_ptr()), step
-
-
-def _dtype_ok(dtype_code, *tensors):
-    assert all(t is None or t.dtype == torch_dtype(dtype_code) for t in tensors), "tensors must be of the given type"
+    assert t.stride(2) == 1 and (B == 1 or t.stride(0) == n * step), "rows must be evenly spaced"
+    return t.data_ptr(), step
 
 
 def kv8_write(dtype_code, n_q_heads, rope_theta, qkv, bias, depth, kv: KV8, layer, q_out):
     """tlt_kv8_write: qkv [B, n, (Hq+2Hkv)*d], bias [(Hq+2Hkv)*d] or None, depth [B, n] int32 or None (a chain), q_out [B, n, Hq*d] (contiguous, or
     the first Hq*d columns of wider rows: qkv[..., :Hq*d] itself)."""
-    B, n, width = qkv.shape
-    _, _, n_kv, page, d = kv.k_pool.shape
-    _dtype_ok(dtype_code, qkv, bias, q_out)
-    assert width == (n_q_heads + 2 * n_kv) * d and q_out.shape == (B, n, n_q_heads * d) and kv.seq_len.shape[0] == B
-    assert (bias is None or bias.shape == (width,)) and (depth is None or (depth.shape == (B, n) and depth.dtype == torch.int32))
-    q, stride = _rows(q_out)
-    kvc = kv.c(layer)
-    rc = load().tlt_kv8_write(_stream(), dtype_code, B, n, n_q_heads, n_kv, d, page, rope_theta, _ptr(qkv), _ptr(bias), _ptr(depth), C.byref(kvc), q, stride)
+    _, _, n_kv, page, d = kv.dims
+    B, n, width = kv.table_dims[0], qkv.shape[1], (n_q_heads + 2 * n_kv) * d
+    dt = torch_dtype(dtype_code)
+    q, step = _rows(q_out, kv, (B, n, n_q_heads * d), dt)
+    rc = load().tlt_kv8_write(_stream_of(kv), dtype_code, B, n, n_q_heads, n_kv, d, page, rope_theta, _addr(qkv, kv, (B, n, width), dt),
+                              _addr(bias, kv, (width,), dt), _addr(depth, kv, (B, n), torch.int32), kv.c(layer), q, step)
     if rc:
         raise TltError(rc, "tlt_kv8_write")
 
@@ -565,39 +593,34 @@ def kv8_attention_workspace(B, n, n_q_heads, n_kv_heads, head_dim, max_ctx) -> t
 
 def kv8_attention(dtype_code, n_q_heads, q, anc_mask, kv: KV8, layer, out, ws, impl=-1):
     """tlt_kv8_attention: q [B, n, Hq*d] (rows as kv8_write's q_out), anc_mask [B, n] int64 or None (a chain), out [B, n, Hq*d]."""
-    B, n, width = q.shape
-    _, _, n_kv, page, d = kv.k_pool.shape
-    _dtype_ok(dtype_code, q, out)
-    assert width == n_q_heads * d and out.shape == q.shape and kv.seq_len.shape[0] == B
-    assert anc_mask is None or (anc_mask.shape == (B, n) and anc_mask.element_size() == 8)
-    qp, stride = _rows(q)
-    kvc = kv.c(layer)
-    rc = load().tlt_kv8_attention(_stream(), dtype_code, B, n, n_q_heads, n_kv, d, page, qp, stride, _ptr(anc_mask), C.byref(kvc), _ptr(out), _ptr(ws),
-                                  ws.numel() * ws.element_size(), impl)
+    _, _, n_kv, page, d = kv.dims
+    B, n = kv.table_dims[0], q.shape[1]
+    shape, dt = (B, n, n_q_heads * d), torch_dtype(dtype_code)
+    qp, step = _rows(q, kv, shape, dt)
+    assert ws.is_contiguous() and ws.get_device() == kv.k_pool.get_device()
+    rc = load().tlt_kv8_attention(_stream_of(kv), dtype_code, B, n, n_q_heads, n_kv, d, page, qp, step, _addr(anc_mask, kv, (B, n), 8), kv.c(layer),
+                                  _addr(out, kv, shape, dt), ws.data_ptr(), ws.numel() * ws.element_size(), impl)
     if rc:
         raise TltError(rc, "tlt_kv8_attention")
 
 
 def kv8_commit(kv: KV8, accept_len, path_idx):
     """tlt_kv8_commit over all layers: accept_len [B], path_idx [B, stride] int32.  kv.seq_len_bound is left to the caller, as in kv_commit."""
-    L, _, n_kv, page, d = kv.k_pool.shape
-    B, stride = path_idx.shape
-    assert accept_len.shape == (B,) and kv.seq_len.shape[0] == B and accept_len.dtype == path_idx.dtype == torch.int32
-    kvc = kv.c()
-    rc = load().tlt_kv8_commit(_stream(), B, L, n_kv, d, page, C.byref(kvc), _ptr(accept_len), _ptr(path_idx), stride)
+    L, _, n_kv, page, d = kv.dims
+    B, stride = kv.table_dims[0], path_idx.shape[1]
+    rc = load().tlt_kv8_commit(_stream_of(kv), B, L, n_kv, d, page, kv.c(), _addr(accept_len, kv, (B,), torch.int32), _addr(path_idx, kv, (B, stride), torch.int32),
+                               stride)
     if rc:
         raise TltError(rc, "tlt_kv8_commit")
 
 
 def kv8_read(dtype_code, kv: KV8, first, count, out_k, out_v):
     """tlt_kv8_read over all layers: first [B] int32, count [B] int32 or None, out_k / out_v [L, B, n, Hkv, d] of dtype_code's type."""
-    L, _, n_kv, page, d = kv.k_pool.shape
-    B, n = out_k.shape[1], out_k.shape[2]
-    _dtype_ok(dtype_code, out_k, out_v)
-    assert out_k.shape == out_v.shape == (L, B, n, n_kv, d) and kv.seq_len.shape[0] == B and first.shape == (B,) and first.dtype == torch.int32
-    assert count is None or (count.shape == (B,) and count.dtype == torch.int32)
-    kvc = kv.c()
-    rc = load().tlt_kv8_read(_stream(), dtype_code, L, B, n, n_kv, d, page, C.byref(kvc), _ptr(first), _ptr(count), _ptr(out_k), _ptr(out_v))
+    L, _, n_kv, page, d = kv.dims
+    B, n, dt = kv.table_dims[0], out_k.shape[2], torch_dtype(dtype_code)
+    shape = (L, B, n, n_kv, d)
+    rc = load().tlt_kv8_read(_stream_of(kv), dtype_code, L, B, n, n_kv, d, page, kv.c(), _addr(first, kv, (B,), torch.int32), _addr(count, kv, (B,), torch.int32),
+                             _addr(out_k, kv, shape, dt), _addr(out_v, kv, shape, dt))
     if rc:
         raise TltError(rc, "tlt_kv8_read")
 
