@@ -408,12 +408,21 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
     const int lane = threadIdx.x & 63;
     auto len_of = [&](int b) { return min(max(seq_len[b], 0), len_bound); };
     auto ceil_div = [](int x, int T) { return (int)__umulhi((uint32_t)(x + T - 1), 0xffffffffu / (uint32_t)T + 1u); };   // (exact: x < 2^26, 2 <= T <= 64)
-    auto cut = [&](int tiles, int k, int c) { return (int)((int64_t)tiles * c / k); };
-    if (B > kPlanned) {
-        const int b = item % B, c = item / B, len = len_of(b), tiles = (len + n + kKT - 1) / kKT, k = (tiles + sp.t_max - 1) / sp.t_max;
-        if (c >= k) return false;
-        out = KV8Item{b, len, cut(tiles, k, c), cut(tiles, k, c + 1), item, b, k};
+    // (everything about an item is uniform, and said to be)
+    auto give = [&](int b, int len, int tiles, int slot, int first, int k) {
+        const int c = __builtin_amdgcn_readfirstlane(B > kPlanned ? slot / B : slot - first), per = tiles / k, more = tiles - per * k;   // the first `more` ranges are one tile longer
+        out.b = __builtin_amdgcn_readfirstlane(b);
+        out.ctx = __builtin_amdgcn_readfirstlane(len);
+        out.lo = __builtin_amdgcn_readfirstlane(c * per + min(c, more));
+        out.hi = __builtin_amdgcn_readfirstlane(out.lo + per + (c < more ? 1 : 0));
+        out.slot = __builtin_amdgcn_readfirstlane(slot);
+        out.first = __builtin_amdgcn_readfirstlane(first);
+        out.k = __builtin_amdgcn_readfirstlane(k);
         return true;
+    };
+    if (B > kPlanned) {
+        const int b = item % B, len = len_of(b), tiles = (len + n + kKT - 1) / kKT, k = (tiles + sp.t_max - 1) / sp.t_max;
+        return item / B < k && give(b, len, tiles, item, b, k);
     }
     int len[kPlanned / 64], tiles[kPlanned / 64];
 #pragma unroll
@@ -429,11 +438,20 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
             if (64 * j < B) s += ceil_div(tiles[j], T);
         return wave_sum_i(s);
     };
-    const int most = (items(sp.t_max) + sp.slots - 1) / sp.slots * sp.slots;
-    int T = sp.t_min, up = sp.t_max;
-    while (T < up) {   // (longer ranges never make more items)
-        const int mid = (T + up) >> 1;
-        if (items(mid) <= most) up = mid; else T = mid + 1;
+    int T = sp.t_min;
+    if (items(T) > sp.slots) {
+        const int most = (items(sp.t_max) + sp.slots - 1) / sp.slots * sp.slots;
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPlanned / 64; ++j) sum += tiles[j];
+        sum = wave_sum_i(sum);
+        // items(T) is at least sum / T and at most sum / T + B, and longer ranges never make more items
+        T = min(max(T, (sum + most - 1) / most), sp.t_max);
+        int up = most > B ? min(max((sum + most - B - 1) / (most - B), T), sp.t_max) : sp.t_max;
+        while (T < up) {
+            const int mid = (T + up) >> 1;
+            if (items(mid) <= most) up = mid; else T = mid + 1;
+        }
     }
     T = __builtin_amdgcn_readfirstlane(T);
     int base = 0;
@@ -450,9 +468,7 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
         if (hit) {
             const int l = __ffsll((unsigned long long)hit) - 1;
             const int kk = __builtin_amdgcn_readlane(k, l), tt = __builtin_amdgcn_readlane(tiles[j], l);
-            const int first = base + __builtin_amdgcn_readlane(end, l) - kk, c = item - first;
-            out = KV8Item{64 * j + l, __builtin_amdgcn_readlane(len[j], l), cut(tt, kk, c), cut(tt, kk, c + 1), item, first, kk};
-            return true;
+            return give(64 * j + l, __builtin_amdgcn_readlane(len[j], l), tt, item, base + __builtin_amdgcn_readlane(end, l) - kk, kk);
         }
         base += __builtin_amdgcn_readlane(end, min(B - 64 * j, 64) - 1);
     }
@@ -484,37 +500,195 @@ struct KV8Seg {   // per sequence, for the joining kernel
     int first, k;
 };
 
-// Few rows (NT tiles of 16): bound by memory.  A wave owns every fourth tile of the item's range with all rows, takes codes from memory straight into
-// the registers that the products want (no LDS, no barrier until the end) and keeps the next tile's in flight: keys once the scores are done,
-// values once the sums are.  d is permuted alike on both sides of the first product (a key's row in two pieces of 16 bytes per lane); for the second one a lane
-// loads 8 bytes of each of its 8 keys, so that d = 8 * (lane % 16) + instruction, converts pairs of d, and pairs up keys by byte permutations.
-// The four waves are joined through LDS.
+// What a wave holds of NT tiles of rows: queries in the order of the keys' pieces, unnormalised sums, the weights' sums, the reference of the
+// exponentials.  Lane (l16, g4) has row l16 of a tile.
 template <int NT>
-__global__ __launch_bounds__(256) void kv8_attn_few_k(KV8Split sp, int n_q_heads, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv,
-                                                      uint16_t* __restrict__ out, KV8Seg* __restrict__ seg, float* __restrict__ part_o,
-                                                      float* __restrict__ part_ml, float scale_log2) {
+struct KV8Tiles {
+    u32x4_t q[NT][4];
+    f32x4_t acc[NT][8], l[NT];
+    float m[NT];
+};
+// Visibility of row r over the new rows
+__device__ __forceinline__ uint64_t kv8_mask(const KV8Rows& rows, int b, int G, int r) {
+    const int n = rows.n, i = r / G;
+    return r >= n * G ? 0ull : (rows.mask ? rows.mask[b * n + i] : (2ull << i) - 1ull) & (~0ull >> (64 - n));
+}
+template <int NT, typename F>   // row_of_tile(t): first row of tile t
+__device__ __forceinline__ void kv8_tiles(KV8Tiles<NT>& x, const KV8Rows& rows, int b, int kh, int G, const uint16_t* __restrict__ q, int64_t q_stride, F row_of_tile) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, n = rows.n;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int r = row_of_tile(t) + l16, i = r / G, g = r - i * G;
+        const bool on = r < n * G;
+        const uint16_t* p = q + (int64_t)(b * n + (on ? i : 0)) * q_stride + (kh * G + (on ? g : 0)) * kD + 16 * g4;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const u32x4_t z = {0u, 0u, 0u, 0u};
+            x.q[t][ks] = on ? *(const u32x4_t*)(p + (ks >> 1) * 64 + (ks & 1) * 8) : z;
+        }
+        x.m[t] = kNegBig;
+        x.l[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) x.acc[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+}
+// S^T of 16 keys, whose codes lane (l16, g4) has of key l16, pieces g4 and 4 + g4.  Values that are not finite: their codes are zero, the NaN comes through the
+// score, which only rows that see the key keep.
+template <int NT>
+__device__ __forceinline__ void kv8_scores(const KV8Tiles<NT>& x, u32x4_t c0, u32x4_t c1, uint32_t k_exp, uint32_t v_exp, f32x4_t* const (&sc)[NT]) {
+    const float scale = __uint_as_float((v_exp == 255u ? 255u : k_exp) << 23);
+    bf16x8_t kf[4];
+    kf[0] = __builtin_bit_cast(bf16x8_t, cvt8(c0[0], c0[1], scale));
+    kf[1] = __builtin_bit_cast(bf16x8_t, cvt8(c0[2], c0[3], scale));
+    kf[2] = __builtin_bit_cast(bf16x8_t, cvt8(c1[0], c1[1], scale));
+    kf[3] = __builtin_bit_cast(bf16x8_t, cvt8(c1[2], c1[3], scale));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        *sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) *sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], __builtin_bit_cast(bf16x8_t, x.q[t][ks]), *sc[t], 0, 0, 0);
+    }
+}
+// Scores sc[t][s][v] of keys t0 + 16 * s + 4 * g4 + v to weights, packed for the second product: k slot 4 * (s & 1) + v of half s / 2.  behind: t0 less the
+// context's length; edge: some keys are new rows or lie behind the last; mask_of(t, lane): visibility of the lane's row of tile t.
+// SN: groups of 16 keys.
+template <int SN, int NT, typename F>
+__device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][SN], u32x4_t (&pb)[NT][SN / 2], bool edge, int behind, F mask_of, float scale_log2, float lazy) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (edge) {
+            int ln = threadIdx.x & 63;
+            asm volatile("" : "+v"(ln));   // (worked out anew where it is wanted: kept through the loop, such values cost registers that the products need)
+            const uint64_t seen = seen_from(behind + 4 * (ln >> 4), mask_of(t, ln));
+#pragma unroll
+            for (int s = 0; s < SN; ++s)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sc[t][s][v] = seen >> (16 * s + v) & 1ull ? sc[t][s][v] : kNegBig;
+        }
+        float tmax = kNegBig;
+#pragma unroll
+        for (int s = 0; s < SN; ++s)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) tmax = fmaxf(tmax, sc[t][s][v]);
+        // the reference of the exponentials only has to keep them in range: it follows the maximum when some score exceeds it by 2^8
+        if (__builtin_amdgcn_ballot_w64(tmax > x.m[t] + lazy) != 0) {
+            const float m_new = fmaxf(x.m[t], group_max4(tmax));
+            const float alpha = __builtin_amdgcn_exp2f((x.m[t] - m_new) * scale_log2);
+            x.m[t] = m_new;
+            x.l[t] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) x.acc[t][dt] *= alpha;
+        }
+        const float mc = fmaxf(x.m[t], -1e29f) * scale_log2;   // (rows that have seen nothing yet: exp2(-1e30 * c + 1e29 * c) = 0)
+#pragma unroll
+        for (int s = 0; s < SN; ++s) {
+            float e[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(fmaf(sc[t][s][v], scale_log2, -mc));
+            pb[t][s >> 1][2 * (s & 1)] = pack_bf16x2(e[0], e[1]);       // weights are rounded to bf16 for the second product; their sum is that of the rounded ones
+            pb[t][s >> 1][2 * (s & 1) + 1] = pack_bf16x2(e[2], e[3]);
+        }
+    }
+}
+// O^T += V^T P^T over 32 keys: vc[sub][v] has 8 codes, d = 8 * l16 .., of key 16 * sub + 4 * g4 + v, byte v of ve[sub] its exponent.  Pairs of d are converted,
+// pairs of keys made by byte permutations; instruction dt has d = 8 * l16 + dt.
+template <int NT>
+__device__ __forceinline__ void kv8_sums(KV8Tiles<NT>& x, const u32x2_t (&vc)[2][4], uint32_t ve0, uint32_t ve1, const u32x4_t* const (&pb)[NT]) {
+    float scale[8];
+#pragma unroll
+    for (int a = 0; a < 8; ++a) {
+        const uint32_t e8 = ((a < 4 ? ve0 : ve1) >> (8 * (a & 3))) & 255u;
+        scale[a] = __uint_as_float((e8 == 255u ? 127u : e8) << 23);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t y[8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            const uint32_t w = vc[a >> 2][a & 3][c >> 1];
+            y[a] = c & 1 ? cvt2<true>(w, scale[a]) : cvt2<false>(w, scale[a]);
+        }
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            u32x4_t a;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) a[p] = __builtin_amdgcn_perm(y[2 * p + 1], y[2 * p], o ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                x.acc[t][2 * c + o] =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, *pb[t]), x.acc[t][2 * c + o], 0, 0, 0);
+        }
+    }
+    const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        x.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, *pb[t]), x.l[t], 0, 0, 0);
+}
+// Where a row's result goes: the output, or the partial results of its range
+struct KV8Out {
+    uint16_t* out;
+    float *part_o, *part_ml;
+    int n, n_q_heads, n_kv, r_pad;
+    __device__ __forceinline__ void put4(const KV8Item& it, int kh, int G, int r, int c, f32x4_t o, float M, float L) const {
+        if (it.k == 1) {
+            const float inv = L == 0.f ? 0.f : 1.0f / L;
+            const int i = r / G, g = r - i * G;
+            *(u32x2_t*)(out + ((int64_t)(it.b * n + i) * n_q_heads + kh * G + g) * kD + c) = u32x2_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+        } else {
+            const int64_t at = ((int64_t)it.slot * n_kv + kh) * r_pad + r;
+            *(f32x4_t*)(part_o + at * kD + c) = o;
+            if (c == 0) part_ml[at * 2] = M, part_ml[at * 2 + 1] = L;
+        }
+    }
+    // `COUNT` sums (8 or 32) of row r from column c on, their weights' sum L and reference M
+    template <int COUNT>
+    __device__ __forceinline__ void put(const KV8Item& it, int kh, int G, int r, int c, const float* o, float M, float L) const {
+        if (it.k == 1) {
+            const float inv = L == 0.f ? 0.f : 1.0f / L;
+            const int i = r / G, g = r - i * G;
+            uint16_t* p = out + ((int64_t)(it.b * n + i) * n_q_heads + kh * G + g) * kD + c;
+#pragma unroll
+            for (int e = 0; e < COUNT; e += 8)
+                *(u32x4_t*)(p + e) = u32x4_t{pack_bf16x2(o[e] * inv, o[e + 1] * inv), pack_bf16x2(o[e + 2] * inv, o[e + 3] * inv),
+                                             pack_bf16x2(o[e + 4] * inv, o[e + 5] * inv), pack_bf16x2(o[e + 6] * inv, o[e + 7] * inv)};
+        } else {
+            const int64_t at = ((int64_t)it.slot * n_kv + kh) * r_pad + r;
+#pragma unroll
+            for (int e = 0; e < COUNT; e += 4) *(f32x4_t*)(part_o + at * kD + c + e) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            if (c == 0) part_ml[at * 2] = M, part_ml[at * 2 + 1] = L;
+        }
+    }
+};
+
+// Few rows (NT tiles of 16): bound by memory.  A wave of the workgroup's four owns every fourth tile of the item's range with all rows, takes codes from
+// memory straight into the registers that the products want (no LDS, no barrier until the end) and keeps the next tile's in flight: keys once the
+// scores are done, values once the sums are.  The waves are joined through LDS.
+template <int NT>
+__global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
+                                                                      KV8Seg* __restrict__ seg, float scale_log2, float lazy) {
     constexpr int kPad = kD + 4;
     __shared__ __align__(16) float o_s[4][16][kPad];
-    __shared__ float m_s[4][16 * NT], l_s[4][16 * NT];
+    __shared__ float m_s[4][16], l_s[4][16];
     const int n_kv = kv.n_kv, kh = blockIdx.x % n_kv;
     KV8Item it;
     if (!kv8_item(kv.seq_len, rows.B, rows.n, kv.seq_len_bound, sp, blockIdx.x / n_kv, it)) return;   // uniform
-    const int b = it.b, ctx = it.ctx, n = rows.n, total = ctx + n;
+    const int b = it.b, ctx = it.ctx, total = ctx + rows.n;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
-    const int G = n_q_heads / n_kv, R = n * G;
+    const int G = to.n_q_heads / n_kv, R = rows.n * G;
     if (kh == 0 && it.slot == it.first && tid == 0) seg[b] = KV8Seg{it.first, it.k};
-    // pages of this wave's tiles (at most 16 of them: ranges are 64 tiles at most), lane 4 * i + s: page s of its i-th tile; -1: none
+    // pages of this wave's tiles (ranges are 64 tiles at most, so 16 of them), lane 4 * i + s: page s of the i-th; -1: none
     const int my_tiles = (it.hi - it.lo - wave + 3) >> 2;   // (0 or less: none)
     int pages;
     {
         const int lp = (it.lo + wave + 4 * (lane >> 2)) * 4 + (lane & 3);
-        pages = lp < kv.max_pages && lp * 16 < total && (lane >> 2) < my_tiles ? kv.block_table[(int64_t)b * kv.max_pages + lp] : -1;
+        pages = (lane >> 2) < my_tiles && lp < kv.max_pages && lp * 16 < total ? kv.block_table[(int64_t)b * kv.max_pages + lp] : -1;
         pages = pages < kv.n_pages ? pages : -1;
     }
     // codes and exponents of tile i; a page that is not there reads as zeros
     u32x4_t kc[4][2];
-    u32x2_t vc[4][4];
+    u32x2_t vc[2][2][4];
     uint32_t ke[4], kve[4], ve[4];   // (kve: the exponents of the values of the lane's key)
+    const int k_off = l16 * kD + 16 * g4, v_off = g4 * (4 * kD) + 8 * l16;
     auto page_row = [&](int pg) { return ((int64_t)max(pg, 0) * n_kv + kh) * 16; };
     auto load_k = [&](int i) {
 #pragma unroll
@@ -526,7 +700,7 @@ __global__ __launch_bounds__(256) void kv8_attn_few_k(KV8Split sp, int n_q_heads
             ke[s] = __builtin_amdgcn_raw_buffer_load_b8(re, l16, 0, 0);
             kve[s] = __builtin_amdgcn_raw_buffer_load_b8(rv, l16, 0, 0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) kc[s][h] = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * kD + 64 * h + 16 * g4, 0, 2);   // (2: read once)
+            for (int h = 0; h < 2; ++h) kc[s][h] = __builtin_amdgcn_raw_buffer_load_b128(r, k_off, 64 * h, 2);   // (2: read once)
         }
     };
     auto load_v = [&](int i) {
@@ -537,316 +711,193 @@ __global__ __launch_bounds__(256) void kv8_attn_few_k(KV8Split sp, int n_q_heads
             const buffer_t r = buffer_of(kv.v + row * kD, pg < 0 ? 0 : 16 * kD), re = buffer_of(kv.v_exp + row, pg < 0 ? 0 : 16);
             ve[s] = __builtin_amdgcn_raw_buffer_load_b32(re, 4 * g4, 0, 0);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) vc[s][v] = __builtin_amdgcn_raw_buffer_load_b64(r, (4 * g4 + v) * kD + 8 * l16, 0, 2);
+            for (int v = 0; v < 4; ++v) vc[s >> 1][s & 1][v] = __builtin_amdgcn_raw_buffer_load_b64(r, v_off, v * kD, 2);
         }
     };
     if (my_tiles > 0) load_k(0), load_v(0);
-    // queries of this lane's row, in the order of the keys' pieces; visibility of the new rows
-    u32x4_t qf[NT][4];
+    KV8Tiles<NT> x;
+    kv8_tiles(x, rows, b, kh, G, q, q_stride, [](int t) { return 16 * t; });
     uint64_t mask[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int r = 16 * t + l16, i = r / G, g = r - i * G;
-        const bool on = r < R;
-        const uint16_t* p = q + (int64_t)(b * n + (on ? i : 0)) * q_stride + (kh * G + (on ? g : 0)) * kD + 16 * g4;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            const u32x4_t z = {0u, 0u, 0u, 0u};
-            qf[t][ks] = on ? *(const u32x4_t*)(p + (ks >> 1) * 64 + (ks & 1) * 8) : z;
-        }
-        mask[t] = !on ? 0ull : (rows.mask ? rows.mask[b * n + i] : (2ull << i) - 1ull) & (~0ull >> (64 - n));
-    }
-    f32x4_t acc[NT][8], acc_l[NT];
-    float m_run[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        m_run[t] = kNegBig;
-        acc_l[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) acc[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    const float lazy = 8.0f / scale_log2;
+    for (int t = 0; t < NT; ++t) mask[t] = kv8_mask(rows, b, G, 16 * t + l16);
     for (int i = 0; i < my_tiles; ++i) {
         const int t0 = (it.lo + wave + 4 * i) * kKT;
-        const bool edge = t0 + kKT > ctx;   // new rows, or keys behind the last
-        // ---- S^T = K Q^T
+        const bool edge = t0 + kKT > ctx;
         f32x4_t sc[NT][4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            // (values that are not finite: their codes are zero, the NaN comes through the score, which only rows that see the key keep)
-            const float scale = __uint_as_float((kve[s] == 255u ? 255u : ke[s]) << 23);
-            bf16x8_t kf[4];
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) kf[ks] = __builtin_bit_cast(bf16x8_t, cvt8(kc[s][ks >> 1][2 * (ks & 1)], kc[s][ks >> 1][2 * (ks & 1) + 1], scale));
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                sc[t][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], __builtin_bit_cast(bf16x8_t, qf[t][ks]), sc[t][s], 0, 0, 0);
-            }
-        }
-        if (i + 1 < my_tiles) load_k(i + 1);
-        // ---- running maximum and weights
         u32x4_t pb[NT][2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (edge) {
-                const uint64_t seen = seen_from(t0 + 4 * g4 - ctx, mask[t]);
+        for (int s = 0; s < 4; ++s) {
+            f32x4_t* to_sc[NT];
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) sc[t][s][v] = seen >> (16 * s + v) & 1ull ? sc[t][s][v] : kNegBig;
-            }
-            float tmax = kNegBig;
+            for (int t = 0; t < NT; ++t) to_sc[t] = &sc[t][s];
+            kv8_scores(x, kc[s][0], kc[s][1], ke[s], kve[s], to_sc);
+        }
+        if (i + 1 < my_tiles) load_k(i + 1);
+        kv8_weights<4>(x, sc, pb, edge, t0 - ctx, [&](int t, int) { return mask[t]; }, scale_log2, lazy);
+        if (edge) {   // (keys behind the last are weighted with zero, and slots that nobody has written may hold anything)
+            int ln = lane;
+            asm volatile("" : "+v"(ln));
+            const int left = total - t0 - 4 * (ln >> 4);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) tmax = fmaxf(tmax, sc[t][s][v]);
-            // the reference of the exponentials only has to keep them in range: it follows the maximum when some score exceeds it by 2^8
-            if (__builtin_amdgcn_ballot_w64(tmax > m_run[t] + lazy) != 0) {
-                const float m_new = fmaxf(m_run[t], group_max4(tmax));
-                const float alpha = __builtin_amdgcn_exp2f((m_run[t] - m_new) * scale_log2);
-                m_run[t] = m_new;
-                acc_l[t] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) acc[t][dt] *= alpha;
-            }
-            const float mc = fmaxf(m_run[t], -1e29f) * scale_log2;   // (rows that have seen nothing yet: exp2(-1e30 * c + 1e29 * c) = 0)
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                float e[4];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(fmaf(sc[t][s][v], scale_log2, -mc));
-                pb[t][s >> 1][2 * (s & 1)] = pack_bf16x2(e[0], e[1]);       // weights are rounded to bf16 for the second product, their sum is that of the rounded ones
-                pb[t][s >> 1][2 * (s & 1) + 1] = pack_bf16x2(e[2], e[3]);
-            }
+                for (int v = 0; v < 4; ++v) vc[s >> 1][s & 1][v] = 16 * s + v < left ? vc[s >> 1][s & 1][v] : u32x2_t{0u, 0u};
         }
-        // ---- O^T += V^T P^T: k slot 4 * sub + v of lane group g4 is key 16 * (2 * half + sub) + 4 * g4 + v
-        const int left = total - t0;   // (keys from there on are weighted with zero; slots that nobody has written may hold anything)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            uint32_t vv[8][4];
+            const u32x4_t* w[NT];
 #pragma unroll
-            for (int a = 0; a < 8; ++a) {
-                const int s = 2 * half + (a >> 2), v = a & 3;
-                uint32_t e8 = (ve[s] >> (8 * v)) & 255u;
-                e8 = e8 == 255u ? 127u : e8;
-                const float scale = __uint_as_float(e8 << 23);
-                u32x4_t x = cvt8(vc[s][v][0], vc[s][v][1], scale);
-                if (edge) {
-                    const bool in = 16 * s + 4 * g4 + v < left;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[c] = in ? x[c] : 0u;
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) vv[a][c] = x[c];
-            }
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                u32x4_t a;
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    a[p] = __builtin_amdgcn_perm(vv[2 * p + 1][dt >> 1], vv[2 * p][dt >> 1], dt & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    acc[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, pb[t][half]), acc[t][dt], 0, 0, 0);
-            }
-            const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-                acc_l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, pb[t][half]), acc_l[t], 0, 0, 0);
+            for (int t = 0; t < NT; ++t) w[t] = &pb[t][half];
+            kv8_sums(x, vc[half], ve[2 * half], ve[2 * half + 1], w);
         }
         if (i + 1 < my_tiles) load_v(i + 1);
     }
-    // ---- the four waves joined, a tile of rows at a time: lane (l16, g4) holds d = 32 * g4 + 8 * v + dt of row l16
-    const int64_t pbase = ((int64_t)it.slot * n_kv + kh) * (16 * NT);
+    // ---- the waves joined, a tile of rows at a time: lane (l16, g4) holds d = 32 * g4 + 8 * v + dt of row l16
+    int le = lane;
+    asm volatile("" : "+v"(le));
+    const int row_e = le & 15, grp_e = le >> 4;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t > 0) __syncthreads();
-        if (16 * t >= R) break;   // uniform
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            *(f32x4_t*)&o_s[wave][l16][32 * g4 + 8 * v] = f32x4_t{acc[t][0][v], acc[t][1][v], acc[t][2][v], acc[t][3][v]};
-            *(f32x4_t*)&o_s[wave][l16][32 * g4 + 8 * v + 4] = f32x4_t{acc[t][4][v], acc[t][5][v], acc[t][6][v], acc[t][7][v]};
+            *(f32x4_t*)&o_s[wave][row_e][32 * grp_e + 8 * v] = f32x4_t{x.acc[t][0][v], x.acc[t][1][v], x.acc[t][2][v], x.acc[t][3][v]};
+            *(f32x4_t*)&o_s[wave][row_e][32 * grp_e + 8 * v + 4] = f32x4_t{x.acc[t][4][v], x.acc[t][5][v], x.acc[t][6][v], x.acc[t][7][v]};
         }
-        if (g4 == 0) m_s[wave][16 * t + l16] = m_run[t], l_s[wave][16 * t + l16] = acc_l[t][0];
+        if (grp_e == 0) m_s[wave][row_e] = x.m[t], l_s[wave][row_e] = x.l[t][0];
         __syncthreads();
-        const int rl = tid >> 4, r = 16 * t + rl, c = (tid & 15) * 8;
-        if (r >= R) continue;
-        float M = kNegBig, L = 0.f, w[4];
+        const int rl = tid >> 4, c = (tid & 15) * 8;
+        if (16 * t + rl >= R) continue;
+        float M = kNegBig, L = 0.f, w[4], o[8];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) M = fmaxf(M, m_s[x][r]);
+        for (int y = 0; y < 4; ++y) M = fmaxf(M, m_s[y][rl]);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) w[x] = __builtin_amdgcn_exp2f((m_s[x][r] - M) * scale_log2), L += w[x] * l_s[x][r];
-        float o[8];
+        for (int y = 0; y < 4; ++y) w[y] = __builtin_amdgcn_exp2f((m_s[y][rl] - M) * scale_log2), L += w[y] * l_s[y][rl];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(w[x], o_s[x][rl][c + e], o[e]);
-        if (it.k == 1) {
-            const float inv = L == 0.f ? 0.f : 1.0f / L;
-            const int i = r / G, g = r - i * G;
-            *(u32x4_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD + c) =
-                u32x4_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv)};
-        } else {
-            float* po = part_o + (pbase + r) * kD + c;
-            *(f32x4_t*)po = f32x4_t{o[0], o[1], o[2], o[3]};
-            *(f32x4_t*)(po + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
-            if (c == 0) part_ml[(pbase + r) * 2] = M, part_ml[(pbase + r) * 2 + 1] = L;
-        }
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(w[y], o_s[y][rl][c + e], o[e]);
+        to.put<8>(it, kh, G, 16 * t + rl, c, o, M, L);
     }
 }
 
-// Many rows: bound by the matrix pipe and, side by side with it, the exponentials.  One workgroup of eight waves, two per SIMD, streams the item's range once
-// for up to 24 tiles of rows, dealt round-robin to the waves, which keep their queries and accumulators in registers (NT tiles each).  A tile of
-// 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead, a wave's eight keys (1 KB each of K and V) to a
-// place that only this wave reads; the wave converts them to bf16 and stores them for all, K rows swizzled by the key (the 16-byte fragments of 16
-// keys hit 16 distinct places), V rows by twice the key (a transposing read takes two neighbouring places of each of 8 keys).
-// The two waves of a SIMD run half a period apart, so that one's softmax runs under the other's products: per tile a wave does [P V of the tile
-// before, Q K^T] and then [softmax, conversion of the next tile], and the early waves 0 .. 3 meet the tile's barrier in front of the first half, the
-// late ones 4 .. 7 between the two.  Between barriers `it` and `it + 1` all read K of tile it and V of it - 1, and write both of tile it + 1: two
-// stages of K and three of V.
-constexpr int kRaw = 3;
-constexpr int kRawBytes = 2 * kKT * kD + 128, kStageK = kKT * kD * 2;   // (raw: K codes, V codes, 16 exponent bytes per wave)
-constexpr int kManyPages = 64 * 4;
-constexpr int kManyLds = kRaw * kRawBytes + 5 * kStageK + kManyPages * 4 + 64 * 8;
-
-__device__ __forceinline__ void dma_16(u32x4_t rsrc, uint32_t voff, uint32_t lds_bytes) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds" : : "v"(voff), "s"(rsrc), "s"(lds_bytes) : "memory", "m0");
+// From memory straight into LDS, lane i's 16 (4) bytes at base + offset to lds_bytes + 16 (4) * i.  The compiler does not count these loads: they are
+// waited for by number.
+__device__ __forceinline__ void dma_16(const uint8_t* base, uint32_t offset, uint32_t lds_bytes) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(lds_bytes) : "memory", "m0");
 }
-__device__ __forceinline__ void dma_4(u32x4_t rsrc, uint32_t voff, uint32_t lds_bytes) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(voff), "s"(rsrc), "s"(lds_bytes) : "memory", "m0");
+__device__ __forceinline__ void dma_4(const uint8_t* base, uint32_t offset, uint32_t lds_bytes) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(lds_bytes) : "memory", "m0");
 }
-
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t offset) { return (__attribute__((address_space(3))) T*)(uintptr_t)offset; }
 
-template <int NT>
-__device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg, int n_q_heads, int64_t q_stride, const uint16_t* __restrict__ q, const KV8Rows& rows,
-                                              const KV8Layer& kv, uint16_t* __restrict__ out, float* __restrict__ part_o, float* __restrict__ part_ml,
-                                              int row_tiles, int per_group, float scale_log2, uint8_t* lds) {
-    constexpr int TPW = NT > 0 ? NT : 1;
+// More rows: bound by the matrix pipe and, side by side with it, the exponentials.  One workgroup of eight waves, two per SIMD, streams the item's range once for up to 24
+// tiles of rows.  With KS = 2 (up to 12 tiles of rows) waves are paired on the rows and take half of a tile's keys each, which halves what a tile
+// costs in reads of LDS; NT: tiles of rows of a wave.  A tile of 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead,
+// a wave's eight keys (1 KB each of K and V) to a place that only this wave reads; the wave converts them to bf16 and stores them for all, K rows swizzled by
+// the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by twice the key (a transposing read takes two neighbouring places of each of 8
+// keys).  The two waves of a SIMD run half a period apart, so that one's softmax runs under the other's products: per tile a wave does [P V of the tile
+// before, Q K^T] and then [softmax, conversion of the next tile], and the early waves 0 .. 3 meet the tile's barrier in front of the first half, the
+// late ones 4 .. 7 between the two.  Between barriers `it` and `it + 1` all read K of tile it and V of it - 1, and write both of tile it + 1: two
+// stages of K and three of V.
+constexpr int kRaw = 3, kRawBytes = 2 * kKT * kD + 2 * kKT, kStage = kKT * kD * 2;   // (raw: K codes, V codes, exponents of K and V)
+constexpr int kManyLds = 5 * kStage + kRaw * kRawBytes + 64 * 8;
+
+template <int NT, int KS>
+__device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg, int64_t q_stride, const uint16_t* __restrict__ q, const KV8Rows& rows, const KV8Layer& kv,
+                                              const KV8Out& to, int per_group, float scale_log2, float lazy, uint8_t* lds) {
+    constexpr int TPW = NT > 0 ? NT : 1, RW = 8 / KS, SN = 4 / KS;   // waves that share the rows; groups of 16 keys of a tile that a wave takes
     typedef __attribute__((ext_vector_type(4))) short s16x4_t;
     typedef __attribute__((ext_vector_type(8))) short s16x8_t;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
-    const int b = it.b, ctx = it.ctx, n = rows.n, total = ctx + n, n_kv = kv.n_kv, G = n_q_heads / n_kv, R = n * G;
-    const int n_tiles = it.hi - it.lo, k0 = it.lo * kKT;
-    uint16_t* st_k = (uint16_t*)lds;   // (the stages first: their places are worked out with exclusive ors below 256)
-    uint16_t* st_v = st_k + 2 * (kStageK / 2);
-    uint8_t* raw = lds + 5 * kStageK;
-    int32_t* page_ids = (int32_t*)(raw + kRaw * kRawBytes);
-    uint64_t* mask_lds = (uint64_t*)(page_ids + kManyPages);
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds, raw_base = lds_base + 5 * kStageK;
+    const int b = it.b, ctx = it.ctx, n = rows.n, total = ctx + n, n_kv = kv.n_kv, G = to.n_q_heads / n_kv, R = n * G;
+    const int n_tiles = it.hi - it.lo, k0 = it.lo * kKT, kg = wave % KS, rw = wave / KS;
+    uint8_t* raw = lds + 5 * kStage;   // (the stages first: their places are worked out with exclusive ors below 256)
+    uint64_t* mask_lds = (uint64_t*)(raw + kRaw * kRawBytes);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
 
-    // ---- this wave's row tiles
-    u32x4_t qf[TPW][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int r = (rg * per_group + wave + 8 * t) * 16 + l16, i = r / G, g = r - i * G;
-        const bool on = r < R;
-        const uint16_t* p = q + (int64_t)(b * n + (on ? i : 0)) * q_stride + (kh * G + (on ? g : 0)) * kD + g4 * 8;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            const u32x4_t z = {0u, 0u, 0u, 0u};
-            qf[t][ks] = on ? *(const u32x4_t*)(p + ks * 32) : z;
-        }
-    }
-    // ---- codes and exponents from memory: this wave's keys 8 * wave .. + 7 of a tile lie in one page
-    auto rsrc = [&](const uint8_t* p, uint32_t bytes) {
-        const uint64_t a = (uint64_t)(uintptr_t)p;
-        u32x4_t d;
-        d[0] = __builtin_amdgcn_readfirstlane((uint32_t)a);
-        d[1] = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xffffu);
-        d[2] = __builtin_amdgcn_readfirstlane(bytes);
-        d[3] = 0x00020000u;
-        return d;
-    };
-    auto fetch = [&](int slot, int pg) {   // pg < 0: nothing is fetched (the conversion does not look)
-        const int64_t row = ((int64_t)max(pg, 0) * n_kv + kh) * 16 + (wave & 1) * 8;
-        const uint32_t some = pg < 0 ? 0u : 1u, at = raw_base + slot * kRawBytes + wave * 1024;
-        dma_16(rsrc(kv.k + row * kD, some * 1024u), lane * 16, __builtin_amdgcn_readfirstlane(at));
-        dma_16(rsrc(kv.v + row * kD, some * 1024u), lane * 16, __builtin_amdgcn_readfirstlane(at + kKT * kD));
-        const uint32_t ex = raw_base + slot * kRawBytes + 2 * kKT * kD + wave * 16;
-        if (lane < 2) dma_4(rsrc(kv.k_exp + row, some * 8u), lane * 4, __builtin_amdgcn_readfirstlane(ex));
-        if (lane < 2) dma_4(rsrc(kv.v_exp + row, some * 8u), lane * 4, __builtin_amdgcn_readfirstlane(ex + 8));
-    };
-    constexpr int kOps = 4;   // loads of a fetch
-    auto page_at = [&](int lp) {
-        const int pg = lp < kv.max_pages && lp * 16 < total ? kv.block_table[(int64_t)b * kv.max_pages + lp] : -1;
-        return pg < kv.n_pages ? pg : -1;
-    };
+    // ---- codes and exponents from memory: this wave's keys 8 * wave .. + 7 of a tile lie in one page, lane t of `pages` has that of tile t (a range is 64 tiles at
+    // most); -1: none
+    int pages;
     {
-        int pg[kRaw];
-#pragma unroll
-        for (int t = 0; t < kRaw; ++t) pg[t] = t < n_tiles ? page_at((it.lo + t) * 4 + (wave >> 1)) : -1;
-#pragma unroll
-        for (int t = 0; t < kRaw; ++t)
-            if (t < n_tiles) fetch(t, __builtin_amdgcn_readfirstlane(pg[t]));
+        const int lp = (it.lo + lane) * 4 + (wave >> 1);
+        pages = lane < n_tiles && lp < kv.max_pages && lp * 16 < total ? kv.block_table[(int64_t)b * kv.max_pages + lp] : -1;
+        pages = pages < kv.n_pages ? pages : -1;
     }
-    for (int i = tid; i < 4 * n_tiles; i += 512) page_ids[i] = page_at(it.lo * 4 + i);
-    for (int i = tid; i < n; i += 512) mask_lds[i] = (rows.mask ? rows.mask[b * n + i] : (2ull << i) - 1ull) & (~0ull >> (64 - n));
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr int kOps = 4;   // loads of a fetch
+    auto fetch = [&](int t) {   // (of a page that is not there, page 0 instead: the conversion does not look)
+        const int64_t row = ((int64_t)max(__builtin_amdgcn_readlane(pages, t), 0) * n_kv + kh) * 16 + (wave & 1) * 8;
+        const uint32_t at = __builtin_amdgcn_readfirstlane(base + 5 * kStage + (t % kRaw) * kRawBytes);
+        dma_16(kv.k + row * kD, lane * 16, at + wave * 1024);
+        dma_16(kv.v + row * kD, lane * 16, at + kKT * kD + wave * 1024);
+        if (lane < 2) dma_4(kv.k_exp + row, lane * 4, at + 2 * kKT * kD + wave * 8);
+        if (lane < 2) dma_4(kv.v_exp + row, lane * 4, at + 2 * kKT * kD + kKT + wave * 8);
+    };
+#pragma unroll
+    for (int t = 0; t < kRaw; ++t)
+        if (t < n_tiles) fetch(t);
+    if (tid < n) mask_lds[tid] = kv8_mask(rows, b, G, tid * G);
+    KV8Tiles<TPW> x;
+    if constexpr (NT > 0) kv8_tiles(x, rows, b, kh, G, q, q_stride, [&](int t) { return (rg * per_group + rw + RW * t) * 16; });
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 
-    // tile t, which has landed, to bf16; then the fetch of tile t + kRaw into its place
-    auto convert = [&](int t) {
-        if (t >= n_tiles) return;   // uniform
+    // (with three tiles of rows, places in LDS are worked out anew for every tile: kept, they would cost registers that the products need)
+    auto place = [](int ln) {
+        if constexpr (NT >= 3) asm volatile("" : "+v"(ln));
+        return ln;
+    };
+    // this wave's keys of a tile in registers: 16 codes of key lane / 8 of K and V, and the key's exponents
+    struct Raw {
+        u32x4_t k, v;
+        uint32_t ke, ve;
+    };
+    auto read_raw = [&](int t, Raw& r) {   // tile t has landed when all but the fetches behind it have
         if (t + kRaw <= n_tiles) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kOps * (kRaw - 1)) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        int ln = lane;
-        asm volatile("" : "+v"(ln));   // (places are worked out anew for every tile: kept, they would cost registers that the products need)
-        const int slot = t % kRaw, key = 8 * wave + (ln >> 3), p = ln & 7;
-        const uint8_t* rp = raw + slot * kRawBytes;
-        u32x4_t kc = *(const u32x4_t*)(rp + wave * 1024 + ln * 16), vc = *(const u32x4_t*)(rp + kKT * kD + wave * 1024 + ln * 16);
-        uint32_t ke = rp[2 * kKT * kD + wave * 16 + (ln >> 3)], ve = rp[2 * kKT * kD + wave * 16 + 8 + (ln >> 3)];
-        const bool backed = __builtin_amdgcn_readfirstlane(page_ids[4 * t + (wave >> 1)]) >= 0;
-        const int next = t + kRaw < n_tiles ? __builtin_amdgcn_readfirstlane(page_ids[4 * (t + kRaw) + (wave >> 1)]) : -1;
-        const bool in = backed && k0 + t * kKT + key < total;   // (slots that nobody has written may hold anything)
-        // (values that are not finite: their codes are zero, the NaN comes through the key, whose score only rows that see it keep)
-        ke = !backed ? 127u : (in && ve == 255u ? 255u : ke);
-        ve = ve == 255u ? 127u : ve;
+        const int ln = place(lane);
+        const uint8_t* p = raw + (t % kRaw) * kRawBytes;
+        r.k = *(const u32x4_t*)(p + wave * 1024 + ln * 16), r.v = *(const u32x4_t*)(p + kKT * kD + wave * 1024 + ln * 16);
+        r.ke = p[2 * kKT * kD + wave * 8 + (ln >> 3)], r.ve = p[2 * kKT * kD + kKT + wave * 8 + (ln >> 3)];
+    };
+    auto convert = [&](int t, Raw& r) {
+        const int ln = place(lane), key = 8 * wave + (ln >> 3), p = ln & 7;
+        const bool there = __builtin_amdgcn_readlane(pages, t) >= 0;
+        const int left = there ? total - k0 - t * kKT : 0;   // (slots that nobody has written may hold anything)
+        for (int rep = left < kKT ? 0 : 1; rep < 1; ++rep) {   // (a loop, which stays a branch)
+            const bool in = key < left;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) kc[c] = backed ? kc[c] : 0u, vc[c] = in ? vc[c] : 0u;
-        const float sk = __uint_as_float(ke << 23), sv = __uint_as_float(ve << 23);
-        uint16_t* ko = st_k + (t & 1) * (kStageK / 2) + key * kD;
-        uint16_t* vo = st_v + (t % 3) * (kStageK / 2) + key * kD;
-        *(u32x4_t*)(ko + ((2 * p) ^ (key & 15)) * 8) = cvt8(kc[0], kc[1], sk);
-        *(u32x4_t*)(ko + ((2 * p + 1) ^ (key & 15)) * 8) = cvt8(kc[2], kc[3], sk);
-        // (rows of odd keys start with their other half: even pieces of one row and odd ones of its neighbour share no bank)
-        const u32x4_t v0 = cvt8(vc[0], vc[1], sv), v1 = cvt8(vc[2], vc[3], sv);
-        const int odd = key & 1;
-        *(u32x4_t*)(vo + ((2 * p + odd) ^ ((2 * key) & 15)) * 8) = odd ? v1 : v0;
-        *(u32x4_t*)(vo + ((2 * p + 1 - odd) ^ ((2 * key) & 15)) * 8) = odd ? v0 : v1;
-        if (t + kRaw < n_tiles) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the codes have been read)
-            fetch(slot, next);
+            for (int y = 0; y < 4; ++y) r.v[y] = in ? r.v[y] : 0u, r.k[y] = there ? r.k[y] : 0u;
+            r.ke = there ? r.ke : 127u, r.ve = there ? r.ve : 127u;
         }
+        // (values that are not finite: their codes are zero, the NaN comes through the key, whose score only rows that see it keep)
+        const float sk = __uint_as_float((r.ve == 255u ? 255u : r.ke) << 23), sv = __uint_as_float((r.ve == 255u ? 127u : r.ve) << 23);
+        uint8_t* ko = lds + (t & 1) * kStage + key * (2 * kD);
+        uint8_t* vo = lds + (2 + t % 3) * kStage + key * (2 * kD);
+        *(u32x4_t*)(ko + ((2 * p) ^ (key & 15)) * 16) = cvt8(r.k[0], r.k[1], sk);
+        *(u32x4_t*)(ko + ((2 * p + 1) ^ (key & 15)) * 16) = cvt8(r.k[2], r.k[3], sk);
+        *(u32x4_t*)(vo + ((2 * p) ^ ((2 * key) & 15)) * 16) = cvt8(r.v[0], r.v[1], sv);
+        *(u32x4_t*)(vo + ((2 * p + 1) ^ ((2 * key) & 15)) * 16) = cvt8(r.v[2], r.v[3], sv);
+        if (t + kRaw < n_tiles) fetch(t + kRaw);   // (the codes have been read: they are converted)
     };
     auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    f32x4_t acc[TPW][8], acc_l[TPW];
-    float m_run[TPW];
-    u32x4_t pb[TPW][2];   // weights of the tile whose second product is still owed
+    u32x4_t pb[TPW][2 / KS];   // weights of the tile whose second product is still owed
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        m_run[t] = kNegBig;
-        acc_l[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        pb[t][0] = pb[t][1] = u32x4_t{0u, 0u, 0u, 0u};
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) acc[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    // ---- O^T += V^T P^T: a transposing read hands lane (l16, g4) keys 4 * g4 .. + 3 of 16 for d = 16 * dt + l16; two of them are 8 k slots.  Four batches
-    // (half of the keys, half of d), each read under the products of the one before.
+        for (int h = 0; h < 2 / KS; ++h) pb[t][h] = u32x4_t{0u, 0u, 0u, 0u};
+    // ---- O^T += V^T P^T: a transposing read hands lane (l16, g4) keys 4 * g4 .. + 3 of 16 for d = 16 * dt + l16; two of them are 8 k slots.  Batches of
+    // half of d (and half of the keys), each read under the products of the one before.
     auto second = [&](int stage) {
         if constexpr (NT == 0) return;
         s16x4_t vv[2][4][2];
-        int ln = lane;
-        asm volatile("" : "+v"(ln));   // (as in the conversion)
+        const int ln = place(lane);
         // key 4 * g4 + l16 / 4 of the 16, its piece 2 * dt + (l16 & 3) / 2 swizzled by twice the key (16 keys further on: by the same)
         const int kr = 4 * (ln >> 4) + ((ln & 15) >> 2);
-        const uint32_t at = lds_base + 2 * kStageK + stage * kStageK + kr * (2 * kD) + ((((ln & 3) >> 1) ^ ((2 * kr) & 15)) * 16) + (ln & 1) * 8;
+        const uint32_t at = base + (2 + stage) * kStage + (kg * (SN * 16) + kr) * (2 * kD) + ((((ln & 3) >> 1) ^ ((2 * kr) & 15)) * 16) + (ln & 1) * 8;
         auto read_v = [&](int half, int dq, s16x4_t (*v)[2]) {
 #pragma unroll
             for (int d4 = 0; d4 < 4; ++d4)
@@ -861,154 +912,158 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
                 const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    acc_l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, pb[t][half]), acc_l[t], 0, 0, 0);
+                    x.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, pb[t][half]), x.l[t], 0, 0, 0);
             }
 #pragma unroll
             for (int d4 = 0; d4 < 4; ++d4) {
                 const s16x8_t a = {v[d4][0][0], v[d4][0][1], v[d4][0][2], v[d4][0][3], v[d4][1][0], v[d4][1][1], v[d4][1][2], v[d4][1][3]};
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    acc[t][dq * 4 + d4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, pb[t][half]),
-                                                                                  acc[t][dq * 4 + d4], 0, 0, 0);
+                    x.acc[t][dq * 4 + d4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, pb[t][half]),
+                                                                                    x.acc[t][dq * 4 + d4], 0, 0, 0);
             }
         };
         read_v(0, 0, vv[0]);
         read_v(0, 1, vv[1]);
         mul_v(0, 0, vv[0]);
-        read_v(1, 0, vv[0]);
-        mul_v(0, 1, vv[1]);
-        read_v(1, 1, vv[1]);
-        mul_v(1, 0, vv[0]);
-        mul_v(1, 1, vv[1]);
-        __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 5 * NT, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
+        if constexpr (KS == 1) {
+            read_v(1, 0, vv[0]);
+            mul_v(0, 1, vv[1]);
+            read_v(1, 1, vv[1]);
+            mul_v(1, 0, vv[0]);
+            mul_v(1, 1, vv[1]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 5 * NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
+        } else {
+            mul_v(0, 1, vv[1]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
+        }
     };
-    const float lazy = 8.0f / scale_log2;
     const bool late = wave >= 4;
-    convert(0);
-    if (late) {
-        meet();
-        convert(1);
+    {
+        Raw r;
+        read_raw(0, r);
+        convert(0, r);
+        if (late) {
+            meet();
+            if (n_tiles > 1) {
+                read_raw(1, r);
+                convert(1, r);
+            }
+        }
     }
     for (int i = 0; i < n_tiles; ++i) {
         if (!late) meet();
         __builtin_amdgcn_s_setprio(2);
         if (i > 0) second((i - 1) % 3);
-        const int t0 = k0 + i * kKT;
-        int lk = lane;
-        asm volatile("" : "+v"(lk));
-        const uint32_t k_at = lds_base + (i & 1) * kStageK + (lk & 15) * (2 * kD) + (((lk >> 4) ^ (lk & 15)) * 16);
         // ---- S^T = K Q^T, the next 16 keys' fragments read under the products of those before
-        f32x4_t sc[TPW][4];
-        bf16x8_t kf[2][4];
-        auto read_k = [&](int s, bf16x8_t* f) {
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                f[ks] = __builtin_bit_cast(bf16x8_t, *lds_at<u32x4_t>((k_at ^ (uint32_t)(ks * 64)) + s * 16 * (2 * kD)));
-        };
-        auto mul_k = [&](int s, const bf16x8_t* f) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sc[t][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[ks], __builtin_bit_cast(bf16x8_t, qf[t][ks]), sc[t][s], 0, 0, 0);
-        };
+        f32x4_t sc[TPW][SN];
         if constexpr (NT > 0) {
+            const int ln = place(lane);
+            // key l16 of 16, pieces of 8 elements 2 * g4, 2 * g4 + 1 and 8 further on, swizzled by the key
+            const uint32_t k_at = base + (i & 1) * kStage + (kg * (SN * 16) + (ln & 15)) * (2 * kD) + (((2 * (ln >> 4)) ^ (ln & 15)) * 16);
+            bf16x8_t kf[2][4];
+            auto read_k = [&](int s, bf16x8_t* f) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    f[ks] = __builtin_bit_cast(bf16x8_t, *lds_at<u32x4_t>((k_at ^ (uint32_t)((ks >> 1) * 128 + (ks & 1) * 16)) + s * 16 * (2 * kD)));
+            };
+            auto mul_k = [&](int s, const bf16x8_t* f) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sc[t][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[ks], __builtin_bit_cast(bf16x8_t, x.q[t][ks]), sc[t][s], 0, 0, 0);
+            };
             read_k(0, kf[0]);
             read_k(1, kf[1]);
             mul_k(0, kf[0]);
-            read_k(2, kf[0]);
-            mul_k(1, kf[1]);
-            read_k(3, kf[1]);
-            mul_k(2, kf[0]);
-            mul_k(3, kf[1]);
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
+            if constexpr (KS == 1) {
+                read_k(2, kf[0]);
+                mul_k(1, kf[1]);
+                read_k(3, kf[1]);
+                mul_k(2, kf[0]);
+                mul_k(3, kf[1]);
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
+            } else {
+                mul_k(1, kf[1]);
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
         if (late && i + 1 < n_tiles) meet();
-        // ---- running maximum and weights
-        const int edge = t0 + kKT > ctx ? 1 : 0;   // new rows, or keys behind the last (a trip count: an `if` around so many selects would run on every tile)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            for (int rep = 0; rep < edge; ++rep) {
-                int ln = lane;
-                asm volatile("" : "+v"(ln));
-                const int r = (rg * per_group + wave + 8 * t) * 16 + (ln & 15);
-                const uint64_t seen = seen_from(t0 + 4 * (ln >> 4) - ctx, r < R ? mask_lds[r / G] : 0ull);
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) sc[t][s][v] = seen >> (16 * s + v) & 1ull ? sc[t][s][v] : kNegBig;
-            }
-            float tmax = kNegBig;
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) tmax = fmaxf(tmax, sc[t][s][v]);
-            if (__builtin_amdgcn_ballot_w64(tmax > m_run[t] + lazy) != 0) {   // (as in the kernel of few rows)
-                const float m_new = fmaxf(m_run[t], group_max4(tmax));
-                const float alpha = __builtin_amdgcn_exp2f((m_run[t] - m_new) * scale_log2);
-                m_run[t] = m_new;
-                acc_l[t] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) acc[t][dt] *= alpha;
-            }
-            const float mc = fmaxf(m_run[t], -1e29f) * scale_log2;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                float e[4];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(fmaf(sc[t][s][v], scale_log2, -mc));
-                pb[t][s >> 1][2 * (s & 1)] = pack_bf16x2(e[0], e[1]);
-                pb[t][s >> 1][2 * (s & 1) + 1] = pack_bf16x2(e[2], e[3]);
-            }
-        }
+        // ---- softmax, with the next tile's codes on their way
+        const int next = i + (late ? 2 : 1);
+        Raw r;
+        if (next < n_tiles) read_raw(next, r);
+        if constexpr (NT > 0)
+            kv8_weights<SN>(x, sc, pb, k0 + i * kKT + kKT > ctx, k0 + i * kKT + kg * (SN * 16) - ctx,
+                            [&](int t, int ln) {
+                                const int row = (rg * per_group + rw + RW * t) * 16 + (ln & 15);
+                                return row < R ? mask_lds[row / G] : 0ull;
+                            },
+                            scale_log2, lazy);
         __builtin_amdgcn_sched_barrier(0);   // (registers again: neither half of the period may reach into the conversion)
-        convert(i + (late ? 2 : 1));
+        if (next < n_tiles) convert(next, r);
         __builtin_amdgcn_sched_barrier(0);
     }
     second((n_tiles - 1) % 3);
+    if constexpr (KS > 1) {   // the waves of a row's two halves of the keys joined, by way of the stages
+        static_assert(KS == 2, "one partner");
+        f32x4_t* other = (f32x4_t*)lds + rw * (3 * 8 * 64) + lane;                            // [rw][t][dt][lane]
+        float2* other_ml = (float2*)((f32x4_t*)lds + RW * 3 * 8 * 64) + rw * (3 * 64) + lane;   // [rw][t][lane]
+        meet();
+        if (kg == 1) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) other[(t * 8 + dt) * 64] = x.acc[t][dt];
+                other_ml[t * 64] = make_float2(x.m[t], x.l[t][0]);
+            }
+        }
+        meet();
+        if (kg == 1) return;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float2 o = other_ml[t * 64];
+            const float M = fmaxf(x.m[t], o.x), w0 = __builtin_amdgcn_exp2f((x.m[t] - M) * scale_log2), w1 = __builtin_amdgcn_exp2f((o.x - M) * scale_log2);
+            x.m[t] = M;
+            x.l[t][0] = w0 * x.l[t][0] + w1 * o.y;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                if ((dt & 3) == 0) asm volatile("" ::: "memory");   // (a few reads at a time)
+                x.acc[t][dt] = w0 * x.acc[t][dt] + w1 * other[(t * 8 + dt) * 64];
+            }
+        }
+    }
     // ---- lane (l16, g4) holds d = 16 * dt + 4 * g4 + v of row l16
-    const int r_pad = row_tiles * 16;
-    const int64_t pbase = ((int64_t)it.slot * n_kv + kh) * r_pad;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int r = (rg * per_group + wave + 8 * t) * 16 + l16;
-        if (r >= R) continue;
-        const float l = acc_l[t][0];
-        if (it.k == 1) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            const int i = r / G, g = r - i * G;
-            uint16_t* o = out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD + 4 * g4;
+        const int row = (rg * per_group + rw + RW * t) * 16 + l16;
+        if (row >= R) continue;
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-                *(u32x2_t*)(o + 16 * dt) = u32x2_t{pack_bf16x2(acc[t][dt][0] * inv, acc[t][dt][1] * inv), pack_bf16x2(acc[t][dt][2] * inv, acc[t][dt][3] * inv)};
-        } else {
-            float* po = part_o + (pbase + r) * kD + 4 * g4;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) *(f32x4_t*)(po + 16 * dt) = acc[t][dt];
-            if (g4 == 0) part_ml[(pbase + r) * 2] = m_run[t], part_ml[(pbase + r) * 2 + 1] = l;
-        }
+        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0]);
     }
 }
 
 // Workgroup id -> (item, kv head, group of row tiles).  Ids are dealt round-robin over the 8 XCDs, and the groups of one (item, kv head) read the same keys and
 // values: they get ids 8 apart, so that they run on one XCD at the same time.
-template <int TPW>
-__global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int n_q_heads, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv,
-                                                       uint16_t* __restrict__ out, KV8Seg* __restrict__ seg, float* __restrict__ part_o,
-                                                       float* __restrict__ part_ml, int row_tiles, int groups, int per_group, float scale_log2) {
+template <int TPW, int KS>
+__global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
+                                                       KV8Seg* __restrict__ seg, int row_tiles, int groups, int per_group, float scale_log2, float lazy) {
     __shared__ __align__(256) uint8_t lds[kManyLds];
     const int id = blockIdx.x, g = id / (8 * groups), within = id - g * 8 * groups, rg = within >> 3, pair = g * 8 + (within & 7);
     const int item = pair / kv.n_kv, kh = pair - item * kv.n_kv;
@@ -1016,9 +1071,10 @@ __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int n_q_head
     if (!kv8_item(kv.seq_len, rows.B, rows.n, kv.seq_len_bound, sp, item, it)) return;   // uniform
     if (kh == 0 && rg == 0 && it.slot == it.first && threadIdx.x == 0) seg[it.b] = KV8Seg{it.first, it.k};
     // row tiles of this wave (a wave runs the program for as many as it has; all pass the same barriers)
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int mine = min(per_group, row_tiles - rg * per_group), n_on = mine > wave ? (mine - wave + 7) / 8 : 0;
-#define TLT_BODY(N) kv8_many_body<N>(it, kh, rg, n_q_heads, q_stride, q, rows, kv, out, part_o, part_ml, row_tiles, per_group, scale_log2, lds)
+    constexpr int RW = 8 / KS;
+    const int rw = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / KS;
+    const int mine = min(per_group, row_tiles - rg * per_group), n_on = mine > rw ? (mine - rw + RW - 1) / RW : 0;
+#define TLT_BODY(N) kv8_many_body<N, KS>(it, kh, rg, q_stride, q, rows, kv, to, per_group, scale_log2, lazy, lds)
     if (n_on >= TPW) TLT_BODY(TPW);
     else if (TPW >= 2 && n_on == TPW - 1) TLT_BODY((TPW >= 2 ? TPW - 1 : 0));
     else if (TPW >= 3 && n_on == TPW - 2) TLT_BODY((TPW >= 3 ? TPW - 2 : 0));
@@ -1026,15 +1082,19 @@ __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int n_q_head
 #undef TLT_BODY
 }
 
-// The ranges of a sequence joined: a wave per row, in the order of the ranges; the lanes read a range's maximum and sum each, and the outputs of
-// 16 ranges are requested together.
+// The ranges of a sequence joined: WPR waves per row, 16 ranges of each requested together, added up in a fixed order; the lanes read a range's maximum and
+// sum each.
+template <int WPR>
 __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg, const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                   uint16_t* __restrict__ out, int n, int n_q_heads, int n_kv, int r_pad, int slot_step, float scale_log2) {
     constexpr int U = 16;
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), kh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
+    __shared__ float2 s_a[WPR > 1 ? WPR - 1 : 1][64];
+    __shared__ float s_l[WPR];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), part = wave % WPR, lane = threadIdx.x & 63;
+    const int r = blockIdx.x * (4 / WPR) + wave / WPR, kh = blockIdx.y, b = blockIdx.z;
     const int G = n_q_heads / n_kv;
     const KV8Seg sg = seg[b];
-    if (r >= n * G || sg.k <= 1) return;   // (one range: its workgroup has written the row)
+    if (r >= n * G || sg.k <= 1) return;   // (one range: its workgroup has written the row; with several waves per row: uniform for the workgroup)
     const int64_t base = ((int64_t)sg.first * n_kv + kh) * r_pad + r, step = (int64_t)slot_step * n_kv * r_pad;
     float2 ml = make_float2(kNegBig, 0.f), v[U];
     auto fetch = [&](int c) {
@@ -1043,16 +1103,17 @@ __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg
             v[u] = c + u < sg.k ? *(const float2*)(part_o + (base + (c + u) * step) * kD + lane * 2) : make_float2(0.f, 0.f);
     };
     if (lane < sg.k) ml = *(const float2*)(part_ml + (base + lane * step) * 2);
-    fetch(0);
+    fetch(U * part);
     float M = ml.x;
     for (int c = lane + 64; c < sg.k; c += 64) M = fmaxf(M, part_ml[(base + c * step) * 2]);
     M = wave_max(M);
     float w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w, a0 = 0.f, a1 = 0.f, L = 0.f;
-    for (int c0 = 0; c0 < sg.k; c0 += U) {   // (uniform)
-        if (c0 > 0) {
+    for (int c0 = U * part; c0 < sg.k; c0 += U * WPR) {   // (uniform for the wave)
+        if (c0 > U * part) {
             fetch(c0);
-            if ((c0 & 63) == 0) {
-                ml = c0 + lane < sg.k ? *(const float2*)(part_ml + (base + (c0 + lane) * step) * 2) : make_float2(kNegBig, 0.f);
+            if (c0 - U * part != 0 && ((c0 ^ (c0 - U * WPR)) & ~63) != 0) {   // another 64 ranges
+                const int c = (c0 & ~63) + lane;
+                ml = c < sg.k ? *(const float2*)(part_ml + (base + c * step) * 2) : make_float2(kNegBig, 0.f);
                 w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w;
             }
         }
@@ -1064,28 +1125,34 @@ __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg
             a0 = fmaf(wu, v[u].x, a0), a1 = fmaf(wu, v[u].y, a1);
         }
     }
+    if constexpr (WPR > 1) {
+        if (part > 0) s_a[part - 1][lane] = make_float2(a0, a1);
+        if (lane == 0) s_l[part] = L;
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int p = 1; p < WPR; ++p) a0 += s_a[p - 1][lane].x, a1 += s_a[p - 1][lane].y, L += s_l[p];
+    }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     const int i = r / G, g = r - i * G;
     ((uint32_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD))[lane] = pack_bf16x2(a0 * inv, a1 * inv);
 }
 
-constexpr int kFewRows = 16;
 struct KV8Plan {
     KV8Split sp;
     bool few;        // the kernel of few rows
     bool one_each;   // no sequence has a second range
-    int row_tiles, groups, per_group, tpw;
+    int row_tiles, groups, per_group;
     size_t seg, part_o, part_ml, total;   // byte offsets into the workspace
 };
 static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) {
     KV8Plan p;
     const int R = n * (n_q_heads / n_kv), tiles = (bound_total + kKT - 1) / kKT;
-    p.few = R <= kFewRows;
     p.row_tiles = (R + 15) / 16;
+    p.few = p.row_tiles <= 2;
     p.groups = p.few ? 1 : (p.row_tiles + 23) / 24;
     p.per_group = (p.row_tiles + p.groups - 1) / p.groups;
-    p.tpw = (p.per_group + 7) / 8;
-    p.sp.slots = std::max(1, (p.few ? 768 : 256) / (n_kv * p.groups));
+    p.sp.slots = std::max(1, (p.few ? 512 : 256) / (n_kv * p.groups));   // (workgroups that the chip holds)
     p.sp.t_min = 4;
     p.sp.t_max = 64;
     p.one_each = tiles <= p.sp.t_min || (B > kPlanned && tiles <= p.sp.t_max);
@@ -1115,25 +1182,31 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         const KV8Plan p = plan_kv8(rows.B, rows.n, n_q_heads, kv.n_kv, kv.seq_len_bound + rows.n);
         if (p.total > ws_bytes) return hipErrorInvalidValue;
         KV8Seg* seg = (KV8Seg*)((char*)ws + p.seg);
-        float *part_o = (float*)((char*)ws + p.part_o), *part_ml = (float*)((char*)ws + p.part_ml);
-        const float scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
+        const KV8Out to{(uint16_t*)out, (float*)((char*)ws + p.part_o), (float*)((char*)ws + p.part_ml), rows.n, n_q_heads, kv.n_kv, p.row_tiles * 16};
+        const float scale_log2 = 1.4426950408889634f / sqrtf((float)kD), lazy = 8.0f / scale_log2;
         const unsigned pairs = (unsigned)(p.sp.max_items * kv.n_kv);
-        if (p.few) {
-            hipLaunchKernelGGL(kv8_attn_few_k<1>, dim3(pairs), dim3(256), 0, s, p.sp, n_q_heads, q_stride, (const uint16_t*)q, rows, kv, (uint16_t*)out, seg, part_o,
-                               part_ml, scale_log2);
-        } else {
-            auto many = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3((pairs + 7) / 8 * 8 * p.groups), dim3(512), 0, s, p.sp, n_q_heads, q_stride, (const uint16_t*)q, rows, kv,
-                                   (uint16_t*)out, seg, part_o, part_ml, p.row_tiles, p.groups, p.per_group, scale_log2);
-            };
-            if (p.tpw == 1) many(kv8_attn_many_k<1>);
-            else if (p.tpw == 2) many(kv8_attn_many_k<2>);
-            else many(kv8_attn_many_k<3>);
-        }
+        auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pairs), dim3(256), 0, s, p.sp, q_stride, (const uint16_t*)q, rows, kv, to, seg, scale_log2, lazy); };
+        auto many = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((pairs + 7) / 8 * 8 * p.groups), dim3(512), 0, s, p.sp, q_stride, (const uint16_t*)q, rows, kv, to, seg, p.row_tiles, p.groups,
+                               p.per_group, scale_log2, lazy);
+        };
+        if (p.row_tiles == 1) few(kv8_attn_few_k<1>);
+        else if (p.few) few(kv8_attn_few_k<2>);
+        else if (p.per_group <= 4) many(kv8_attn_many_k<1, 2>);
+        else if (p.per_group <= 8) many(kv8_attn_many_k<2, 2>);
+        else if (p.per_group <= 12) many(kv8_attn_many_k<3, 2>);
+        else if (p.per_group <= 16) many(kv8_attn_many_k<2, 1>);
+        else many(kv8_attn_many_k<3, 1>);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.one_each) return e;
-        hipLaunchKernelGGL(kv8_join_k, dim3((R + 3) / 4, kv.n_kv, rows.B), dim3(256), 0, s, seg, part_o, part_ml, (uint16_t*)out, rows.n, n_q_heads, kv.n_kv,
-                           p.row_tiles * 16, rows.B > kPlanned ? rows.B : 1, scale_log2);
+        auto join = [&](auto kernel, int blocks) {
+            hipLaunchKernelGGL(kernel, dim3(blocks, kv.n_kv, rows.B), dim3(256), 0, s, seg, to.part_o, to.part_ml, (uint16_t*)out, rows.n, n_q_heads, kv.n_kv,
+                               p.row_tiles * 16, rows.B > kPlanned ? rows.B : 1, scale_log2);
+        };
+        // the most ranges that a sequence can have: those of one round, fewer where they would be shorter than t_min
+        const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, ranges = std::max(std::min(p.sp.slots, (tiles + p.sp.t_min - 1) / p.sp.t_min), (tiles + 63) / 64);
+        if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_k<4>, R);
+        else join(kv8_join_k<1>, (R + 3) / 4);
         return hipGetLastError();
     }
     const float scale = 1.0f / sqrtf((float)kv.d);
