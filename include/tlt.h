@@ -347,8 +347,8 @@ int tlt_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
  * All of them: head_dim 64, 128, 192 or 256, any page size, any number of query heads per kv head; slots that the block table does not
  * back are not written, and count as keys and values of zero.  dtype (TLT_F32 / TLT_BF16) is that of the activations.
  * Sums, softmax and rotations are fp32, angles double.  No memory is kept between calls; calls may be captured into
- * graphs.  Errors: TLT_EINVAL, TLT_ESHAPE (a workspace that is too small, or an `impl` that does not cover the shape),
- * TLT_ENOPAGES, TLT_EHIP. */
+ * graphs.  Errors: TLT_EINVAL, TLT_ESHAPE (a workspace that is too small, or more work than a launch holds), TLT_ENOPAGES,
+ * TLT_EHIP. */
 typedef struct tlt_kv8 {
     void *k_pool, *v_pool, *k_exp, *v_exp;
     int64_t n_pages;
@@ -373,7 +373,9 @@ int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
  * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
  * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
  * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).
- * impl: -1 automatic, 0 a workgroup per row and query head (any shape). */
+ * At most 2^26 keys per sequence; the workspace function returns 0 for arguments that the call refuses.
+ * impl: -1 automatic: matrix instructions for bf16, head_dim 128, pages of 16 and 4-byte aligned exponents, else 0; 0 a workgroup
+ * per row and query head (any shape). */
 size_t tlt_kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int max_ctx);
 int tlt_kv8_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size,
                       const void *q, int64_t q_stride, const uint64_t *anc_mask, const tlt_kv8 *kv, void *out, void *ws,

@@ -1229,8 +1229,10 @@ int tlt_kv8_write(void* stream, int dtype, int B, int n, int n_q_heads, int n_kv
     return e == hipSuccess ? TLT_OK : TLT_EHIP;
 }
 
+constexpr int kMostKV8Keys = 1 << 26;   // keys of a sequence in tlt_kv8_attention, whose planning counts tiles in 32 bits
+
 size_t tlt_kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int max_ctx) {
-    if (B < 1 || B > 65535 || n < 1 || n > TLT_MAX_TREE || !heads_ok(n_q_heads, n_kv_heads) || head_dim < 64 || head_dim % 64 || head_dim > 256 || max_ctx < 1)
+    if (B < 1 || B > 65535 || n < 1 || n > TLT_MAX_TREE || !heads_ok(n_q_heads, n_kv_heads) || head_dim < 64 || head_dim % 64 || head_dim > 256 || max_ctx < 1 || max_ctx > kMostKV8Keys)
         return 0;
     return kv8_attention_workspace_bytes(B, n, n_q_heads, n_kv_heads, head_dim, max_ctx);
 }
@@ -1242,7 +1244,7 @@ int tlt_kv8_attention(void* stream, int dtype, int B, int n, int n_q_heads, int 
         return TLT_EINVAL;
     const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, n);
     if (rc) return rc;
-    if (!q_rows_ok(q, q_stride, dtype, n_q_heads, head_dim)) return TLT_EINVAL;
+    if (!q_rows_ok(q, q_stride, dtype, n_q_heads, head_dim) || (int64_t)kv->seq_len_bound + n > kMostKV8Keys) return TLT_EINVAL;
     KV8Rows rows;
     rows.B = B;
     rows.n = n;

@@ -55,9 +55,9 @@ __global__ __launch_bounds__(512) void kv8_write_k(const T* __restrict__ qkv, co
     const int r = blockIdx.x, b = r / n, i = r - b * n, d = kv.d, half = d >> 1, n_kv = kv.n_kv;
     const int heads = n_q_heads + 2 * n_kv;
     const T* row = qkv + (int64_t)r * heads * d;
-    const int ctx = max(kv.seq_len[b], 0);
+    const int ctx = min(max(kv.seq_len[b], 0), 0x7fffffff - n);   // (so that no slot number overflows, whatever stands there)
     if ((int)threadIdx.x < half) {
-        const int pos = ctx + (depth ? depth[r] : i);
+        const int64_t pos = (int64_t)ctx + (depth ? depth[r] : i);
         double s, c;
         sincos((double)pos * exp2(-2.0 * (double)threadIdx.x / (double)d * log2_theta), &s, &c);
         cs[threadIdx.x] = (float)c, sn[threadIdx.x] = (float)s;
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kCommitThreads) void kv8_commit_k(int n_layers, KV8
         int64_t src = -1, dst = -1;
         if (tid >= 1 && tid <= a) {
             const int ctx = kv.seq_len[b], p = path_idx[(int64_t)b * stride + tid];
-            if (p > tid && p < 64 && ctx >= 0) src = row_of(kv, b, ctx + p), dst = row_of(kv, b, ctx + tid);
+            if (p > tid && p < 64 && ctx >= 0 && ctx < 0x7fffffff - 64) src = row_of(kv, b, ctx + p), dst = row_of(kv, b, ctx + tid);
         }
         s_src[tid] = dst < 0 ? -1 : src, s_dst[tid] = dst;
     }
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, r = b * rows.n + i, d = kv.d;
     const int kh = hq / (n_q_heads / kv.n_kv);
-    const int ctx = max(kv.seq_len[b], 0), total = ctx + rows.n;
+    const int ctx = min(max(kv.seq_len[b], 0), kv.seq_len_bound), total = ctx + rows.n;
     const uint64_t mask = rows.mask ? rows.mask[r] : (2ull << i) - 1ull;   // (none: the rows up to this one)
     if (tid < d) q_s[tid] = to_float(q[(int64_t)r * q_stride + hq * d + tid]) * scale;
     __syncthreads();
@@ -369,18 +369,21 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
 // device: every wave works them out for itself (up to 256 sequences), which costs less than a kernel in front.
 constexpr int kD = 128, kKT = 64;
 constexpr float kNegBig = -1e30f;
-constexpr int kPlanned = 256;   // sequences whose ranges are balanced
+constexpr int kPlanned = 256;   // most sequences whose ranges are balanced
 
-__device__ __forceinline__ int wave_sum_i(int v) {
+template <typename F>
+__device__ __forceinline__ int wave_all(int v, F op) {
     const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = (int)(a[0] + a[1]);
+    v = op((int)a[0], (int)a[1]);
     const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = (int)(b[0] + b[1]);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);
-    return v;
+    v = op((int)b[0], (int)b[1]);
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false));
+    return op(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false));
+}
+__device__ __forceinline__ int wave_sum_i(int v) {
+    return wave_all(v, [](int x, int y) { return x + y; });
 }
 // the maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float group_max4(float x) {
@@ -398,19 +401,27 @@ struct KV8Item {
 };
 struct KV8Split {
     int slots;         // items that run at once
-    int t_min, t_max;  // shortest and longest range, in tiles
+    int t_max;         // longest range, in tiles
+    bool planned;      // ranges are balanced, else all are of t_max
     int max_items;     // upper bound of the item count, from the host's bound on the lengths
 };
 
-// Item number `item`: false where there is none.  Up to kPlanned sequences: of the range lengths t_min .. t_max the smallest whose items fit the
-// fewest rounds of `slots` that t_max allows; items are numbered sequence by sequence.  Beyond: ranges of t_max, item = range * B + sequence.
+// Shortest range of a sequence of that many tiles: a range's time grows with its length, the joining with the number of ranges, so their best
+// balance grows with the root of the tiles.
+__host__ __device__ __forceinline__ int shortest_range(int tiles) {
+    const int t = (int)sqrtf((float)tiles * (1.f / 7.f));
+    return t < 2 ? 2 : (t > 32 ? 32 : t);
+}
+
+// Item number `item`: false where there is none.  Planned: of the range lengths from the shortest to t_max the smallest whose items fit the
+// fewest rounds of `slots` that t_max allows; items are numbered sequence by sequence.  Not planned: ranges of t_max, item = range * B + sequence.
 __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, int B, int n, int len_bound, const KV8Split& sp, int item, KV8Item& out) {
     const int lane = threadIdx.x & 63;
     auto len_of = [&](int b) { return min(max(seq_len[b], 0), len_bound); };
     auto ceil_div = [](int x, int T) { return (int)__umulhi((uint32_t)(x + T - 1), 0xffffffffu / (uint32_t)T + 1u); };   // (exact: x < 2^26, 2 <= T <= 64)
     // (everything about an item is uniform, and said to be)
     auto give = [&](int b, int len, int tiles, int slot, int first, int k) {
-        const int c = __builtin_amdgcn_readfirstlane(B > kPlanned ? slot / B : slot - first), per = tiles / k, more = tiles - per * k;   // the first `more` ranges are one tile longer
+        const int c = __builtin_amdgcn_readfirstlane(sp.planned ? slot - first : slot / B), per = tiles / k, more = tiles - per * k;   // the first `more` ranges are one tile longer
         out.b = __builtin_amdgcn_readfirstlane(b);
         out.ctx = __builtin_amdgcn_readfirstlane(len);
         out.lo = __builtin_amdgcn_readfirstlane(c * per + min(c, more));
@@ -420,7 +431,7 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
         out.k = __builtin_amdgcn_readfirstlane(k);
         return true;
     };
-    if (B > kPlanned) {
+    if (!sp.planned) {
         const int b = item % B, len = len_of(b), tiles = (len + n + kKT - 1) / kKT, k = (tiles + sp.t_max - 1) / sp.t_max;
         return item / B < k && give(b, len, tiles, item, b, k);
     }
@@ -438,7 +449,10 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
             if (64 * j < B) s += ceil_div(tiles[j], T);
         return wave_sum_i(s);
     };
-    int T = sp.t_min;
+    int longest = 0;
+#pragma unroll
+    for (int j = 0; j < kPlanned / 64; ++j) longest = max(longest, tiles[j]);
+    int T = shortest_range(__builtin_amdgcn_readfirstlane(wave_all(longest, [](int x, int y) { return max(x, y); })));
     if (items(T) > sp.slots) {
         const int most = (items(sp.t_max) + sp.slots - 1) / sp.slots * sp.slots;
         int sum = 0;
@@ -1142,6 +1156,7 @@ struct KV8Plan {
     KV8Split sp;
     bool few;        // the kernel of few rows
     bool one_each;   // no sequence has a second range
+    bool runs;       // the launch fits a grid
     int row_tiles, groups, per_group;
     size_t seg, part_o, part_ml, total;   // byte offsets into the workspace
 };
@@ -1153,11 +1168,19 @@ static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) 
     p.groups = p.few ? 1 : (p.row_tiles + 23) / 24;
     p.per_group = (p.row_tiles + p.groups - 1) / p.groups;
     p.sp.slots = std::max(1, (p.few ? 512 : 256) / (n_kv * p.groups));   // (workgroups that the chip holds)
-    p.sp.t_min = 4;
     p.sp.t_max = 64;
-    p.one_each = tiles <= p.sp.t_min || (B > kPlanned && tiles <= p.sp.t_max);
-    p.sp.max_items = p.one_each ? B : (int)(B > kPlanned ? (int64_t)B * ((tiles + p.sp.t_max - 1) / p.sp.t_max) : (int64_t)B * tiles / p.sp.t_max + B + p.sp.slots);
+    // Planning costs every workgroup some 2 us (7 at 256 sequences) and is worth it where sequences are cut to fill the chip or whole rounds of it: long ones while
+    // the workgroups' rounds are few, any length while there are fewer sequences than places.  Planned / ranges of t_max: 96 sequences of ~4000, 28 and 4 heads, 8 nodes
+    // (64 places) 164 / 198 us; 192 of them 337 / 361; 256, 40 and 8 heads, 16 nodes (32 places) 964 / 899; of ~500: 65, one node (128 places) 17.7 / 21.3; 128 32.4 / 28.2;
+    // 256, 8 nodes, 110 / 83.
+    p.sp.planned = B <= kPlanned && (tiles > p.sp.t_max ? B <= 4 * p.sp.slots : B < p.sp.slots);
+    p.one_each = tiles <= (p.sp.planned ? 2 : p.sp.t_max);
+    // (planned: items that fit `slots`, or those of ranges of t_max rounded up to whole rounds)
+    const int64_t longest = (int64_t)B * ((tiles + p.sp.t_max - 1) / p.sp.t_max);
+    const int64_t rounds = (std::min(longest, (int64_t)B * tiles / p.sp.t_max + B) + p.sp.slots - 1) / p.sp.slots;
+    p.sp.max_items = (int)(p.one_each ? B : (p.sp.planned ? rounds * p.sp.slots : longest));
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    p.runs = (rounds * p.sp.slots + longest) * n_kv * p.groups < (1 << 23);   // (a grid holds fewer than 2^32 threads, the kernel of many rows 512 in a workgroup)
     const size_t rows = (size_t)p.sp.max_items * n_kv * p.row_tiles * 16;
     p.seg = 0;
     p.part_ml = up((size_t)B * sizeof(KV8Seg));
@@ -1169,8 +1192,11 @@ static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) 
 size_t kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int d, int max_ctx) {
     size_t need = 256;
     if (d == kD)
-        for (int m = 1; m <= n; ++m)   // (any number of rows up to n may be asked for later)
-            need = std::max(need, plan_kv8(B, m, n_q_heads, n_kv_heads, max_ctx).total);
+        for (int m = 1; m <= n; ++m) {   // (any number of rows up to n may be asked for later)
+            const KV8Plan p = plan_kv8(B, m, n_q_heads, n_kv_heads, max_ctx);
+            if (!p.runs) return 0;
+            need = std::max(need, p.total);
+        }
     return need;
 }
 
@@ -1180,7 +1206,7 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
     const bool fits = dtype == BF16 && kv.d == kD && kv.page_size == 16 && (((uintptr_t)kv.k_exp | (uintptr_t)kv.v_exp) & 3) == 0;
     if (fits && impl != 0) {
         const KV8Plan p = plan_kv8(rows.B, rows.n, n_q_heads, kv.n_kv, kv.seq_len_bound + rows.n);
-        if (p.total > ws_bytes) return hipErrorInvalidValue;
+        if (!p.runs || p.total > ws_bytes) return hipErrorInvalidValue;
         KV8Seg* seg = (KV8Seg*)((char*)ws + p.seg);
         const KV8Out to{(uint16_t*)out, (float*)((char*)ws + p.part_o), (float*)((char*)ws + p.part_ml), rows.n, n_q_heads, kv.n_kv, p.row_tiles * 16};
         const float scale_log2 = 1.4426950408889634f / sqrtf((float)kD), lazy = 8.0f / scale_log2;
@@ -1194,17 +1220,17 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         else if (p.few) few(kv8_attn_few_k<2>);
         else if (p.per_group <= 4) many(kv8_attn_many_k<1, 2>);
         else if (p.per_group <= 8) many(kv8_attn_many_k<2, 2>);
-        else if (p.per_group <= 12) many(kv8_attn_many_k<3, 2>);
         else if (p.per_group <= 16) many(kv8_attn_many_k<2, 1>);
         else many(kv8_attn_many_k<3, 1>);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.one_each) return e;
         auto join = [&](auto kernel, int blocks) {
             hipLaunchKernelGGL(kernel, dim3(blocks, kv.n_kv, rows.B), dim3(256), 0, s, seg, to.part_o, to.part_ml, (uint16_t*)out, rows.n, n_q_heads, kv.n_kv,
-                               p.row_tiles * 16, rows.B > kPlanned ? rows.B : 1, scale_log2);
+                               p.row_tiles * 16, p.sp.planned ? 1 : rows.B, scale_log2);
         };
-        // the most ranges that a sequence can have: those of one round, fewer where they would be shorter than t_min
-        const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, ranges = std::max(std::min(p.sp.slots, (tiles + p.sp.t_min - 1) / p.sp.t_min), (tiles + 63) / 64);
+        // the most ranges that a sequence can have
+        const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, shortest = shortest_range(tiles);
+        const int ranges = std::max(std::min(p.sp.slots, (tiles + shortest - 1) / shortest), (tiles + p.sp.t_max - 1) / p.sp.t_max);
         if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_k<4>, R);
         else join(kv8_join_k<1>, (R + 3) / 4);
         return hipGetLastError();

@@ -351,6 +351,19 @@ def test_many_sequences(B):
     check_attention(c, "bf16", q, None, run_attention(c, "bf16", q, None), rows=sorted(set(range(0, B, 7)) | set(range(5, B, 50))))
 
 
+@pytest.mark.parametrize("B,n,Hq,Hkv", [(200, 1, 4, 1), (256, 12, 8, 1), (300, 2, 4, 1), (257, 12, 8, 1), (110, 2, 40, 20)])
+def test_many_sequences_a_few_of_them_long(B, n, Hq, Hkv):
+    """More sequences than a wave has lanes, some cut into several ranges: balanced ones, and those of a fixed length."""
+    ctxs = [3 * (i % 11) for i in range(B)]
+    long = {7: 9000, B // 2: 4095, B - 1: 4200}
+    for b, x in long.items():
+        ctxs[b] = x
+    c = m.Cache(ctxs, n, Hkv, 128, 16, seed=4)
+    q = np.random.default_rng(2).standard_normal((B, n, Hq, 128)).astype(np.float32)
+    print("attention,", B, "sequences,", n, "rows", flush=True)
+    check_attention(c, "bf16", q, None, run_attention(c, "bf16", q, None), rows=sorted(set(range(0, B, 13)) | set(long)))
+
+
 def test_offsets_past_32_bits():
     """Pages beyond 4 GB of codes, in every operator."""
     Hq, Hkv, d, page, n = 8, 8, 128, 16, 3

@@ -99,3 +99,13 @@ def test_the_model_of_the_format():
     x = np.random.default_rng(3).standard_normal((50, 64)).astype(np.float32)
     for a, b in zip(m.encode(x), m._encode_fast(x)):
         np.testing.assert_array_equal(a, b)
+
+
+def test_attention_past_what_a_launch_holds():
+    size = tlt.load().tlt_kv8_attention_workspace_bytes
+    long = dict(max_pages=1 << 23)
+    assert attend(handle(seq_len_bound=(1 << 26) - 3, **long)) == -1 and size(2, 4, 8, 2, 128, (1 << 26) + 1) == 0   # n = 4
+    assert size(2, 4, 8, 2, 128, 1 << 26) > 0
+    # 65535 sequences of 8192 ranges each and 64 kv heads
+    assert attend(handle(seq_len_bound=(1 << 25) - 4, **long), B=65535, Hq=64, Hkv=64, stride=64 * 128, bytes=1 << 62) == -2
+    assert size(65535, 4, 64, 64, 128, 1 << 25) == 0
