@@ -402,14 +402,17 @@ struct KV8Item {
 struct KV8Split {
     int slots;         // items that run at once
     int t_max;         // longest range, in tiles
+    int whole;         // sequences of that many tiles are not cut to fill the chip
     bool planned;      // ranges are balanced, else all are of t_max
     int max_items;     // upper bound of the item count, from the host's bound on the lengths
 };
 
-// Shortest range of a sequence of that many tiles: a range's time grows with its length, the joining with the number of ranges, so their best
-// balance grows with the root of the tiles.
-__host__ __device__ __forceinline__ int shortest_range(int tiles) {
-    const int t = (int)sqrtf((float)tiles * (1.f / 7.f));
+// Shortest range where the longest sequence has that many tiles: a range's time grows with its length, the joining with the number of ranges, so their
+// best balance grows with the root of the tiles.  (One sequence, 28 and 4 heads, ranges of 2, 4, 8 and 16: one token at 2048 keys 8.6, 9.8, 10.5, 11.6 us, at 8192
+// 11.8, 9.7, 11.1, 14.0, at 30000 16.3, 15.5, 13.2, 17.0; 8 nodes at 2048 11.8, 14.1, 15.8, 19.3, at 30000 21.9, 21.8, 20.9, 26.1.)  Up to `whole` tiles cost less
+// than a joining (32 sequences of 200 keys with 16 nodes, four tiles: 13 us, cut in two 22).
+__host__ __device__ __forceinline__ int shortest_range(int tiles, int whole) {
+    const int t = tiles <= whole ? tiles : (int)sqrtf((float)tiles * (1.f / 7.f));
     return t < 2 ? 2 : (t > 32 ? 32 : t);
 }
 
@@ -452,7 +455,7 @@ __device__ __forceinline__ bool kv8_item(const int32_t* __restrict__ seq_len, in
     int longest = 0;
 #pragma unroll
     for (int j = 0; j < kPlanned / 64; ++j) longest = max(longest, tiles[j]);
-    int T = shortest_range(__builtin_amdgcn_readfirstlane(wave_all(longest, [](int x, int y) { return max(x, y); })));
+    int T = shortest_range(__builtin_amdgcn_readfirstlane(wave_all(longest, [](int x, int y) { return max(x, y); })), sp.whole);
     if (items(T) > sp.slots) {
         const int most = (items(sp.t_max) + sp.slots - 1) / sp.slots * sp.slots;
         int sum = 0;
@@ -565,9 +568,8 @@ __device__ __forceinline__ void kv8_scores(const KV8Tiles<NT>& x, u32x4_t c0, u3
 }
 // Scores sc[t][s][v] of keys t0 + 16 * s + 4 * g4 + v to weights, packed for the second product: k slot 4 * (s & 1) + v of half s / 2.  behind: t0 less the
 // context's length; edge: some keys are new rows or lie behind the last; mask_of(t, lane): visibility of the lane's row of tile t.
-// SN: groups of 16 keys.
-template <int SN, int NT, typename F>
-__device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][SN], u32x4_t (&pb)[NT][SN / 2], bool edge, int behind, F mask_of, float scale_log2, float lazy) {
+template <int NT, typename F>
+__device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][4], u32x4_t (&pb)[NT][2], bool edge, int behind, F mask_of, float scale_log2, float lazy) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (edge) {
@@ -575,13 +577,13 @@ __device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][S
             asm volatile("" : "+v"(ln));   // (worked out anew where it is wanted: kept through the loop, such values cost registers that the products need)
             const uint64_t seen = seen_from(behind + 4 * (ln >> 4), mask_of(t, ln));
 #pragma unroll
-            for (int s = 0; s < SN; ++s)
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) sc[t][s][v] = seen >> (16 * s + v) & 1ull ? sc[t][s][v] : kNegBig;
         }
         float tmax = kNegBig;
 #pragma unroll
-        for (int s = 0; s < SN; ++s)
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int v = 0; v < 4; ++v) tmax = fmaxf(tmax, sc[t][s][v]);
         // the reference of the exponentials only has to keep them in range: it follows the maximum when some score exceeds it by 2^8
@@ -595,7 +597,7 @@ __device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][S
         }
         const float mc = fmaxf(x.m[t], -1e29f) * scale_log2;   // (rows that have seen nothing yet: exp2(-1e30 * c + 1e29 * c) = 0)
 #pragma unroll
-        for (int s = 0; s < SN; ++s) {
+        for (int s = 0; s < 4; ++s) {
             float e[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(fmaf(sc[t][s][v], scale_log2, -mc));
@@ -747,7 +749,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_
             kv8_scores(x, kc[s][0], kc[s][1], ke[s], kve[s], to_sc);
         }
         if (i + 1 < my_tiles) load_k(i + 1);
-        kv8_weights<4>(x, sc, pb, edge, t0 - ctx, [&](int t, int) { return mask[t]; }, scale_log2, lazy);
+        kv8_weights(x, sc, pb, edge, t0 - ctx, [&](int t, int) { return mask[t]; }, scale_log2, lazy);
         if (edge) {   // (keys behind the last are weighted with zero, and slots that nobody has written may hold anything)
             int ln = lane;
             asm volatile("" : "+v"(ln));
@@ -809,8 +811,7 @@ template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t offset) { return (__attribute__((address_space(3))) T*)(uintptr_t)offset; }
 
 // More rows: bound by the matrix pipe and, side by side with it, the exponentials.  One workgroup of eight waves, two per SIMD, streams the item's range once for up to 24
-// tiles of rows.  With KS = 2 (up to 12 tiles of rows) waves are paired on the rows and take half of a tile's keys each, which halves what a tile
-// costs in reads of LDS; NT: tiles of rows of a wave.  A tile of 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead,
+// tiles of rows, dealt round-robin to the waves (NT each).  A tile of 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead,
 // a wave's eight keys (1 KB each of K and V) to a place that only this wave reads; the wave converts them to bf16 and stores them for all, K rows swizzled by
 // the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by twice the key (a transposing read takes two neighbouring places of each of 8
 // keys).  The two waves of a SIMD run half a period apart, so that one's softmax runs under the other's products: per tile a wave does [P V of the tile
@@ -820,15 +821,15 @@ __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t 
 constexpr int kRaw = 3, kRawBytes = 2 * kKT * kD + 2 * kKT, kStage = kKT * kD * 2;   // (raw: K codes, V codes, exponents of K and V)
 constexpr int kManyLds = 5 * kStage + kRaw * kRawBytes + 64 * 8;
 
-template <int NT, int KS>
+template <int NT>
 __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg, int64_t q_stride, const uint16_t* __restrict__ q, const KV8Rows& rows, const KV8Layer& kv,
                                               const KV8Out& to, int per_group, float scale_log2, float lazy, uint8_t* lds) {
-    constexpr int TPW = NT > 0 ? NT : 1, RW = 8 / KS, SN = 4 / KS;   // waves that share the rows; groups of 16 keys of a tile that a wave takes
+    constexpr int TPW = NT > 0 ? NT : 1;
     typedef __attribute__((ext_vector_type(4))) short s16x4_t;
     typedef __attribute__((ext_vector_type(8))) short s16x8_t;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int b = it.b, ctx = it.ctx, n = rows.n, total = ctx + n, n_kv = kv.n_kv, G = to.n_q_heads / n_kv, R = n * G;
-    const int n_tiles = it.hi - it.lo, k0 = it.lo * kKT, kg = wave % KS, rw = wave / KS;
+    const int n_tiles = it.hi - it.lo, k0 = it.lo * kKT;
     uint8_t* raw = lds + 5 * kStage;   // (the stages first: their places are worked out with exclusive ors below 256)
     uint64_t* mask_lds = (uint64_t*)(raw + kRaw * kRawBytes);
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -855,7 +856,7 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         if (t < n_tiles) fetch(t);
     if (tid < n) mask_lds[tid] = kv8_mask(rows, b, G, tid * G);
     KV8Tiles<TPW> x;
-    if constexpr (NT > 0) kv8_tiles(x, rows, b, kh, G, q, q_stride, [&](int t) { return (rg * per_group + rw + RW * t) * 16; });
+    if constexpr (NT > 0) kv8_tiles(x, rows, b, kh, G, q, q_stride, [&](int t) { return (rg * per_group + wave + 8 * t) * 16; });
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 
     // (with three tiles of rows, places in LDS are worked out anew for every tile: kept, they would cost registers that the products need)
@@ -898,11 +899,11 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
     };
     auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    u32x4_t pb[TPW][2 / KS];   // weights of the tile whose second product is still owed
+    u32x4_t pb[TPW][2];   // weights of the tile whose second product is still owed
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int h = 0; h < 2 / KS; ++h) pb[t][h] = u32x4_t{0u, 0u, 0u, 0u};
+        for (int h = 0; h < 2; ++h) pb[t][h] = u32x4_t{0u, 0u, 0u, 0u};
     // ---- O^T += V^T P^T: a transposing read hands lane (l16, g4) keys 4 * g4 .. + 3 of 16 for d = 16 * dt + l16; two of them are 8 k slots.  Batches of
     // half of d (and half of the keys), each read under the products of the one before.
     auto second = [&](int stage) {
@@ -911,7 +912,7 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         const int ln = place(lane);
         // key 4 * g4 + l16 / 4 of the 16, its piece 2 * dt + (l16 & 3) / 2 swizzled by twice the key (16 keys further on: by the same)
         const int kr = 4 * (ln >> 4) + ((ln & 15) >> 2);
-        const uint32_t at = base + (2 + stage) * kStage + (kg * (SN * 16) + kr) * (2 * kD) + ((((ln & 3) >> 1) ^ ((2 * kr) & 15)) * 16) + (ln & 1) * 8;
+        const uint32_t at = base + (2 + stage) * kStage + kr * (2 * kD) + ((((ln & 3) >> 1) ^ ((2 * kr) & 15)) * 16) + (ln & 1) * 8;
         auto read_v = [&](int half, int dq, s16x4_t (*v)[2]) {
 #pragma unroll
             for (int d4 = 0; d4 < 4; ++d4)
@@ -940,23 +941,17 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         read_v(0, 0, vv[0]);
         read_v(0, 1, vv[1]);
         mul_v(0, 0, vv[0]);
-        if constexpr (KS == 1) {
-            read_v(1, 0, vv[0]);
-            mul_v(0, 1, vv[1]);
-            read_v(1, 1, vv[1]);
-            mul_v(1, 0, vv[0]);
-            mul_v(1, 1, vv[1]);
-            __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 5 * NT, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
-        } else {
-            mul_v(0, 1, vv[1]);
-            __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
-        }
+        read_v(1, 0, vv[0]);
+        mul_v(0, 1, vv[1]);
+        read_v(1, 1, vv[1]);
+        mul_v(1, 0, vv[0]);
+        mul_v(1, 1, vv[1]);
+        __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 5 * NT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 9 * NT, 0);
     };
     const bool late = wave >= 4;
     {
@@ -976,11 +971,11 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         __builtin_amdgcn_s_setprio(2);
         if (i > 0) second((i - 1) % 3);
         // ---- S^T = K Q^T, the next 16 keys' fragments read under the products of those before
-        f32x4_t sc[TPW][SN];
+        f32x4_t sc[TPW][4];
         if constexpr (NT > 0) {
             const int ln = place(lane);
             // key l16 of 16, pieces of 8 elements 2 * g4, 2 * g4 + 1 and 8 further on, swizzled by the key
-            const uint32_t k_at = base + (i & 1) * kStage + (kg * (SN * 16) + (ln & 15)) * (2 * kD) + (((2 * (ln >> 4)) ^ (ln & 15)) * 16);
+            const uint32_t k_at = base + (i & 1) * kStage + (ln & 15) * (2 * kD) + (((2 * (ln >> 4)) ^ (ln & 15)) * 16);
             bf16x8_t kf[2][4];
             auto read_k = [&](int s, bf16x8_t* f) {
 #pragma unroll
@@ -999,23 +994,17 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
             read_k(0, kf[0]);
             read_k(1, kf[1]);
             mul_k(0, kf[0]);
-            if constexpr (KS == 1) {
-                read_k(2, kf[0]);
-                mul_k(1, kf[1]);
-                read_k(3, kf[1]);
-                mul_k(2, kf[0]);
-                mul_k(3, kf[1]);
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
-            } else {
-                mul_k(1, kf[1]);
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
-            }
+            read_k(2, kf[0]);
+            mul_k(1, kf[1]);
+            read_k(3, kf[1]);
+            mul_k(2, kf[0]);
+            mul_k(3, kf[1]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4 * NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 8 * NT, 0);
         }
         __builtin_amdgcn_s_setprio(0);
         if (late && i + 1 < n_tiles) meet();
@@ -1024,9 +1013,9 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         Raw r;
         if (next < n_tiles) read_raw(next, r);
         if constexpr (NT > 0)
-            kv8_weights<SN>(x, sc, pb, k0 + i * kKT + kKT > ctx, k0 + i * kKT + kg * (SN * 16) - ctx,
+            kv8_weights(x, sc, pb, k0 + i * kKT + kKT > ctx, k0 + i * kKT - ctx,
                             [&](int t, int ln) {
-                                const int row = (rg * per_group + rw + RW * t) * 16 + (ln & 15);
+                                const int row = (rg * per_group + wave + 8 * t) * 16 + (ln & 15);
                                 return row < R ? mask_lds[row / G] : 0ull;
                             },
                             scale_log2, lazy);
@@ -1035,38 +1024,10 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         __builtin_amdgcn_sched_barrier(0);
     }
     second((n_tiles - 1) % 3);
-    if constexpr (KS > 1) {   // the waves of a row's two halves of the keys joined, by way of the stages
-        static_assert(KS == 2, "one partner");
-        f32x4_t* other = (f32x4_t*)lds + rw * (3 * 8 * 64) + lane;                            // [rw][t][dt][lane]
-        float2* other_ml = (float2*)((f32x4_t*)lds + RW * 3 * 8 * 64) + rw * (3 * 64) + lane;   // [rw][t][lane]
-        meet();
-        if (kg == 1) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) other[(t * 8 + dt) * 64] = x.acc[t][dt];
-                other_ml[t * 64] = make_float2(x.m[t], x.l[t][0]);
-            }
-        }
-        meet();
-        if (kg == 1) return;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float2 o = other_ml[t * 64];
-            const float M = fmaxf(x.m[t], o.x), w0 = __builtin_amdgcn_exp2f((x.m[t] - M) * scale_log2), w1 = __builtin_amdgcn_exp2f((o.x - M) * scale_log2);
-            x.m[t] = M;
-            x.l[t][0] = w0 * x.l[t][0] + w1 * o.y;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                if ((dt & 3) == 0) asm volatile("" ::: "memory");   // (a few reads at a time)
-                x.acc[t][dt] = w0 * x.acc[t][dt] + w1 * other[(t * 8 + dt) * 64];
-            }
-        }
-    }
     // ---- lane (l16, g4) holds d = 16 * dt + 4 * g4 + v of row l16
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int row = (rg * per_group + rw + RW * t) * 16 + l16;
+        const int row = (rg * per_group + wave + 8 * t) * 16 + l16;
         if (row >= R) continue;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0]);
@@ -1075,7 +1036,7 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
 
 // Workgroup id -> (item, kv head, group of row tiles).  Ids are dealt round-robin over the 8 XCDs, and the groups of one (item, kv head) read the same keys and
 // values: they get ids 8 apart, so that they run on one XCD at the same time.
-template <int TPW, int KS>
+template <int TPW>
 __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
                                                        KV8Seg* __restrict__ seg, int row_tiles, int groups, int per_group, float scale_log2, float lazy) {
     __shared__ __align__(256) uint8_t lds[kManyLds];
@@ -1085,15 +1046,234 @@ __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int64_t q_st
     if (!kv8_item(kv.seq_len, rows.B, rows.n, kv.seq_len_bound, sp, item, it)) return;   // uniform
     if (kh == 0 && rg == 0 && it.slot == it.first && threadIdx.x == 0) seg[it.b] = KV8Seg{it.first, it.k};
     // row tiles of this wave (a wave runs the program for as many as it has; all pass the same barriers)
-    constexpr int RW = 8 / KS;
-    const int rw = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / KS;
-    const int mine = min(per_group, row_tiles - rg * per_group), n_on = mine > rw ? (mine - rw + RW - 1) / RW : 0;
-#define TLT_BODY(N) kv8_many_body<N, KS>(it, kh, rg, q_stride, q, rows, kv, to, per_group, scale_log2, lazy, lds)
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int mine = min(per_group, row_tiles - rg * per_group), n_on = mine > wave ? (mine - wave + 7) / 8 : 0;
+#define TLT_BODY(N) kv8_many_body<N>(it, kh, rg, q_stride, q, rows, kv, to, per_group, scale_log2, lazy, lds)
     if (n_on >= TPW) TLT_BODY(TPW);
     else if (TPW >= 2 && n_on == TPW - 1) TLT_BODY((TPW >= 2 ? TPW - 1 : 0));
     else if (TPW >= 3 && n_on == TPW - 2) TLT_BODY((TPW >= 3 ? TPW - 2 : 0));
     else TLT_BODY(0);
 #undef TLT_BODY
+}
+
+// Up to 8 tiles of rows: workgroups of four waves, two of them on a CU, so that one's softmax runs under the other's products and one's end and the next one's
+// start under the other's work.  They stream the item's range for all tiles of rows, dealt round-robin to the waves (NT each).  A tile of 64 keys passes
+// through LDS twice: its codes come from memory by direct loads, two tiles ahead, a wave's page (2 KB each of K and V) to a place that only this wave reads;
+// the wave converts them to bf16 and stores them for all, K rows swizzled by the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by
+// twice the key (a transposing read takes two neighbouring places of each of 8 keys).  There is one stage of either: V of a tile is converted
+// under Q K^T, K of the next one under P V.
+constexpr int kMidRaw = 2, kMidLds = 2 * kStage + kMidRaw * kRawBytes + 64 * 8;
+
+template <int NT>
+__device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t q_stride, const uint16_t* __restrict__ q, const KV8Rows& rows, const KV8Layer& kv,
+                                              const KV8Out& to, float scale_log2, float lazy, uint8_t* lds) {
+    constexpr int TPW = NT > 0 ? NT : 1;
+    typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+    typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
+    const int b = it.b, ctx = it.ctx, n = rows.n, total = ctx + n, n_kv = kv.n_kv, G = to.n_q_heads / n_kv, R = n * G;
+    const int n_tiles = it.hi - it.lo, k0 = it.lo * kKT;
+    uint8_t* raw = lds + 2 * kStage;   // (the stages first: their places are worked out with exclusive ors below 256)
+    uint64_t* mask_lds = (uint64_t*)(raw + kMidRaw * kRawBytes);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+
+    int pages;   // lane t: this wave's page of tile t (a range is 64 tiles at most); -1: none
+    {
+        const int lp = (it.lo + lane) * 4 + wave;
+        pages = lane < n_tiles && lp < kv.max_pages && lp * 16 < total ? kv.block_table[(int64_t)b * kv.max_pages + lp] : -1;
+        pages = pages < kv.n_pages ? pages : -1;
+    }
+    constexpr int kOps = 6;   // loads of a fetch
+    auto fetch = [&](int t) {   // (of a page that is not there, page 0 instead: the conversion does not look)
+        const int64_t row = ((int64_t)max(__builtin_amdgcn_readlane(pages, t), 0) * n_kv + kh) * 16;
+        const uint32_t at = __builtin_amdgcn_readfirstlane(base + 2 * kStage + (t & 1) * kRawBytes);
+        dma_16(kv.k + row * kD, lane * 16, at + wave * 2048);
+        dma_16(kv.k + row * kD + 1024, lane * 16, at + wave * 2048 + 1024);
+        dma_16(kv.v + row * kD, lane * 16, at + kKT * kD + wave * 2048);
+        dma_16(kv.v + row * kD + 1024, lane * 16, at + kKT * kD + wave * 2048 + 1024);
+        if (lane < 4) dma_4(kv.k_exp + row, lane * 4, at + 2 * kKT * kD + wave * 16);
+        if (lane < 4) dma_4(kv.v_exp + row, lane * 4, at + 2 * kKT * kD + kKT + wave * 16);
+    };
+    fetch(0);
+    if (n_tiles > 1) fetch(1);
+    if (tid < n) mask_lds[tid] = kv8_mask(rows, b, G, tid * G);
+    KV8Tiles<TPW> x;
+    if constexpr (NT > 0) kv8_tiles(x, rows, b, kh, G, q, q_stride, [&](int t) { return (wave + 4 * t) * 16; });
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+    // this wave's page of a tile in registers, of K or V: 16 codes of rows lane / 8 and 8 + lane / 8, and the rows' exponents (of K: of V too)
+    struct Raw {
+        u32x4_t c[2];
+        uint32_t e[2], ev[2];
+    };
+    auto read_raw = [&](int t, bool v, Raw& r) {
+        const int ln = lane;
+        const uint8_t* p = raw + (t & 1) * kRawBytes;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            r.c[j] = *(const u32x4_t*)(p + (v ? kKT * kD : 0) + wave * 2048 + j * 1024 + ln * 16);
+            r.ev[j] = p[2 * kKT * kD + kKT + wave * 16 + 8 * j + (ln >> 3)];
+            if (!v) r.e[j] = p[2 * kKT * kD + wave * 16 + 8 * j + (ln >> 3)];
+        }
+    };
+    auto backed = [&](int t) { return __builtin_amdgcn_readlane(pages, t) >= 0; };
+    auto write_k = [&](Raw& r, bool there) {
+        const int ln = lane;
+        for (int rep = there ? 1 : 0; rep < 1; ++rep)   // (a loop, which stays a branch)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) r.c[j] = u32x4_t{0u, 0u, 0u, 0u}, r.e[j] = r.ev[j] = 127u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
+            // (values that are not finite: their codes are zero, the NaN comes through the key, whose score only rows that see it keep)
+            const float s = __uint_as_float((r.ev[j] == 255u ? 255u : r.e[j]) << 23);
+            uint8_t* o = lds + key * (2 * kD);
+            *(u32x4_t*)(o + ((2 * p) ^ (key & 15)) * 16) = cvt8(r.c[j][0], r.c[j][1], s);
+            *(u32x4_t*)(o + ((2 * p + 1) ^ (key & 15)) * 16) = cvt8(r.c[j][2], r.c[j][3], s);
+        }
+    };
+    auto write_v = [&](Raw& r, int t, bool there) {
+        const int ln = lane;
+        const int left = there ? total - k0 - t * kKT : 0;   // (slots that nobody has written may hold anything)
+        for (int rep = left < kKT ? 0 : 1; rep < 1; ++rep)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) r.c[j][y] = 16 * wave + 8 * j + (ln >> 3) < left ? r.c[j][y] : 0u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
+            const float s = __uint_as_float((r.ev[j] == 255u ? 127u : r.ev[j]) << 23);
+            uint8_t* o = lds + kStage + key * (2 * kD);
+            *(u32x4_t*)(o + ((2 * p) ^ ((2 * key) & 15)) * 16) = cvt8(r.c[j][0], r.c[j][1], s);
+            *(u32x4_t*)(o + ((2 * p + 1) ^ ((2 * key) & 15)) * 16) = cvt8(r.c[j][2], r.c[j][3], s);
+        }
+    };
+    auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    bool there = backed(0);
+    {
+        Raw r;
+        read_raw(0, false, r);
+        write_k(r, there);
+    }
+    for (int i = 0; i < n_tiles; ++i) {
+        meet();   // K of tile i stands in its stage, and V's is free
+        Raw rv, rk;
+        read_raw(i, true, rv);
+        f32x4_t sc[TPW][4];
+        u32x4_t pb[TPW][2];
+        if constexpr (NT > 0) {
+            const int ln = lane;
+            // key l16 of 16, pieces of 8 elements 2 * g4, 2 * g4 + 1 and 8 further on, swizzled by the key
+            const uint32_t k_at = base + (ln & 15) * (2 * kD) + (((2 * (ln >> 4)) ^ (ln & 15)) * 16);
+            bf16x8_t kf[2][4];
+            auto read_k = [&](int s, bf16x8_t* f) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    f[ks] = __builtin_bit_cast(bf16x8_t, *lds_at<u32x4_t>((k_at ^ (uint32_t)((ks >> 1) * 128 + (ks & 1) * 16)) + s * 16 * (2 * kD)));
+            };
+            auto mul_k = [&](int s, const bf16x8_t* f) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sc[t][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[ks], __builtin_bit_cast(bf16x8_t, x.q[t][ks]), sc[t][s], 0, 0, 0);
+            };
+            read_k(0, kf[0]);
+            read_k(1, kf[1]);
+            mul_k(0, kf[0]);
+            read_k(2, kf[0]);
+            mul_k(1, kf[1]);
+            read_k(3, kf[1]);
+            mul_k(2, kf[0]);
+            mul_k(3, kf[1]);
+        }
+        write_v(rv, i, there);
+        meet();   // V of tile i stands, and K's stage is free; this wave has read tile i's codes
+        if (i + 2 < n_tiles) fetch(i + 2);
+        const bool more = i + 1 < n_tiles;
+        if (more) {
+            if (i + 2 < n_tiles) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kOps) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            there = backed(i + 1);
+            read_raw(i + 1, false, rk);
+        }
+        if constexpr (NT > 0)
+            kv8_weights(x, sc, pb, k0 + i * kKT + kKT > ctx, k0 + i * kKT - ctx,
+                            [&](int t, int ln) {
+                                const int row = (wave + 4 * t) * 16 + (ln & 15);
+                                return row < R ? mask_lds[row / G] : 0ull;
+                            },
+                            scale_log2, lazy);
+        if (more) write_k(rk, there);
+        if constexpr (NT > 0) {
+            // O^T += V^T P^T: a transposing read hands lane (l16, g4) keys 4 * g4 .. + 3 of 16 for d = 16 * dt + l16; two of them are 8 k slots
+            s16x4_t vv[2][4][2];
+            const int ln = lane;
+            // key 4 * g4 + l16 / 4 of the 16, its piece 2 * dt + (l16 & 3) / 2 swizzled by twice the key (16 keys further on: by the same)
+            const int kr = 4 * (ln >> 4) + ((ln & 15) >> 2);
+            const uint32_t at = base + kStage + kr * (2 * kD) + ((((ln & 3) >> 1) ^ ((2 * kr) & 15)) * 16) + (ln & 1) * 8;
+            auto read_v = [&](int half, int dq, s16x4_t (*v)[2]) {
+#pragma unroll
+                for (int d4 = 0; d4 < 4; ++d4)
+#pragma unroll
+                    for (int sub = 0; sub < 2; ++sub) {
+                        const uint32_t vp = (at ^ (uint32_t)((dq * 4 + d4) * 32)) + (half * 32 + sub * 16) * (2 * kD);
+                        v[d4][sub] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4_t>(vp));
+                    }
+            };
+            auto mul_v = [&](int half, int dq, s16x4_t (*v)[2]) {
+                if (dq == 0) {   // the weights' sum: the same product against ones
+                    const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        x.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, pb[t][half]), x.l[t], 0, 0, 0);
+                }
+#pragma unroll
+                for (int d4 = 0; d4 < 4; ++d4) {
+                    const s16x8_t a = {v[d4][0][0], v[d4][0][1], v[d4][0][2], v[d4][0][3], v[d4][1][0], v[d4][1][1], v[d4][1][2], v[d4][1][3]};
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        x.acc[t][dq * 4 + d4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, pb[t][half]),
+                                                                                        x.acc[t][dq * 4 + d4], 0, 0, 0);
+                }
+            };
+            read_v(0, 0, vv[0]);
+            read_v(0, 1, vv[1]);
+            mul_v(0, 0, vv[0]);
+            read_v(1, 0, vv[0]);
+            mul_v(0, 1, vv[1]);
+            read_v(1, 1, vv[1]);
+            mul_v(1, 0, vv[0]);
+            mul_v(1, 1, vv[1]);
+        }
+    }
+    // ---- lane (l16, g4) holds d = 16 * dt + 4 * g4 + v of row l16
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = (wave + 4 * t) * 16 + l16;
+        if (row >= R) continue;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0]);
+    }
+}
+
+template <int TPW>
+__global__ __launch_bounds__(256, 2) void kv8_attn_mid_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
+                                                         KV8Seg* __restrict__ seg, int row_tiles, float scale_log2, float lazy) {
+    __shared__ __align__(256) uint8_t lds[kMidLds];
+    const int item = blockIdx.x / kv.n_kv, kh = blockIdx.x - item * kv.n_kv;
+    KV8Item it;
+    if (!kv8_item(kv.seq_len, rows.B, rows.n, kv.seq_len_bound, sp, item, it)) return;   // uniform
+    if (kh == 0 && it.slot == it.first && threadIdx.x == 0) seg[it.b] = KV8Seg{it.first, it.k};
+    // (a wave runs the program for as many row tiles as it has; all pass the same barriers)
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n_on = row_tiles > wave ? (row_tiles - wave + 3) / 4 : 0;
+    if (n_on >= TPW) kv8_mid_body<TPW>(it, kh, q_stride, q, rows, kv, to, scale_log2, lazy, lds);
+    else if (n_on == TPW - 1) kv8_mid_body<TPW - 1>(it, kh, q_stride, q, rows, kv, to, scale_log2, lazy, lds);
+    else kv8_mid_body<0>(it, kh, q_stride, q, rows, kv, to, scale_log2, lazy, lds);
 }
 
 // The ranges of a sequence joined: WPR waves per row, 16 ranges of each requested together, added up in a fixed order; the lanes read a range's maximum and
@@ -1154,7 +1334,7 @@ __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg
 
 struct KV8Plan {
     KV8Split sp;
-    bool few;        // the kernel of few rows
+    bool few, mid;   // the kernels of few rows and of up to 8 tiles of rows
     bool one_each;   // no sequence has a second range
     bool runs;       // the launch fits a grid
     int row_tiles, groups, per_group;
@@ -1164,17 +1344,22 @@ static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) 
     KV8Plan p;
     const int R = n * (n_q_heads / n_kv), tiles = (bound_total + kKT - 1) / kKT;
     p.row_tiles = (R + 15) / 16;
+    // Which kernel, 28 and 4 heads unless said otherwise.  Two tiles of rows: few / mid 38.4 / 42.0 us for 16 sequences of 8192 with 4 nodes, 39.4 / 49.1 for 32 of ~4096
+    // (32 and 8 heads, 16 of 8192: 58.3 / 56.1); a third tile has no registers there.  Mid / many: 4 tiles of rows, 256 of ~4000, 363 / 466; 5 tiles (40 and
+    // 8 heads), 256 of ~4000, 763 / 897; 7 tiles, 16 of 8192, 62.0 / 61.8; 21 tiles, 32 of ~4096, 141 (three a wave, in two groups) / 122.
     p.few = p.row_tiles <= 2;
+    p.mid = !p.few && p.row_tiles <= 8;
     p.groups = p.few ? 1 : (p.row_tiles + 23) / 24;
     p.per_group = (p.row_tiles + p.groups - 1) / p.groups;
-    p.sp.slots = std::max(1, (p.few ? 512 : 256) / (n_kv * p.groups));   // (workgroups that the chip holds)
+    p.sp.slots = std::max(1, (p.few || p.mid ? 512 : 256) / (n_kv * p.groups));   // (workgroups that the chip holds)
     p.sp.t_max = 64;
+    p.sp.whole = p.few ? 8 : 4;
     // Planning costs every workgroup some 2 us (7 at 256 sequences) and is worth it where sequences are cut to fill the chip or whole rounds of it: long ones while
     // the workgroups' rounds are few, any length while there are fewer sequences than places.  Planned / ranges of t_max: 96 sequences of ~4000, 28 and 4 heads, 8 nodes
     // (64 places) 164 / 198 us; 192 of them 337 / 361; 256, 40 and 8 heads, 16 nodes (32 places) 964 / 899; of ~500: 65, one node (128 places) 17.7 / 21.3; 128 32.4 / 28.2;
     // 256, 8 nodes, 110 / 83.
     p.sp.planned = B <= kPlanned && (tiles > p.sp.t_max ? B <= 4 * p.sp.slots : B < p.sp.slots);
-    p.one_each = tiles <= (p.sp.planned ? 2 : p.sp.t_max);
+    p.one_each = tiles <= (p.sp.planned ? p.sp.whole : p.sp.t_max);
     // (planned: items that fit `slots`, or those of ranges of t_max rounded up to whole rounds)
     const int64_t longest = (int64_t)B * ((tiles + p.sp.t_max - 1) / p.sp.t_max);
     const int64_t rounds = (std::min(longest, (int64_t)B * tiles / p.sp.t_max + B) + p.sp.slots - 1) / p.sp.slots;
@@ -1212,16 +1397,17 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         const float scale_log2 = 1.4426950408889634f / sqrtf((float)kD), lazy = 8.0f / scale_log2;
         const unsigned pairs = (unsigned)(p.sp.max_items * kv.n_kv);
         auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pairs), dim3(256), 0, s, p.sp, q_stride, (const uint16_t*)q, rows, kv, to, seg, scale_log2, lazy); };
+        auto mid = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pairs), dim3(256), 0, s, p.sp, q_stride, (const uint16_t*)q, rows, kv, to, seg, p.row_tiles, scale_log2, lazy); };
         auto many = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((pairs + 7) / 8 * 8 * p.groups), dim3(512), 0, s, p.sp, q_stride, (const uint16_t*)q, rows, kv, to, seg, p.row_tiles, p.groups,
                                p.per_group, scale_log2, lazy);
         };
         if (p.row_tiles == 1) few(kv8_attn_few_k<1>);
         else if (p.few) few(kv8_attn_few_k<2>);
-        else if (p.per_group <= 4) many(kv8_attn_many_k<1, 2>);
-        else if (p.per_group <= 8) many(kv8_attn_many_k<2, 2>);
-        else if (p.per_group <= 16) many(kv8_attn_many_k<2, 1>);
-        else many(kv8_attn_many_k<3, 1>);
+        else if (p.row_tiles <= 4) mid(kv8_attn_mid_k<1>);
+        else if (p.mid) mid(kv8_attn_mid_k<2>);
+        else if (p.per_group <= 16) many(kv8_attn_many_k<2>);
+        else many(kv8_attn_many_k<3>);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.one_each) return e;
         auto join = [&](auto kernel, int blocks) {
@@ -1229,7 +1415,7 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
                                p.row_tiles * 16, p.sp.planned ? 1 : rows.B, scale_log2);
         };
         // the most ranges that a sequence can have
-        const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, shortest = shortest_range(tiles);
+        const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, shortest = shortest_range(tiles, p.sp.whole);
         const int ranges = std::max(std::min(p.sp.slots, (tiles + shortest - 1) / shortest), (tiles + p.sp.t_max - 1) / p.sp.t_max);
         if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_k<4>, R);
         else join(kv8_join_k<1>, (R + 3) / 4);
