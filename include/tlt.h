@@ -362,14 +362,14 @@ typedef struct tlt_kv8 {
  * (NULL: none), q and k are rotated at position seq_len[b] + depth[b][i] (depth DEVICE [B][n]; NULL: i), and keys and values go to
  * slot seq_len[b] + i.  The rotated queries go to q_out: rows of Hq*d elements of dtype, q_stride elements apart (a multiple of
  * 16 bytes, at least Hq*d); q_out may be qkv with q_stride = (Hq+2Hkv)*d.  seq_len is unchanged.  qkv, bqkv and q_out
- * are 16-byte aligned.  Any n >= 1. */
+ * are 16-byte aligned.  Any n >= 1, B * n < 2^23. */
 int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size,
                   float rope_theta, const void *qkv, const void *bqkv, const int32_t *depth, const tlt_kv8 *kv, void *q_out,
                   int64_t q_stride);
 
 /* Attention of the rows that tlt_kv8_write has written (n <= TLT_MAX_TREE per sequence): row (b, i) attends to every slot below
  * seq_len[b] and to slot seq_len[b] + j (j < n) where bit j of anc_mask[b][i] is set (anc_mask NULL: j <= i, a chain); a row that
- * sees nothing gives zeros.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
+ * sees nothing gives zeros.  Scores are taken to lie within +-1e29.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
  * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
  * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
  * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).

@@ -1218,12 +1218,12 @@ static bool q_rows_ok(const void* q, int64_t stride, int dtype, int n_q_heads, i
 
 int tlt_kv8_write(void* stream, int dtype, int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int page_size, float rope_theta, const void* qkv,
                   const void* bqkv, const int32_t* depth, const tlt_kv8* kv, void* q_out, int64_t q_stride) {
-    if ((dtype != TLT_F32 && dtype != TLT_BF16) || n < 1 || !(rope_theta > 0.f) || !heads_ok(n_q_heads, n_kv_heads) || !qkv ||
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || n < 1 || !(rope_theta > 0.f) || rope_theta > 3.0e38f || !heads_ok(n_q_heads, n_kv_heads) || !qkv ||
         (((uintptr_t)qkv | (uintptr_t)bqkv) & 15) != 0)
         return TLT_EINVAL;
     const int rc = check_kv8(kv, B, n_kv_heads, head_dim, page_size, n);
     if (rc) return rc;
-    if (!q_rows_ok(q_out, q_stride, dtype, n_q_heads, head_dim) || (int64_t)B * n > 0x7fffffff) return TLT_EINVAL;
+    if (!q_rows_ok(q_out, q_stride, dtype, n_q_heads, head_dim) || (int64_t)B * n >= (1 << 23)) return TLT_EINVAL;   // (a workgroup per row)
     const hipError_t e = kv8_write((hipStream_t)stream, dtype, B, n, kv8_layer(kv, n_kv_heads, head_dim, page_size), qkv, bqkv, depth, n_q_heads, rope_theta,
                                    q_out, q_stride);
     return e == hipSuccess ? TLT_OK : TLT_EHIP;

@@ -62,6 +62,8 @@ def test_write():
         assert write(**over) == -1, over
     assert write(dtype=0, stride=8 * 128 + 2) == -1        # fp32 rows: 16 bytes are four elements
     assert write(n=61) == -3                              # 100 + 61 rows
+    assert write(theta=float("inf")) == -1
+    assert write(handle(max_pages=1 << 23), B=2, n=1 << 22) == -1   # more rows than a launch has workgroups
 
 
 def test_attention():
