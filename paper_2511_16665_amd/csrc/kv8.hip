@@ -202,62 +202,74 @@ hipError_t kv8_read(hipStream_t s, int dtype, int n_layers, int B, int n, const 
 // ---- commit
 // Row seq_len + path[j] -> row seq_len + j, j = 1 .. accept_len.  A thread owns one 16-byte column of a (layer, kv head)'s K or V rows, or the exponent
 // bytes of either, for all j, and walks j upward in batches of 8 (8 loads in flight, then 8 stores).  A row that is written can only be the source
-// of an earlier j (path[j] >= j), which the same thread has read by then.
-constexpr int kCommitThreads = 256;
-__global__ __launch_bounds__(kCommitThreads) void kv8_commit_k(int n_layers, KV8Layer kv, const int32_t* __restrict__ accept_len,
-                                                               const int32_t* __restrict__ path_idx, int stride) {
+// of an earlier j (path[j] >= j), which the same thread has read by then.  ONE: a workgroup has all columns of its sequence and advances the length too;
+// else workgroups of a sequence may still have to read it, and a second kernel does.
+__device__ __forceinline__ int accepted(const int32_t* __restrict__ accept_len, int b, int stride) { return max(min(accept_len[b], min(stride - 1, 63)), 0); }
+
+template <bool ONE>
+__global__ __launch_bounds__(1024) void kv8_commit_k(int n_layers, KV8Layer kv, int32_t* __restrict__ seq_len, const int32_t* __restrict__ accept_len,
+                                                     const int32_t* __restrict__ path_idx, int stride) {
     __shared__ int64_t s_src[64], s_dst[64];
     const int b = blockIdx.y, tid = threadIdx.x;
-    const int a = min(accept_len[b], min(stride - 1, 63));
-    if (a <= 0) return;
+    const int a = accepted(accept_len, b, stride);
+    if (!ONE && a == 0) return;
     if (tid < 64) {
         int64_t src = -1, dst = -1;
+        const int ctx = seq_len[b];
         if (tid >= 1 && tid <= a) {
-            const int ctx = kv.seq_len[b], p = path_idx[(int64_t)b * stride + tid];
+            const int p = path_idx[(int64_t)b * stride + tid];
             if (p > tid && p < 64 && ctx >= 0 && ctx < 0x7fffffff - 64) src = row_of(kv, b, ctx + p), dst = row_of(kv, b, ctx + tid);
         }
         s_src[tid] = dst < 0 ? -1 : src, s_dst[tid] = dst;
+        if (ONE && tid == 0) seq_len[b] = ctx + a + 1;
     }
     __syncthreads();
-    const int cols = kv.d / 16, per_head = 2 * cols + 2;
+    const int cols = kv.d / 16, per_head = 2 * cols + 2, units = a > 0 ? n_layers * kv.n_kv * per_head : 0;
     const int64_t rows_per_layer = kv.n_pages * kv.n_kv * kv.page_size;
-    const int u = blockIdx.x * kCommitThreads + tid;
-    if (u >= n_layers * kv.n_kv * per_head) return;
-    const int head = u / per_head, c = u - head * per_head, layer = head / kv.n_kv, kh = head - layer * kv.n_kv;
-    const int64_t base = layer * rows_per_layer + (int64_t)kh * kv.page_size;
-    if (c < 2 * cols) {
-        uint8_t* pool = (c < cols ? kv.k : kv.v) + base * kv.d + (c < cols ? c : c - cols) * 16;
-        for (int j0 = 1; j0 <= a; j0 += 8) {
-            u32x4_t t[8];
+    for (int u = blockIdx.x * blockDim.x + tid; u < units; u += gridDim.x * blockDim.x) {
+        const int head = u / per_head, c = u - head * per_head, layer = head / kv.n_kv, kh = head - layer * kv.n_kv;
+        const int64_t base = layer * rows_per_layer + (int64_t)kh * kv.page_size;
+        if (c < 2 * cols) {
+            uint8_t* pool = (c < cols ? kv.k : kv.v) + base * kv.d + (c < cols ? c : c - cols) * 16;
+            for (int j0 = 1; j0 <= a; j0 += 8) {
+                u32x4_t t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j0 + e <= a && s_src[j0 + e] >= 0) t[e] = *(const u32x4_t*)(pool + s_src[j0 + e] * kv.d);
+                for (int e = 0; e < 8; ++e)
+                    if (j0 + e <= a && s_src[j0 + e] >= 0) t[e] = *(const u32x4_t*)(pool + s_src[j0 + e] * kv.d);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j0 + e <= a && s_src[j0 + e] >= 0) *(u32x4_t*)(pool + s_dst[j0 + e] * kv.d) = t[e];
-        }
-    } else {
-        uint8_t* pool = (c == 2 * cols ? kv.k_exp : kv.v_exp) + base;
-        for (int j0 = 1; j0 <= a; j0 += 8) {
-            uint8_t t[8];
+                for (int e = 0; e < 8; ++e)
+                    if (j0 + e <= a && s_src[j0 + e] >= 0) *(u32x4_t*)(pool + s_dst[j0 + e] * kv.d) = t[e];
+            }
+        } else {
+            uint8_t* pool = (c == 2 * cols ? kv.k_exp : kv.v_exp) + base;
+            for (int j0 = 1; j0 <= a; j0 += 8) {
+                uint8_t t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j0 + e <= a && s_src[j0 + e] >= 0) t[e] = pool[s_src[j0 + e]];
+                for (int e = 0; e < 8; ++e)
+                    if (j0 + e <= a && s_src[j0 + e] >= 0) t[e] = pool[s_src[j0 + e]];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (j0 + e <= a && s_src[j0 + e] >= 0) pool[s_dst[j0 + e]] = t[e];
+                for (int e = 0; e < 8; ++e)
+                    if (j0 + e <= a && s_src[j0 + e] >= 0) pool[s_dst[j0 + e]] = t[e];
+            }
         }
     }
 }
 
 __global__ void kv8_advance_k(int B, int32_t* __restrict__ seq_len, const int32_t* __restrict__ accept_len, int stride) {
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < B) seq_len[b] += max(min(accept_len[b], min(stride - 1, 63)), 0) + 1;
+    if (b < B) seq_len[b] += accepted(accept_len, b, stride) + 1;
 }
 
 hipError_t kv8_commit(hipStream_t s, int n_layers, int B, const KV8Layer& kv, int32_t* seq_len, const int32_t* accept_len, const int32_t* path_idx, int stride) {
     const int64_t units = (int64_t)n_layers * kv.n_kv * (2 * (kv.d / 16) + 2);
-    hipLaunchKernelGGL(kv8_commit_k, dim3((unsigned)((units + kCommitThreads - 1) / kCommitThreads), B), dim3(kCommitThreads), 0, s, n_layers, kv, accept_len, path_idx, stride);
+    // One launch / two, us in a captured graph behind a fill kernel, 32 sequences, 4 heads of 128: 1 layer (136 columns) 7.1 / 8.7, 4 layers 7.4 / 8.9, 28 layers (3808) 10.7 / 9.4, but
+    // outside a graph the launch costs its caller 3.6 us; 64 layers and 8 heads (17408) 36.6 / 13.0.
+    if (units <= 4096) {
+        const int threads = (int)std::min<int64_t>(1024, (units + 63) / 64 * 64);
+        hipLaunchKernelGGL(kv8_commit_k<true>, dim3(1, B), dim3(threads), 0, s, n_layers, kv, seq_len, accept_len, path_idx, stride);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(kv8_commit_k<false>, dim3((unsigned)((units + 255) / 256), B), dim3(256), 0, s, n_layers, kv, seq_len, accept_len, path_idx, stride);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kv8_advance_k, dim3((B + 63) / 64), dim3(64), 0, s, B, seq_len, accept_len, stride);

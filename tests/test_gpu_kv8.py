@@ -398,7 +398,7 @@ def test_offsets_past_32_bits():
 
 # ---- commit
 
-@pytest.mark.parametrize("Hkv,d,page,L,n", [(4, 128, 16, 5, 24), (2, 64, 16, 2, 64), (1, 192, 5, 1, 9), (3, 256, 16, 2, 17)])
+@pytest.mark.parametrize("Hkv,d,page,L,n", [(4, 128, 16, 5, 24), (2, 64, 16, 2, 64), (1, 192, 5, 1, 9), (3, 256, 16, 2, 17), (8, 256, 16, 16, 40)])
 def test_commit(Hkv, d, page, L, n):
     """Accepted rows move in all layers, in the order that lets a written row have been a source; lengths advance; nothing else changes."""
     ctxs = [0, 5, 100, 33, 60, 7]
