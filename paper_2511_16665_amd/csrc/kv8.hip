@@ -46,7 +46,8 @@ __device__ __forceinline__ int64_t row_of(const KV8Layer& kv, int b, int slot) {
 // ---- write
 // One workgroup per row (b, i).  A head (of q, k or v) belongs to a group of `lanes` lanes (a power of two); a lane holds VEC pairs (j, j + d/2) of it, one
 // 16-byte piece of either half.  The largest magnitude of a k or v head is taken over its group.  Angles are formed in double (positions reach
-// 32K, where an fp32 product position * frequency is 1e-3 rad off), once per row, and shared by the heads.
+// 32K, where an fp32 product position * frequency is 1e-3 rad off), once per row, and shared by the heads.  Bound by memory: 1536 rows of 28 and 4 heads of 128,
+// 27 MB, 9.8 us (0.7 of them the angles; the row's loads in front of the angles change nothing); one row 3.4 us, a launch and three dependent loads.
 template <typename T>
 __global__ __launch_bounds__(512) void kv8_write_k(const T* __restrict__ qkv, const T* __restrict__ bias, T* __restrict__ q_out, int64_t q_stride,
                                                    const int32_t* __restrict__ depth, int n, int n_q_heads, int lanes, double log2_theta, KV8Layer kv) {
@@ -141,7 +142,8 @@ hipError_t kv8_write(hipStream_t s, int dtype, int B, int n, const KV8Layer& kv,
 }
 
 // ---- read
-// One wave per (layer, sequence, 16 rows, kv head): a row's d / 16 pieces of 16 codes go to d / 16 lanes.
+// One wave per (layer, sequence, 16 rows, kv head): a row's d / 16 pieces of 16 codes go to d / 16 lanes.  Bound by memory, mostly what it writes: 4 layers of 7 sequences
+// of 4001 rows, 345 MB, 74 us (4.6 TB/s; a large copy reaches 5.0).
 template <typename T>
 __global__ __launch_bounds__(256) void kv8_read_k(int n_layers, int B, int n, const int32_t* __restrict__ first, const int32_t* __restrict__ count,
                                                   T* __restrict__ out_k, T* __restrict__ out_v, KV8Layer kv) {
@@ -211,13 +213,13 @@ __global__ __launch_bounds__(1024) void kv8_commit_k(int n_layers, KV8Layer kv, 
                                                      const int32_t* __restrict__ path_idx, int stride) {
     __shared__ int64_t s_src[64], s_dst[64];
     const int b = blockIdx.y, tid = threadIdx.x;
+    // (the path does not wait for the length of what was accepted: on cold memory each step of this chain costs 1 to 2 us)
+    const int ctx = seq_len[b], p = tid < min(stride, 64) ? path_idx[(int64_t)b * stride + tid] : 0;
     const int a = accepted(accept_len, b, stride);
     if (!ONE && a == 0) return;
     if (tid < 64) {
         int64_t src = -1, dst = -1;
-        const int ctx = seq_len[b];
         if (tid >= 1 && tid <= a) {
-            const int p = path_idx[(int64_t)b * stride + tid];
             if (p > tid && p < 64 && ctx >= 0 && ctx < 0x7fffffff - 64) src = row_of(kv, b, ctx + p), dst = row_of(kv, b, ctx + tid);
         }
         s_src[tid] = dst < 0 ? -1 : src, s_dst[tid] = dst;
@@ -262,8 +264,8 @@ __global__ void kv8_advance_k(int B, int32_t* __restrict__ seq_len, const int32_
 
 hipError_t kv8_commit(hipStream_t s, int n_layers, int B, const KV8Layer& kv, int32_t* seq_len, const int32_t* accept_len, const int32_t* path_idx, int stride) {
     const int64_t units = (int64_t)n_layers * kv.n_kv * (2 * (kv.d / 16) + 2);
-    // One launch / two, us in a captured graph behind a fill kernel, 32 sequences, 4 heads of 128: 1 layer (136 columns) 7.1 / 8.7, 4 layers 7.4 / 8.9, 28 layers (3808) 10.7 / 9.4, but
-    // outside a graph the launch costs its caller 3.6 us; 64 layers and 8 heads (17408) 36.6 / 13.0.
+    // One launch / two, us in a captured graph behind a fill kernel, 32 sequences, 4 heads of 128: 1 layer (72 columns) 7.1 / 8.7, 4 layers 7.4 / 8.9, 28 layers (2016) 10.7 / 9.4, but
+    // outside a graph the launch costs its caller 3.6 us; 64 layers and 8 heads (9216) 36.6 / 13.0.
     if (units <= 4096) {
         const int threads = (int)std::min<int64_t>(1024, (units + 63) / 64 * 64);
         hipLaunchKernelGGL(kv8_commit_k<true>, dim3(1, B), dim3(threads), 0, s, n_layers, kv, seq_len, accept_len, path_idx, stride);
@@ -278,7 +280,8 @@ hipError_t kv8_commit(hipStream_t s, int n_layers, int B, const KV8Layer& kv, in
 
 // ---- attention, a workgroup per (row, query head): any dtype and shape
 // Four waves, each taking every fourth tile of 64 keys: lanes own keys for the scores and 16-code pieces of value rows for the sums; the running maximum
-// and sum of a wave's tiles, the waves merged at the end.
+// and sum of a wave's tiles, the waves merged at the end.  A simple kernel for small decoders and tests, bound by latency (two sequences of 128 keys with 5 nodes, 7 us);
+// it reads the keys of a kv head once per row and query head.
 constexpr int kRowWaves = 4;
 template <typename T>
 __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, KV8Layer kv, const T* __restrict__ q, int64_t q_stride, T* __restrict__ out,
@@ -690,7 +693,9 @@ struct KV8Out {
 
 // Few rows (NT tiles of 16): bound by memory.  A wave of the workgroup's four owns every fourth tile of the item's range with all rows, takes codes from
 // memory straight into the registers that the products want (no LDS, no barrier until the end) and keeps the next tile's in flight: keys once the
-// scores are done, values once the sums are.  The waves are joined through LDS.
+// scores are done, values once the sums are.  The waves are joined through LDS.  64 sequences of ~8192 keys, 40 and 8 heads, one token: 1.08 GB in 177 us (6.1
+// TB/s); 16 of 8192, 28 and 4 heads: 135 MB in 28 us (4.8 TB/s, most of a fixed 5 us being planning and the first tile's way from memory); one: 6.9 us.
+// Two waves per SIMD: three have no registers for the next tile (the same 64 sequences 205 us).
 template <int NT>
 __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
                                                                       KV8Seg* __restrict__ seg, float scale_log2, float lazy) {
@@ -822,7 +827,8 @@ __device__ __forceinline__ void dma_4(const uint8_t* base, uint32_t offset, uint
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t offset) { return (__attribute__((address_space(3))) T*)(uintptr_t)offset; }
 
-// More rows: bound by the matrix pipe and, side by side with it, the exponentials.  One workgroup of eight waves, two per SIMD, streams the item's range once for up to 24
+// More rows: bound by the matrix pipe and, side by side with it, the exponentials (32 sequences of ~4096 keys, 28 and 4 heads, 48 nodes, 91 GFLOP: 119 us, 63 % of
+// the rate of a large product; the matrix pipes are busy 43 % of it).  One workgroup of eight waves, two per SIMD, streams the item's range once for up to 24
 // tiles of rows, dealt round-robin to the waves (NT each).  A tile of 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead,
 // a wave's eight keys (1 KB each of K and V) to a place that only this wave reads; the wave converts them to bf16 and stores them for all, K rows swizzled by
 // the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by twice the key (a transposing read takes two neighbouring places of each of 8
@@ -1073,7 +1079,8 @@ __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int64_t q_st
 // through LDS twice: its codes come from memory by direct loads, two tiles ahead, a wave's page (2 KB each of K and V) to a place that only this wave reads;
 // the wave converts them to bf16 and stores them for all, K rows swizzled by the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by
 // twice the key (a transposing read takes two neighbouring places of each of 8 keys).  There is one stage of either: V of a tile is converted
-// under Q K^T, K of the next one under P V.
+// under Q K^T, K of the next one under P V.  16 sequences of 8192 keys, 28 and 4 heads, 16 nodes (7 tiles of rows, 30 GFLOP): 56 us; the matrix pipes are busy 29 % of
+// it, the chain of barrier, reads, products and exponentials is what takes the time (two workgroups per CU hide one another's only in part).
 constexpr int kMidRaw = 2, kMidLds = 2 * kStage + kMidRaw * kRawBytes + 64 * 8;
 
 template <int NT>
@@ -1289,7 +1296,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_mid_k(KV8Split sp, int64_t q_
 }
 
 // The ranges of a sequence joined: WPR waves per row, 16 ranges of each requested together, added up in a fixed order; the lanes read a range's maximum and
-// sum each.
+// sum each.  Bound by latency with few rows, by the partial results with many (32 sequences with 336 rows per kv head: 40 MB in 13 us).
 template <int WPR>
 __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg, const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                   uint16_t* __restrict__ out, int n, int n_q_heads, int n_kv, int r_pad, int slot_step, float scale_log2) {
@@ -1429,6 +1436,8 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         // the most ranges that a sequence can have
         const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, shortest = shortest_range(tiles, p.sp.whole);
         const int ranges = std::max(std::min(p.sp.slots, (tiles + shortest - 1) / shortest), (tiles + p.sp.t_max - 1) / p.sp.t_max);
+        // Four waves per row / one, 28 and 4 heads: one sequence, one token, of 8192 10.1 / 14.0 us with the kernel in front, of 30000 15.4 / 22.8; 4 of 8192, 8 nodes,
+        // 22.8 / 24.0; 64 nodes 56.2 / 54.4
         if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_k<4>, R);
         else join(kv8_join_k<1>, (R + 3) / 4);
         return hipGetLastError();
