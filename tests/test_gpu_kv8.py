@@ -433,7 +433,67 @@ def test_commit(Hkv, d, page, L, n):
     np.testing.assert_array_equal(c.kv.seq_len.cpu().numpy(), np.array(ctxs) + np.clip(acc, 0, stride - 1) + 1)
 
 
+def test_commit_takes_a_row_twice():
+    c = m.Cache([40, 3], 12, 2, 128, 16, layers=2, seed=3)
+    path = np.array([[0, 5, 5, 9, 9], [0, 2, 2, 4, 4]], np.int32)      # (sequence 1: row 2 is a place before it is a source again)
+    want = {x: (c.codes[x].copy(), c.exps[x].copy()) for x in ("k", "v")}
+    for b, ctx in enumerate((40, 3)):
+        for j in range(1, 5):
+            if path[b, j] > j:
+                s, t = ctx + path[b, j], ctx + j
+                for x in ("k", "v"):
+                    for arr in want[x]:
+                        arr[:, c.table[b, t // 16], :, t % 16] = arr[:, c.table[b, s // 16], :, s % 16]
+    print("commit, a row twice", flush=True)
+    tlt.kv8_commit(c.kv, cuda(np.array([4, 4], np.int32)), cuda(path))
+    download(c)
+    for x in ("k", "v"):
+        np.testing.assert_array_equal(c.codes[x], want[x][0])
+        np.testing.assert_array_equal(c.exps[x], want[x][1])
+    assert c.kv.seq_len.tolist() == [45, 8]
+
+
 # ---- together
+
+@pytest.mark.parametrize("n", [1, 8, 20])
+def test_padded_batch(n):
+    """A place in the batch without a sequence: length 0, no pages, masks of zero.  Nothing is written for it, its outputs are zeros."""
+    Hq, Hkv, d = 28, 4, 128
+    c = m.Cache([90, 0, 200], n, Hkv, d, 16, seed=2)
+    alone = m.Cache([90, 0, 200], n, Hkv, d, 16, seed=2)
+    qkv = torch.randn((3, n, (Hq + 2 * Hkv) * d), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    mask = np.repeat(((np.uint64(2) << np.arange(n, dtype=np.uint64)) - np.uint64(1))[None], 3, 0)
+    mask[1] = 0
+    print("padded batch", n, flush=True)
+    keep = {k: getattr(c.kv, k).clone() for k in ("k_pool", "v_pool", "k_exp", "v_exp")}
+    own = [int(p) for p in c.table[1] if p >= 0]
+    c.table[1] = -1
+    c.kv.block_table.copy_(cuda(c.table.astype(np.int32)))
+    q = torch.zeros((3, n, Hq * d), dtype=torch.bfloat16, device="cuda")
+    tlt.kv8_write(tlt.TLT_BF16, Hq, 1e6, qkv, None, None, c.kv, 0, q)
+    assert all(torch.equal(getattr(c.kv, k)[:, own], t[:, own]) for k, t in keep.items())
+    tlt.kv8_write(tlt.TLT_BF16, Hq, 1e6, qkv, None, None, alone.kv, 0, q)
+    others = [p for p in range(keep["k_pool"].shape[1]) if p not in own]
+    assert all(torch.equal(getattr(c.kv, k)[:, others], getattr(alone.kv, k)[:, others]) for k in keep)
+    download(c)
+    got = run_attention(c, "bf16", q.float().cpu().numpy().reshape(3, n, Hq, d), mask)
+    assert not got[1].any()
+    check_attention(c, "bf16", q.float().cpu().numpy().reshape(3, n, Hq, d), mask, got)
+
+
+@pytest.mark.parametrize("n", [1, 8, 20])
+@pytest.mark.parametrize("impl", [-1, 0])
+def test_lengths_above_the_bound_stay_inside(n, impl):
+    """A length above the declared bound: that sequence's outputs mean nothing, the other's are right."""
+    Hq, Hkv, d = 28, 4, 128
+    c = m.Cache([500, 200], n, Hkv, d, 16, seed=2)
+    c.kv.seq_len_bound = 200
+    q = np.random.default_rng(1).standard_normal((2, n, Hq, d)).astype(np.float32)
+    ws = tlt.kv8_attention_workspace(2, n, Hq, Hkv, d, 200 + n)
+    for length in (500, 2 ** 31 - 1):
+        print("length above the bound", n, impl, length, flush=True)
+        c.kv.seq_len[0] = length
+        check_attention(c, "bf16", q, None, run_attention(c, "bf16", q, None, impl=impl, ws=ws), rows=[1])
 
 def steps(c, Hq, n, qkv, depth, mask, acc, path, out, ws, q, n_steps=3):
     """A few steps of a layer: write, attend, commit."""
@@ -443,7 +503,7 @@ def steps(c, Hq, n, qkv, depth, mask, acc, path, out, ws, q, n_steps=3):
         tlt.kv8_commit(c.kv, acc, path)
 
 
-@pytest.mark.parametrize("Hq,Hkv,n,ctxs", [(28, 4, 1, [500, 40]), (28, 4, 20, [300, 0, 61])])
+@pytest.mark.parametrize("Hq,Hkv,n,ctxs", [(28, 4, 1, [500, 40]), (28, 4, 8, [600, 7]), (28, 4, 20, [300, 0, 61])])
 def test_steps_in_a_graph_and_on_two_streams(Hq, Hkv, n, ctxs):
     """Three steps, each on what the ones before it left; captured and replayed several times between eager runs, the same bits; two caches on two streams."""
     d, B = 128, len(ctxs)
