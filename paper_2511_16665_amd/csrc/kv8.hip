@@ -671,21 +671,18 @@ struct KV8Out {
             if (c == 0) part_ml[at * 2] = M, part_ml[at * 2 + 1] = L;
         }
     }
-    // `COUNT` sums (8 or 32) of row r from column c on, their weights' sum L and reference M
-    template <int COUNT>
-    __device__ __forceinline__ void put(const KV8Item& it, int kh, int G, int r, int c, const float* o, float M, float L) const {
+    // 8 sums of row r from column c on, their weights' sum L and reference M
+    __device__ __forceinline__ void put8(const KV8Item& it, int kh, int G, int r, int c, const float* o, float M, float L) const {
         if (it.k == 1) {
             const float inv = L == 0.f ? 0.f : 1.0f / L;
             const int i = r / G, g = r - i * G;
             uint16_t* p = out + ((int64_t)(it.b * n + i) * n_q_heads + kh * G + g) * kD + c;
-#pragma unroll
-            for (int e = 0; e < COUNT; e += 8)
-                *(u32x4_t*)(p + e) = u32x4_t{pack_bf16x2(o[e] * inv, o[e + 1] * inv), pack_bf16x2(o[e + 2] * inv, o[e + 3] * inv),
-                                             pack_bf16x2(o[e + 4] * inv, o[e + 5] * inv), pack_bf16x2(o[e + 6] * inv, o[e + 7] * inv)};
+            *(u32x4_t*)p = u32x4_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
+                                   pack_bf16x2(o[6] * inv, o[7] * inv)};
         } else {
             const int64_t at = ((int64_t)it.slot * n_kv + kh) * r_pad + r;
 #pragma unroll
-            for (int e = 0; e < COUNT; e += 4) *(f32x4_t*)(part_o + at * kD + c + e) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            for (int e = 0; e < 8; e += 4) *(f32x4_t*)(part_o + at * kD + c + e) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
             if (c == 0) part_ml[at * 2] = M, part_ml[at * 2 + 1] = L;
         }
     }
@@ -812,7 +809,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_
         for (int y = 0; y < 4; ++y)
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(w[y], o_s[y][rl][c + e], o[e]);
-        to.put<8>(it, kh, G, 16 * t + rl, c, o, M, L);
+        to.put8(it, kh, G, 16 * t + rl, c, o, M, L);
     }
 }
 
@@ -1295,19 +1292,18 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_mid_k(KV8Split sp, int64_t q_
     else kv8_mid_body<0>(it, kh, q_stride, q, rows, kv, to, scale_log2, lazy, lds);
 }
 
-// The ranges of a sequence joined: WPR waves per row, 16 ranges of each requested together, added up in a fixed order; the lanes read a range's maximum and
-// sum each.  Bound by latency with few rows, by the partial results with many (32 sequences with 336 rows per kv head: 40 MB in 13 us).
-template <int WPR>
-__global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg, const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                  uint16_t* __restrict__ out, int n, int n_q_heads, int n_kv, int r_pad, int slot_step, float scale_log2) {
-    constexpr int U = 16;
-    __shared__ float2 s_a[WPR > 1 ? WPR - 1 : 1][64];
-    __shared__ float s_l[WPR];
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), part = wave % WPR, lane = threadIdx.x & 63;
-    const int r = blockIdx.x * (4 / WPR) + wave / WPR, kh = blockIdx.y, b = blockIdx.z;
+// The ranges of a sequence joined, in a fixed order.  Few rows: four waves per row, 16 ranges of each requested together; the lanes read a range's maximum and sum
+// each.  Bound by latency.
+__global__ __launch_bounds__(256) void kv8_join_few_k(const KV8Seg* __restrict__ seg, const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                      uint16_t* __restrict__ out, int n, int n_q_heads, int n_kv, int r_pad, int slot_step, float scale_log2) {
+    constexpr int U = 16, W = 4;
+    __shared__ float2 s_a[W - 1][64];
+    __shared__ float s_l[W];
+    const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int r = blockIdx.x, kh = blockIdx.y, b = blockIdx.z;
     const int G = n_q_heads / n_kv;
     const KV8Seg sg = seg[b];
-    if (r >= n * G || sg.k <= 1) return;   // (one range: its workgroup has written the row; with several waves per row: uniform for the workgroup)
+    if (sg.k <= 1) return;   // (one range: its workgroup has written the row; uniform)
     const int64_t base = ((int64_t)sg.first * n_kv + kh) * r_pad + r, step = (int64_t)slot_step * n_kv * r_pad;
     float2 ml = make_float2(kNegBig, 0.f), v[U];
     auto fetch = [&](int c) {
@@ -1321,14 +1317,12 @@ __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg
     for (int c = lane + 64; c < sg.k; c += 64) M = fmaxf(M, part_ml[(base + c * step) * 2]);
     M = wave_max(M);
     float w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w, a0 = 0.f, a1 = 0.f, L = 0.f;
-    for (int c0 = U * part; c0 < sg.k; c0 += U * WPR) {   // (uniform for the wave)
+    for (int c0 = U * part; c0 < sg.k; c0 += U * W) {   // (a round is 64 ranges; uniform for the wave)
         if (c0 > U * part) {
             fetch(c0);
-            if (c0 - U * part != 0 && ((c0 ^ (c0 - U * WPR)) & ~63) != 0) {   // another 64 ranges
-                const int c = (c0 & ~63) + lane;
-                ml = c < sg.k ? *(const float2*)(part_ml + (base + c * step) * 2) : make_float2(kNegBig, 0.f);
-                w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w;
-            }
+            const int c = (c0 & ~63) + lane;
+            ml = c < sg.k ? *(const float2*)(part_ml + (base + c * step) * 2) : make_float2(kNegBig, 0.f);
+            w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -1338,17 +1332,53 @@ __global__ __launch_bounds__(256) void kv8_join_k(const KV8Seg* __restrict__ seg
             a0 = fmaf(wu, v[u].x, a0), a1 = fmaf(wu, v[u].y, a1);
         }
     }
-    if constexpr (WPR > 1) {
-        if (part > 0) s_a[part - 1][lane] = make_float2(a0, a1);
-        if (lane == 0) s_l[part] = L;
-        __syncthreads();
-        if (part > 0) return;
+    if (part > 0) s_a[part - 1][lane] = make_float2(a0, a1);
+    if (lane == 0) s_l[part] = L;
+    __syncthreads();
+    if (part > 0) return;
 #pragma unroll
-        for (int p = 1; p < WPR; ++p) a0 += s_a[p - 1][lane].x, a1 += s_a[p - 1][lane].y, L += s_l[p];
-    }
+    for (int p = 1; p < W; ++p) a0 += s_a[p - 1][lane].x, a1 += s_a[p - 1][lane].y, L += s_l[p];
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     const int i = r / G, g = r - i * G;
     ((uint32_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD))[lane] = pack_bf16x2(a0 * inv, a1 * inv);
+}
+// Many rows: half a wave per row, four columns a lane.  Bound by the partial results that it reads: 32 sequences with 336 rows per kv head, 40 MB in 9.5 us (a wave
+// per row 12.8).
+__global__ __launch_bounds__(256) void kv8_join_many_k(const KV8Seg* __restrict__ seg, const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                       uint16_t* __restrict__ out, int n, int n_q_heads, int n_kv, int r_pad, int slot_step, float scale_log2) {
+    constexpr int U = 8;
+    const int lane = threadIdx.x & 31, r = blockIdx.x * 8 + (threadIdx.x >> 5), kh = blockIdx.y, b = blockIdx.z, G = n_q_heads / n_kv;
+    const KV8Seg sg = seg[b];
+    if (r >= n * G || sg.k <= 1) return;   // (halves of a wave leave as wholes)
+    const int64_t base = ((int64_t)sg.first * n_kv + kh) * r_pad + r, step = (int64_t)slot_step * n_kv * r_pad;
+    f32x4_t v[U], a = {0.f, 0.f, 0.f, 0.f};
+    float2 ml;
+    float L = 0.f;
+    auto fetch = [&](int c0) {
+        const int c = c0 + (lane & (U - 1));
+        ml = c < sg.k ? *(const float2*)(part_ml + (base + c * step) * 2) : make_float2(kNegBig, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c0 + u < sg.k) v[u] = *(const f32x4_t*)(part_o + (base + (c0 + u) * step) * kD + lane * 4);
+    };
+    fetch(0);
+    float M = ml.x;
+    for (int c = U + lane; c < sg.k; c += 32) M = fmaxf(M, part_ml[(base + c * step) * 2]);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, 32));
+    for (int c0 = 0; c0 < sg.k; c0 += U) {
+        if (c0 > 0) fetch(c0);
+        const float w = exp2f((ml.x - M) * scale_log2), wl = ml.y * w;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + u >= sg.k) break;
+            L += __shfl(wl, u, 32);
+            a += __shfl(w, u, 32) * v[u];
+        }
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const int i = r / G, g = r - i * G;
+    *(u32x2_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD + lane * 4) = u32x2_t{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
 }
 
 struct KV8Plan {
@@ -1438,8 +1468,8 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         const int ranges = std::max(std::min(p.sp.slots, (tiles + shortest - 1) / shortest), (tiles + p.sp.t_max - 1) / p.sp.t_max);
         // Four waves per row / one, 28 and 4 heads: one sequence, one token, of 8192 10.1 / 14.0 us with the kernel in front, of 30000 15.4 / 22.8; 4 of 8192, 8 nodes,
         // 22.8 / 24.0; 64 nodes 56.2 / 54.4
-        if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_k<4>, R);
-        else join(kv8_join_k<1>, (R + 3) / 4);
+        if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_few_k, R);
+        else join(kv8_join_many_k, (R + 7) / 8);
         return hipGetLastError();
     }
     const float scale = 1.0f / sqrtf((float)kv.d);
