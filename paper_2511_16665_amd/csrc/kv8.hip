@@ -1401,7 +1401,7 @@ static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) 
     p.groups = p.few ? 1 : (p.row_tiles + 23) / 24;
     p.per_group = (p.row_tiles + p.groups - 1) / p.groups;
     p.sp.slots = std::max(1, (p.few || p.mid ? 512 : 256) / (n_kv * p.groups));   // (workgroups that the chip holds)
-    p.sp.t_max = 64;
+    p.sp.t_max = 64;   // (as many as a wave has lanes for their pages; 24, 32, 48: 64 sequences of ~8192, 40 and 8 heads, 260, 240, 223 us against 217)
     p.sp.whole = p.few ? 8 : 4;
     // Planning costs every workgroup some 2 us (7 at 256 sequences) and is worth it where sequences are cut to fill the chip or whole rounds of it: long ones while
     // the workgroups' rounds are few, any length while there are fewer sequences than places.  Planned / ranges of t_max: 96 sequences of ~4000, 28 and 4 heads, 8 nodes
@@ -1466,8 +1466,8 @@ hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV
         // the most ranges that a sequence can have
         const int tiles = (kv.seq_len_bound + rows.n + kKT - 1) / kKT, shortest = shortest_range(tiles, p.sp.whole);
         const int ranges = std::max(std::min(p.sp.slots, (tiles + shortest - 1) / shortest), (tiles + p.sp.t_max - 1) / p.sp.t_max);
-        // Four waves per row / one, 28 and 4 heads: one sequence, one token, of 8192 10.1 / 14.0 us with the kernel in front, of 30000 15.4 / 22.8; 4 of 8192, 8 nodes,
-        // 22.8 / 24.0; 64 nodes 56.2 / 54.4
+        // Four waves per row / half a one, 28 and 4 heads, us with the kernel in front: one sequence, one token, of 2048 8.6 / 10.3, of 8192 9.7 / 13.0, of 30000 12.9 / 19.7;
+        // 8 nodes at 30000 22.1 / 29.4; 4 sequences of 8192, 8 nodes, 25.7 / 27.6; 64 nodes 54.1 / 51.0; 64 of 2048, one token (few ranges each), 32.8 / 31.5
         if (ranges > 16 && (int64_t)R * kv.n_kv * rows.B <= 2048) join(kv8_join_few_k, R);
         else join(kv8_join_many_k, (R + 7) / 8);
         return hipGetLastError();
