@@ -111,3 +111,14 @@ def test_attention_past_what_a_launch_holds():
     # 65535 sequences of 8192 ranges each and 64 kv heads
     assert attend(handle(seq_len_bound=(1 << 25) - 4, **long), B=65535, Hq=64, Hkv=64, stride=64 * 128, bytes=1 << 62) == -2
     assert size(65535, 4, 64, 64, 128, 1 << 25) == 0
+
+
+def test_a_workspace_serves_smaller_bounds_and_fewer_rows():
+    size = tlt.load().tlt_kv8_attention_workspace_bytes
+    for B in (1, 3, 33, 70, 96, 129, 192, 256, 257, 600):
+        for Hq, Hkv in ((28, 4), (40, 8), (4, 1), (40, 20)):
+            for n in (1, 2, 5, 8, 20, 64):
+                by_length = [size(B, n, Hq, Hkv, 128, x) for x in (1, 64, 65, 128, 256, 257, 512, 513, 4095, 4096, 4097, 8192, 20000, 40000)]
+                assert by_length == sorted(by_length), (B, n, Hq, Hkv)
+            by_rows = [size(B, n, Hq, Hkv, 128, 5000) for n in range(1, 65)]
+            assert by_rows == sorted(by_rows) and by_rows[0] > 0, (B, Hq, Hkv)
