@@ -2,8 +2,9 @@
 //
 // A row (one token of one kv head, d elements) is d codes in e4m3 (OCP: 4 exponent bits, bias 7, largest value 448, no infinities) and one
 // exponent byte E; its values are code * 2^(E - 127).  E - 127 is the smallest e >= -126 with max|x| <= 448 * 2^e, so scaling by it is exact, the one
-// rounding is that to e4m3, nothing saturates, and a value has four significant bits: it is exact in bf16 too.  A row with an element that is not
-// finite keeps E = 255 and codes of zero, and all of it reads as NaN.
+// rounding is that to e4m3 and a value has four significant bits.  A row with an element that is not finite keeps E = 255 and codes of zero, and all of it
+// reads as NaN.  One code of one exponent has no value in fp32 and bf16: rows from 248 * 2^120 on have E = 247 and the code 256, which would be 2^128;
+// every reader takes the code below it instead (finite4).
 #include <algorithm>
 
 #include "dev_common.h"
@@ -35,6 +36,10 @@ __device__ __forceinline__ void decode4(uint32_t w, float scale, float* out) {
     const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     out[0] = lo[0] * scale, out[1] = lo[1] * scale, out[2] = hi[0] * scale, out[3] = hi[1] * scale;
 }
+// Four codes of a row whose exponent byte is kTopExp, the largest of a finite row, or above it (not finite: zeros stay zeros): 256, four exponent bits of one, becomes 240.
+constexpr uint32_t kTopExp = 247;
+__device__ __forceinline__ uint32_t finite4(uint32_t w) { return w - ((w & w >> 1 & w >> 2 & w >> 3 & 0x08080808u) >> 3); }
+__device__ __forceinline__ u32x4_t finite16(u32x4_t w) { return u32x4_t{finite4(w[0]), finite4(w[1]), finite4(w[2]), finite4(w[3])}; }
 
 // row number of a slot in the pools' rows of kv head 0 (kv head kh: + kh * page_size), -1: the block table does not back it
 __device__ __forceinline__ int64_t row_of(const KV8Layer& kv, int b, int slot) {
@@ -173,6 +178,7 @@ __global__ __launch_bounds__(256) void kv8_read_k(int n_layers, int B, int n, co
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+            if (e[x] >= kTopExp) w[x] = finite16(w[x]);
             T* o = (x == 0 ? out_k : out_v) + to;
             float f[16];
 #pragma unroll
@@ -308,10 +314,14 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
         const int64_t at = at0 < 0 ? -1 : at0 + (int64_t)kh * kv.page_size;
         float s = 0.f;
         if (vis && at >= 0) {
+            const uint32_t ke = kv.k_exp[at];
             for (int c0 = 0; c0 < d; c0 += 64) {
                 u32x4_t w[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = *(const u32x4_t*)(kv.k + at * d + c0 + 16 * c);
+                for (int c = 0; c < 4; ++c) {
+                    w[c] = *(const u32x4_t*)(kv.k + at * d + c0 + 16 * c);
+                    if (ke >= kTopExp) w[c] = finite16(w[c]);
+                }
 #pragma unroll
                 for (int c = 0; c < 16; ++c) {
                     float f[4];
@@ -320,7 +330,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
                     for (int e = 0; e < 4; ++e) s = fmaf(q_s[c0 + 4 * c + e], f[e], s);
                 }
             }
-            s *= scale_of(kv.k_exp[at]);
+            s *= scale_of(ke);
         }
         if (!vis) s = -INFINITY;
         const float m_new = fmaxf(m, wave_max(s));   // (a NaN does not count here; it comes through the weights)
@@ -338,8 +348,10 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
             for (int k = grp; k < 64; k += groups) {
                 const int64_t kat = at_s[wave][k];
                 if (kat < 0) continue;
-                const float w = p_s[wave][k] * scale_of(kv.v_exp[kat]);
-                const u32x4_t v = *(const u32x4_t*)(kv.v + kat * d + piece);
+                const uint32_t ve = kv.v_exp[kat];
+                const float w = p_s[wave][k] * scale_of(ve);
+                u32x4_t v = *(const u32x4_t*)(kv.v + kat * d + piece);
+                if (ve >= kTopExp) v = finite16(v);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     float f[4];
@@ -755,6 +767,20 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_
         const bool edge = t0 + kKT > ctx;
         f32x4_t sc[NT][4];
         u32x4_t pb[NT][2];
+        // (rows near the type's largest value, and those that are not finite; the lanes have the exponents of all 64 keys and values)
+        const uint32_t top_exp = max(max(max(ke[0], ke[1]), max(ke[2], ke[3])), max(max(kve[0], kve[1]), max(kve[2], kve[3])));
+        for (int rep = __builtin_amdgcn_ballot_w64(top_exp >= kTopExp) != 0 ? 0 : 1; rep < 1; ++rep) {   // (a loop, which stays a branch)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kc[s][h] = ke[s] >= kTopExp ? finite16(kc[s][h]) : kc[s][h];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    u32x2_t& c = vc[s >> 1][s & 1][v];
+                    c = (ve[s] >> (8 * v) & 255u) >= kTopExp ? u32x2_t{finite4(c[0]), finite4(c[1])} : c;
+                }
+            }
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             f32x4_t* to_sc[NT];
@@ -896,11 +922,14 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
         const int ln = place(lane), key = 8 * wave + (ln >> 3), p = ln & 7;
         const bool there = __builtin_amdgcn_readlane(pages, t) >= 0;
         const int left = there ? total - k0 - t * kKT : 0;   // (slots that nobody has written may hold anything)
-        for (int rep = left < kKT ? 0 : 1; rep < 1; ++rep) {   // (a loop, which stays a branch)
+        const bool top = __builtin_amdgcn_ballot_w64(max(r.ke, r.ve) >= kTopExp) != 0;
+        for (int rep = left < kKT || top ? 0 : 1; rep < 1; ++rep) {   // (a loop, which stays a branch)
             const bool in = key < left;
 #pragma unroll
             for (int y = 0; y < 4; ++y) r.v[y] = in ? r.v[y] : 0u, r.k[y] = there ? r.k[y] : 0u;
             r.ke = there ? r.ke : 127u, r.ve = there ? r.ve : 127u;
+            r.k = r.ke >= kTopExp ? finite16(r.k) : r.k;
+            r.v = r.ve >= kTopExp ? finite16(r.v) : r.v;
         }
         // (values that are not finite: their codes are zero, the NaN comes through the key, whose score only rows that see it keep)
         const float sk = __uint_as_float((r.ve == 255u ? 255u : r.ke) << 23), sv = __uint_as_float((r.ve == 255u ? 127u : r.ve) << 23);
@@ -1138,6 +1167,9 @@ __device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t 
         for (int rep = there ? 1 : 0; rep < 1; ++rep)   // (a loop, which stays a branch)
 #pragma unroll
             for (int j = 0; j < 2; ++j) r.c[j] = u32x4_t{0u, 0u, 0u, 0u}, r.e[j] = r.ev[j] = 127u;
+        if (__builtin_amdgcn_ballot_w64(max(r.e[0], r.e[1]) >= kTopExp) != 0)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) r.c[j] = r.e[j] >= kTopExp ? finite16(r.c[j]) : r.c[j];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
@@ -1156,6 +1188,9 @@ __device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t 
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) r.c[j][y] = 16 * wave + 8 * j + (ln >> 3) < left ? r.c[j][y] : 0u;
+        if (__builtin_amdgcn_ballot_w64(max(r.ev[0], r.ev[1]) >= kTopExp) != 0)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) r.c[j] = r.ev[j] >= kTopExp ? finite16(r.c[j]) : r.c[j];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
