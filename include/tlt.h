@@ -370,7 +370,8 @@ int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
 
 /* Attention of the rows that tlt_kv8_write has written (n <= TLT_MAX_TREE per sequence): row (b, i) attends to every slot below
  * seq_len[b] and to slot seq_len[b] + j (j < n) where bit j of anc_mask[b][i] is set (anc_mask NULL: j <= i, a chain); a row that
- * sees nothing gives zeros.  Scores are taken to lie within +-1e29.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
+ * sees nothing gives zeros.  Finite scores are taken to lie within +-1e29; a row that sees a score of NaN or +infinity, or of -infinity and
+ * nothing else, is NaN.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
  * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
  * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
  * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).

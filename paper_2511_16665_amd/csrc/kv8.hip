@@ -381,7 +381,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void kv8_attn_row_k(KV8Rows rows, K
         ll += f * l_s[w];
         a += f * o_w;
     }
-    out[((int64_t)r * n_q_heads + hq) * d + tid] = from_float<T>(ll == 0.f ? 0.f : a / ll);
+    const bool sees = ctx > 0 || (mask & (~0ull >> (64 - rows.n))) != 0;   // (a row that sees something and has a sum of zero has scores of -infinity only: 0 / 0)
+    out[((int64_t)r * n_q_heads + hq) * d + tid] = from_float<T>(ll == 0.f && !sees ? 0.f : a / ll);
 }
 
 // ---- attention by matrix instructions: bf16, head_dim 128, pages of 16
@@ -667,14 +668,15 @@ __device__ __forceinline__ void kv8_sums(KV8Tiles<NT>& x, const u32x2_t (&vc)[2]
     for (int t = 0; t < NT; ++t)
         x.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, ones), __builtin_bit_cast(bf16x8_t, *pb[t]), x.l[t], 0, 0, 0);
 }
-// Where a row's result goes: the output, or the partial results of its range
+// Where a row's result goes: the output, or the partial results of its range.  sees: the row sees anything.  Its largest weight is 1 or more, so a sum of zero means
+// that all its scores are -infinity: 0 / 0.  (A sequence of two ranges or more has a context, so that every row does: where ranges are joined, nobody asks.)
 struct KV8Out {
     uint16_t* out;
     float *part_o, *part_ml;
     int n, n_q_heads, n_kv, r_pad;
-    __device__ __forceinline__ void put4(const KV8Item& it, int kh, int G, int r, int c, f32x4_t o, float M, float L) const {
+    __device__ __forceinline__ void put4(const KV8Item& it, int kh, int G, int r, int c, f32x4_t o, float M, float L, bool sees) const {
         if (it.k == 1) {
-            const float inv = L == 0.f ? 0.f : 1.0f / L;
+            const float inv = L == 0.f && !sees ? 0.f : 1.0f / L;
             const int i = r / G, g = r - i * G;
             *(u32x2_t*)(out + ((int64_t)(it.b * n + i) * n_q_heads + kh * G + g) * kD + c) = u32x2_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
         } else {
@@ -684,9 +686,9 @@ struct KV8Out {
         }
     }
     // 8 sums of row r from column c on, their weights' sum L and reference M
-    __device__ __forceinline__ void put8(const KV8Item& it, int kh, int G, int r, int c, const float* o, float M, float L) const {
+    __device__ __forceinline__ void put8(const KV8Item& it, int kh, int G, int r, int c, const float* o, float M, float L, bool sees) const {
         if (it.k == 1) {
-            const float inv = L == 0.f ? 0.f : 1.0f / L;
+            const float inv = L == 0.f && !sees ? 0.f : 1.0f / L;
             const int i = r / G, g = r - i * G;
             uint16_t* p = out + ((int64_t)(it.b * n + i) * n_q_heads + kh * G + g) * kD + c;
             *(u32x4_t*)p = u32x4_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
@@ -835,7 +837,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_
         for (int y = 0; y < 4; ++y)
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(w[y], o_s[y][rl][c + e], o[e]);
-        to.put8(it, kh, G, 16 * t + rl, c, o, M, L);
+        to.put8(it, kh, G, 16 * t + rl, c, o, M, L, ctx > 0 || kv8_mask(rows, b, G, 16 * t + rl) != 0);
     }
 }
 
@@ -1073,8 +1075,9 @@ __device__ __forceinline__ void kv8_many_body(const KV8Item& it, int kh, int rg,
     for (int t = 0; t < NT; ++t) {
         const int row = (rg * per_group + wave + 8 * t) * 16 + l16;
         if (row >= R) continue;
+        const bool sees = ctx > 0 || mask_lds[row / G] != 0;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0]);
+        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0], sees);
     }
 }
 
@@ -1307,8 +1310,9 @@ __device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t 
     for (int t = 0; t < NT; ++t) {
         const int row = (wave + 4 * t) * 16 + l16;
         if (row >= R) continue;
+        const bool sees = ctx > 0 || mask_lds[row / G] != 0;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0]);
+        for (int dt = 0; dt < 8; ++dt) to.put4(it, kh, G, row, 16 * dt + 4 * g4, x.acc[t][dt], x.m[t], x.l[t][0], sees);
     }
 }
 
@@ -1373,7 +1377,7 @@ __global__ __launch_bounds__(256) void kv8_join_few_k(const KV8Seg* __restrict__
     if (part > 0) return;
 #pragma unroll
     for (int p = 1; p < W; ++p) a0 += s_a[p - 1][lane].x, a1 += s_a[p - 1][lane].y, L += s_l[p];
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float inv = 1.0f / L;
     const int i = r / G, g = r - i * G;
     ((uint32_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD))[lane] = pack_bf16x2(a0 * inv, a1 * inv);
 }
@@ -1411,7 +1415,7 @@ __global__ __launch_bounds__(256) void kv8_join_many_k(const KV8Seg* __restrict_
             a += __shfl(w, u, 32) * v[u];
         }
     }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float inv = 1.0f / L;
     const int i = r / G, g = r - i * G;
     *(u32x2_t*)(out + ((int64_t)(b * n + i) * n_q_heads + kh * G + g) * kD + lane * 4) = u32x2_t{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
 }

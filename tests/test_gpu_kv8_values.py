@@ -82,3 +82,30 @@ def test_the_largest_rows_reach_only_the_rows_that_see_them(dtype, Hq, Hkv, d, n
     c.exps["k"][0, :, :, ::3], c.codes["k"][0, :, :, ::3] = 247, m.encode(top[0][None])[0][0]
     c.upload()
     check_attention(c, dtype, q * 0, own, run_attention(c, dtype, q * 0, own, impl=impl))
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,n,impl", [("bf16", 28, 4, 128, 1, -1), ("bf16", 28, 4, 128, 4, -1), ("bf16", 28, 4, 128, 16, -1), ("bf16", 28, 4, 128, 24, -1),
+                                                   ("bf16", 28, 4, 128, 48, -1), ("bf16", 28, 4, 128, 4, 0), ("fp32", 4, 2, 64, 6, -1)])
+def test_scores_of_minus_infinity_alone_are_not_nothing(dtype, Hq, Hkv, d, n, impl):
+    """A row whose visible scores are all -infinity has no softmax: NaN, as the definition gives, in one range or several, in the context or among the new rows.
+    A row that sees nothing is zeros whatever its query; the others are right (they need not keep their bits: scores move the references of a tile's 16 rows)."""
+    ctxs = [90, 0, 3000]
+    c = m.Cache(ctxs, n, Hkv, d, 16, seed=9)
+    c.codes["k"][..., 0] = 0x38                          # 1.0: times -infinity, and the other products finite
+    c.upload()
+    q = np.random.default_rng(n).standard_normal((3, n, Hq, d)).astype(np.float32)
+    mask = np.tile(np.uint64(1) << np.arange(n, dtype=np.uint64), (3, 1))
+    mask[1, n // 2:] = 0
+    print("scores of -infinity", dtype, Hq, Hkv, n, impl, flush=True)
+    q64 = torch.from_numpy(q).to(DTYPE[dtype][1]).double().numpy()
+    q[:, :, 1, 0], q[:, n - 1, Hq - 1, 0] = -np.inf, -np.inf
+    got = run_attention(c, dtype, q, mask, impl=impl).cpu()
+    bad = torch.zeros((3, n, Hq), dtype=torch.bool)
+    bad[:, :, 1], bad[:, n - 1, Hq - 1] = True, True
+    blind = torch.from_numpy((mask == 0) & (np.array(ctxs) == 0)[:, None])[..., None].expand(-1, -1, Hq)
+    assert not got[blind].any() and blind.any()
+    assert torch.isnan(got[bad & ~blind]).all()
+    for b in range(3):
+        want, tol = m.attention(c, b, q64[b], mask[b], rounded=dtype == "bf16")
+        ok = ~bad[b].numpy()
+        assert (np.abs(got[b].double().numpy() - want)[ok] <= tol[ok]).all(), b
