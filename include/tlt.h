@@ -347,7 +347,8 @@ int tlt_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
  * tlt_kv8_attention take ONE layer's pools (advance the four pointers), tlt_kv8_commit and tlt_kv8_read those of n_layers.
  * All of them: head_dim 64, 128, 192 or 256, any page size, any number of query heads per kv head; slots that the block table does not
  * back are not written, and count as keys and values of zero.  dtype (TLT_F32 / TLT_BF16) is that of the activations.
- * Sums, softmax and rotations are fp32, angles double.  No memory is kept between calls; calls may be captured into
+ * Rotations, scores, softmax statistics and sums are fp32, angles double; the matrix kernels round every softmax weight to bf16 (by 2^-8 of it at most) for its
+ * product with the values and divide by the sum of the rounded weights, impl 0 keeps weights in fp32.  No memory is kept between calls; calls may be captured into
  * graphs.  Errors: TLT_EINVAL, TLT_ESHAPE (a workspace that is too small, or more work than a launch holds), TLT_ENOPAGES,
  * TLT_EHIP. */
 typedef struct tlt_kv8 {
@@ -371,7 +372,7 @@ int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
 /* Attention of the rows that tlt_kv8_write has written (n <= TLT_MAX_TREE per sequence): row (b, i) attends to every slot below
  * seq_len[b] and to slot seq_len[b] + j (j < n) where bit j of anc_mask[b][i] is set (anc_mask NULL: j <= i, a chain); a row that
  * sees nothing gives zeros.  Finite scores are taken to lie within +-1e29; a row that sees a score of NaN or +infinity, or of -infinity and
- * nothing else, is NaN.  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
+ * nothing else, is NaN.  Values that a row sees are taken to lie within +-1e28 (weighted sums are formed before they are divided).  q: rotated queries as tlt_kv8_write leaves them; out [B][n][Hq*d] (DEVICE, dtype).
  * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
  * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
  * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).

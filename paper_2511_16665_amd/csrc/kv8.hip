@@ -629,7 +629,10 @@ __device__ __forceinline__ void kv8_weights(KV8Tiles<NT>& x, f32x4_t (&sc)[NT][4
             float e[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(fmaf(sc[t][s][v], scale_log2, -mc));
-            pb[t][s >> 1][2 * (s & 1)] = pack_bf16x2(e[0], e[1]);       // weights are rounded to bf16 for the second product; their sum is that of the rounded ones
+            // Weights are rounded to bf16, what the second product takes beside values in bf16: each by 2^-8 of itself at most, which moves the mean by 2^-8 (mean |v| + |o|) at
+            // most, as much as the rounding of the output to bf16 for values of one size; their sum is that of the rounded ones, so that a common factor cancels.  (Two
+            // products, of a weight's upper and lower half, would double the second product, half of the matrix work.)
+            pb[t][s >> 1][2 * (s & 1)] = pack_bf16x2(e[0], e[1]);
             pb[t][s >> 1][2 * (s & 1) + 1] = pack_bf16x2(e[2], e[3]);
         }
     }
