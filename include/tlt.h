@@ -337,7 +337,8 @@ int tlt_attention(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
  * how many sequences fit, is the cache.  A row (one token of one kv head, d elements) is d codes in e4m3 (the OCP
  * format: bias 7, largest value 448) and one exponent byte E, its values being code * 2^(E - 127).  E - 127 is the
  * smallest e >= -126 with max|x| <= 448 * 2^e; codes are rounded to nearest, ties to even.  Scaling is exact and a value has
- * four significant bits, so reading a row into bf16 or fp32 is exact.  (256 * 2^120, the code of values from 248 * 2^120 on, is past
+ * four significant bits, so reading a row into fp32 is exact, and into bf16 down to 2^-130 (smaller values are rounded to the nearest
+ * multiple of 2^-133, bf16's smallest number).  (256 * 2^120, the code of values from 248 * 2^120 on, is past
  * both types' range: every call reads it as the code below, 240 * 2^120, so that what is finite stays finite.)  A row with an element that is not finite has E =
  * 255 and codes of zero: all of it reads as NaN (and poisons exactly the attention rows that see it).  Codes 0x7f and 0xff
  * and E = 0 are never written and must not be put there.

@@ -2,7 +2,7 @@
 //
 // A row (one token of one kv head, d elements) is d codes in e4m3 (OCP: 4 exponent bits, bias 7, largest value 448, no infinities) and one
 // exponent byte E; its values are code * 2^(E - 127).  E - 127 is the smallest e >= -126 with max|x| <= 448 * 2^e, so scaling by it is exact, the one
-// rounding is that to e4m3 and a value has four significant bits.  A row with an element that is not finite keeps E = 255 and codes of zero, and all of it
+// rounding is that to e4m3 and a value has four significant bits (bf16 holds them all from 2^-130 up).  A row with an element that is not finite keeps E = 255 and codes of zero, and all of it
 // reads as NaN.  One code of one exponent has no value in fp32 and bf16: rows from 248 * 2^120 on have E = 247 and the code 256, which would be 2^128;
 // every reader takes the code below it instead (finite4).
 #include <algorithm>

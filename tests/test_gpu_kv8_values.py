@@ -109,3 +109,24 @@ def test_scores_of_minus_infinity_alone_are_not_nothing(dtype, Hq, Hkv, d, n, im
         want, tol = m.attention(c, b, q64[b], mask[b], rounded=dtype == "bf16")
         ok = ~bad[b].numpy()
         assert (np.abs(got[b].double().numpy() - want)[ok] <= tol[ok]).all(), b
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_smallest_values(dtype):
+    """Exponents 1 to 9: exact in fp32, whose smallest number is 2^-149; in bf16 rounded to its smallest number, 2^-133, below 2^-125."""
+    c = m.Cache([140], 1, 2, 128, 16, seed=4)
+    rng = np.random.default_rng(0)
+    for x in ("k", "v"):
+        c.exps[x][:] = rng.integers(1, 10, c.exps[x].shape)
+        c.codes[x][..., :32] = np.concatenate([np.arange(16), 128 + np.arange(16)])
+    c.upload()
+    code, dt, _ = DTYPE[dtype]
+    out = [torch.full((1, 1, 140, 2, 128), 5.0, dtype=dt, device="cuda") for _ in range(2)]
+    print("the smallest values", dtype, flush=True)
+    tlt.kv8_read(code, c.kv, cuda(np.zeros(1, np.int32)), None, *out)
+    for x, o in zip(("k", "v"), out):
+        want = c.rows(x, 0, 0, 0, 140)
+        if dtype == "bf16":
+            want = np.where(np.abs(want) < 2.0 ** -125, np.rint(want * 2.0 ** 133) * 2.0 ** -133, want)
+            assert (want != c.rows(x, 0, 0, 0, 140)).any()
+        np.testing.assert_array_equal(o[0, 0].double().cpu().numpy(), want)
