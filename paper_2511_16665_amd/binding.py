@@ -500,34 +500,41 @@ def attention(dtype_code, n_q_heads, page_size, qkv, anc_mask, kv: KV, out, ws, 
 
 class KV8:
     """8-bit paged KV cache of one model (tlt_kv8): codes [L, n_pages, Hkv, page, d] and exponent bytes [L, n_pages, Hkv, page] of keys and
-    values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV.  A field is checked when it is set, the
-    tensors' addresses are taken at every call."""
+    values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV.  Fields may be set one by one where their shapes
+    stay, and together by replace(); they are checked against each other first, and one that does not fit leaves the cache as it was.  The tensors'
+    addresses are taken at every call."""
     _TENSORS = ("k_pool", "v_pool", "k_exp", "v_exp", "block_table", "seq_len")
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, block_table: torch.Tensor,
                  seq_len: torch.Tensor, seq_len_bound: int):
-        given = locals()
-        for name in self._TENSORS:
-            object.__setattr__(self, name, given[name])
-        self._check()
-        self.seq_len_bound = int(seq_len_bound)
+        self.replace(k_pool=k_pool, v_pool=v_pool, k_exp=k_exp, v_exp=v_exp, block_table=block_table, seq_len=seq_len, seq_len_bound=seq_len_bound)
 
     def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
         if name in self._TENSORS:
-            self._check()
+            self.replace(**{name: value})
+        else:
+            object.__setattr__(self, name, value)
 
-    def _check(self):
-        k = self.k_pool
-        assert k.dim() == 5 and self.v_pool.shape == k.shape and self.k_exp.shape == self.v_exp.shape == k.shape[:4], "pools' shapes"
-        assert all(t.element_size() == 1 for t in (k, self.v_pool, self.k_exp, self.v_exp)), "pools hold bytes"
-        assert self.block_table.dtype == self.seq_len.dtype == torch.int32 and self.block_table.dim() == 2
-        assert self.seq_len.shape == self.block_table.shape[:1]
-        tensors = [getattr(self, name) for name in self._TENSORS]
-        assert all(t.is_cuda and t.is_contiguous() and t.device == k.device for t in tensors), "device tensors must be contiguous CUDA/HIP tensors"
+    def replace(self, **fields):
+        """Sets several fields together: a batch of another size (block_table, seq_len, seq_len_bound), pools of more pages (all four)."""
+        unknown = set(fields) - {*self._TENSORS, "seq_len_bound"}
+        if unknown:
+            raise TypeError(f"KV8 has no field {sorted(unknown)}")
+        new = {**self.__dict__, **fields}
+        new["seq_len_bound"] = int(new["seq_len_bound"])
+        self._check(**{name: new[name] for name in self._TENSORS})
         # (layers, pages, kv heads, page size, head_dim), sequences, entries of the table per sequence
-        object.__setattr__(self, "dims", tuple(k.shape))
-        object.__setattr__(self, "table_dims", tuple(self.block_table.shape))
+        new["dims"], new["table_dims"] = tuple(new["k_pool"].shape), tuple(new["block_table"].shape)
+        self.__dict__.update(new)
+
+    @staticmethod
+    def _check(k_pool, v_pool, k_exp, v_exp, block_table, seq_len):
+        assert k_pool.dim() == 5 and v_pool.shape == k_pool.shape and k_exp.shape == v_exp.shape == k_pool.shape[:4], "pools' shapes"
+        assert all(t.element_size() == 1 for t in (k_pool, v_pool, k_exp, v_exp)), "pools hold bytes"
+        assert block_table.dtype == seq_len.dtype == torch.int32 and block_table.dim() == 2
+        assert seq_len.shape == block_table.shape[:1]
+        assert all(t.is_cuda and t.is_contiguous() and t.device == k_pool.device for t in (k_pool, v_pool, k_exp, v_exp, block_table, seq_len)), \
+            "device tensors must be contiguous CUDA/HIP tensors"
 
     @staticmethod
     def empty(n_layers, n_pages, n_kv_heads, page_size, head_dim, block_table, seq_len, seq_len_bound) -> "KV8":
