@@ -270,9 +270,15 @@ __global__ void kv8_advance_k(int B, int32_t* __restrict__ seq_len, const int32_
 
 hipError_t kv8_commit(hipStream_t s, int n_layers, int B, const KV8Layer& kv, int32_t* seq_len, const int32_t* accept_len, const int32_t* path_idx, int stride) {
     const int64_t units = (int64_t)n_layers * kv.n_kv * (2 * (kv.d / 16) + 2);
-    // One launch / two, us in a captured graph behind a fill kernel, 32 sequences, 4 heads of 128: 1 layer (72 columns) 7.1 / 8.7, 4 layers 7.4 / 8.9, 28 layers (2016) 10.7 / 9.4, but
-    // outside a graph the launch costs its caller 3.6 us; 64 layers and 8 heads (9216) 36.6 / 13.0.
-    if (units <= 4096) {
+    // One launch while a thread has two columns at most: a second launch costs its caller 2.8 us (3 with cold caches on the GPU, 2 with warm ones), a third turn more. One / two, us,
+    // 8 and 32 sequences, 4 accepted, heads of 128: captured behind a fill kernel, eager behind one (the caller's time), alone on cold caches.
+    //   864 columns (12 layers of 4 heads)   8.6 / 9.6, 8.9 / 9.7       11.3 / 14.1, 11.2 / 14.1   13.8 / 14.6, 14.0 / 14.7
+    //   1152                                 10.2 / 9.7, 10.3 / 9.8     11.3 / 14.1, 11.3 / 14.0   17.6 / 14.7, 18.0 / 15.9
+    //   2016 (28 of 4)                       11.1 / 9.7, 11.8 / 10.0    11.2 / 14.0, 11.2 / 13.9   18.4 / 14.9, 19.5 / 16.0
+    //   2304                                 12.8 / 9.8, 13.4 / 10.2    11.6 / 14.0, 11.7 / 14.0   21.9 / 15.1, 23.7 / 15.9
+    //   4032 (28 of 8)                       15.9 / 9.9, 17.1 / 10.7    14.2 / 13.7, 14.8 / 14.0   27.6 / 15.1, 29.5 / 17.5
+    // (Between 1024 and 2048 columns the caller's gain stands against the GPU's loss: one launch for callers that enqueue step by step, who pay for it in every step.)
+    if (units <= 2048) {
         const int threads = (int)std::min<int64_t>(1024, (units + 63) / 64 * 64);
         hipLaunchKernelGGL(kv8_commit_k<true>, dim3(1, B), dim3(threads), 0, s, n_layers, kv, seq_len, accept_len, path_idx, stride);
         return hipGetLastError();

@@ -6,6 +6,7 @@ import torch
 import kv8_model as m
 from paper_2511_16665_amd import binding as tlt
 from test_gpu_kv8 import check_attention, cuda
+from test_gpu_kv8 import test_commit as commit_case
 
 pytestmark = pytest.mark.gpu
 GUARD = 4096
@@ -53,3 +54,10 @@ def test_write_and_read_stay_inside():
     tlt.kv8_read(tlt.TLT_F32, c.kv, cuda(np.array([33, 5], np.int32)), cuda(np.array([n, 0], np.int32)), *(r[GUARD:-GUARD].view(L, 2, n, Hkv, d) for r in rows))
     for r in rows:
         assert (r[:GUARD] == 7.0).all() and (r[-GUARD:] == 7.0).all() and (r[GUARD:-GUARD].view(L, 2, n, Hkv, d)[:, 1] == 7.0).all()
+
+
+@pytest.mark.parametrize("Hkv,d,page,L,n", [(4, 128, 16, 20, 24), (4, 128, 16, 28, 12), (8, 64, 16, 26, 9), (4, 128, 16, 29, 64), (8, 128, 16, 28, 12), (5, 192, 5, 32, 20)])
+def test_commit_on_both_sides_of_the_rule(Hkv, d, page, L, n):
+    """1440, 2016, 2080, 2088, 4032 and 4160 columns: two turns of a thread in one launch, and two launches."""
+    print(L * Hkv * (d // 8 + 2), "columns", flush=True)
+    commit_case(Hkv, d, page, L, n)
