@@ -1452,11 +1452,11 @@ static KV8Plan plan_kv8(int B, int n, int n_q_heads, int n_kv, int bound_total) 
     p.sp.t_max = 64;   // (as many as a wave has lanes for their pages; 24, 32, 48: 64 sequences of ~8192, 40 and 8 heads, 260, 240, 223 us against 217)
     p.sp.whole = p.few ? 8 : 4;
     // Planning costs every workgroup some 2 us (7 at 256 sequences) and is worth it where sequences are cut to fill the chip or whole rounds of it: long ones while the
-    // rounds are few; short ones while there are fewer sequences than places, or a second round would stand half empty.  Planned / ranges of t_max, 28 and 4 heads: sequences of
-    // ~4000: 96 with 8 nodes (128 places) 139 / 180 us, 192 274 / 302, 128 with 24 nodes (64 places) 344 / 388, 256 with 16 nodes and 8 kv heads (64) 760 / 771, (32) 964 / 899; of
-    // ~500: 64, one token (128) 17.4 / 21.6, 128 32.3 / 28.2, 192 with 8 nodes 59.4 / 65.1, 256 90 / 72; 96 with 24 nodes (64) 61 / 72.
-    const int over = B - p.sp.slots;
-    p.sp.planned = B <= kPlanned && (tiles > p.sp.t_max ? B <= 4 * p.sp.slots : over < 0 || (over >= p.sp.slots / 4 && over <= p.sp.slots / 4 * 3));
+    // rounds are few, short ones while there are fewer sequences than places.  Planned / ranges of t_max: 28 and 4 heads, ~4000 keys: 96 with 8 nodes (128 places) 139 / 180 us, 192
+    // 274 / 302, 128 with 24 nodes (64 places) 344 / 388; 256 with 16 nodes and 8 kv heads (64) 760 / 771, (32) 964 / 899.  Short ones, eight shapes (32 to 128 places) with
+    // lengths of ~400 and ~2000 that differ and of 1000 that do not, unplanned over planned by the share of places taken: 5/8 1.20 and 0.89 (differing, equal), 6/8 1.22 and 0.88, 7/8
+    // 1.10 and 0.87, 15/16 1.01 and 0.87; in the second round 0 0.91 and 0.88, 1/8 1.05 and 0.88, 1/4 1.02 and 0.88, 1/2 1.02 and 0.87, 3/4 0.99 and 0.87; in the third 0.90 to 0.97 and 0.87.
+    p.sp.planned = B <= kPlanned && (tiles > p.sp.t_max ? B <= 4 * p.sp.slots : B < p.sp.slots);
     p.one_each = tiles <= (p.sp.planned ? p.sp.whole : p.sp.t_max);
     // (planned: items that fit `slots`, or those of ranges of t_max rounded up to whole rounds)
     const int64_t longest = (int64_t)B * ((tiles + p.sp.t_max - 1) / p.sp.t_max);

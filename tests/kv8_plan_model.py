@@ -29,8 +29,7 @@ def plan(B, n, Hq, Hkv, total):
     groups = 1 if kernel == "few" else -(-row_tiles // 24)
     slots = max(1, (256 if kernel == "many" else 512) // (Hkv * groups))
     whole = 8 if kernel == "few" else 4
-    over = B - slots
-    planned = B <= 256 and (B <= 4 * slots if tiles > 64 else over < 0 or slots // 4 <= over <= slots // 4 * 3)
+    planned = B <= 256 and (B <= 4 * slots if tiles > 64 else B < slots)
     one_each = tiles <= (whole if planned else 64)
     longest = B * -(-tiles // 64)
     rounds = -(-min(longest, B * tiles // 64 + B) // slots)
