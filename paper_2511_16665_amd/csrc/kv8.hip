@@ -54,7 +54,7 @@ __device__ __forceinline__ int64_t row_of(const KV8Layer& kv, int b, int slot) {
 // 32K, where an fp32 product position * frequency is 1e-3 rad off), once per row, and shared by the heads.  Bound by memory: 1536 rows of 28 and 4 heads of 128,
 // 27 MB, 9.8 us (0.7 of them the angles; the row's loads in front of the angles change nothing); one row 3.4 us, a launch and three dependent loads.
 template <typename T>
-__global__ __launch_bounds__(512) void kv8_write_k(const T* __restrict__ qkv, const T* __restrict__ bias, T* __restrict__ q_out, int64_t q_stride,
+__global__ __launch_bounds__(512) void kv8_write_k(const T* qkv, const T* __restrict__ bias, T* q_out, int64_t q_stride,   // (q_out may be qkv)
                                                    const int32_t* __restrict__ depth, int n, int n_q_heads, int lanes, double log2_theta, KV8Layer kv) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ float cs[128], sn[128];
