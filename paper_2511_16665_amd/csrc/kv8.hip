@@ -1174,14 +1174,16 @@ __device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t 
         }
     };
     auto backed = [&](int t) { return __builtin_amdgcn_readlane(pages, t) >= 0; };
+    bool top = false;   // some key or value of the page of the tile whose K was written last has the largest exponent, or is not finite
     auto write_k = [&](Raw& r, bool there) {
         const int ln = lane;
-        for (int rep = there ? 1 : 0; rep < 1; ++rep)   // (a loop, which stays a branch)
+        top = __builtin_amdgcn_ballot_w64(max(max(r.e[0], r.e[1]), max(r.ev[0], r.ev[1])) >= kTopExp) != 0;
+        for (int rep = there && !top ? 1 : 0; rep < 1; ++rep)   // (a loop, which stays a branch)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) r.c[j] = u32x4_t{0u, 0u, 0u, 0u}, r.e[j] = r.ev[j] = 127u;
-        if (__builtin_amdgcn_ballot_w64(max(r.e[0], r.e[1]) >= kTopExp) != 0)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) r.c[j] = r.e[j] >= kTopExp ? finite16(r.c[j]) : r.c[j];
+            for (int j = 0; j < 2; ++j) {
+                r.c[j] = there ? (r.e[j] >= kTopExp ? finite16(r.c[j]) : r.c[j]) : u32x4_t{0u, 0u, 0u, 0u};
+                r.e[j] = there ? r.e[j] : 127u, r.ev[j] = there ? r.ev[j] : 127u;
+            }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
@@ -1195,14 +1197,13 @@ __device__ __forceinline__ void kv8_mid_body(const KV8Item& it, int kh, int64_t 
     auto write_v = [&](Raw& r, int t, bool there) {
         const int ln = lane;
         const int left = there ? total - k0 - t * kKT : 0;   // (slots that nobody has written may hold anything)
-        for (int rep = left < kKT ? 0 : 1; rep < 1; ++rep)
+        for (int rep = left < kKT || top ? 0 : 1; rep < 1; ++rep)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) r.c[j][y] = 16 * wave + 8 * j + (ln >> 3) < left ? r.c[j][y] : 0u;
-        if (__builtin_amdgcn_ballot_w64(max(r.ev[0], r.ev[1]) >= kTopExp) != 0)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) r.c[j] = r.ev[j] >= kTopExp ? finite16(r.c[j]) : r.c[j];
+                r.c[j] = r.ev[j] >= kTopExp ? finite16(r.c[j]) : r.c[j];
+            }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = 16 * wave + 8 * j + (ln >> 3), p = ln & 7;
