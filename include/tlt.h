@@ -377,7 +377,7 @@ int tlt_kv8_write(void *stream, int dtype, int B, int n, int n_q_heads, int n_kv
  * ws: DEVICE scratch (256-byte aligned) of tlt_kv8_attention_workspace_bytes(...) bytes for this n or a larger one and a bound max_ctx >=
  * kv->seq_len_bound + n; it need not be cleared, and calls that may overlap in time need one each.  A seq_len[b] above
  * seq_len_bound is a caller error: the outputs of that call are undefined (no memory outside the buffers is touched).
- * At most 2^26 keys per sequence; the workspace function returns 0 for arguments that the call refuses.
+ * At most 2^26 keys per sequence; the workspace function returns 0 for arguments that the call refuses, in every dtype or with matrix instructions.
  * impl: -1 automatic: matrix instructions for bf16, head_dim 128, pages of 16 and 4-byte aligned exponents, else 0; 0 a workgroup
  * per row and query head (any shape). */
 size_t tlt_kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads, int head_dim, int max_ctx);

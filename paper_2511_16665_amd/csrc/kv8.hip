@@ -51,8 +51,9 @@ __device__ __forceinline__ int64_t row_of(const KV8Layer& kv, int b, int slot) {
 // ---- write
 // One workgroup per row (b, i).  A head (of q, k or v) belongs to a group of `lanes` lanes (a power of two); a lane holds VEC pairs (j, j + d/2) of it, one
 // 16-byte piece of either half.  The largest magnitude of a k or v head is taken over its group.  Angles are formed in double (positions reach
-// 32K, where an fp32 product position * frequency is 1e-3 rad off), once per row, and shared by the heads.  Bound by memory: 1536 rows of 28 and 4 heads of 128,
-// 27 MB, 9.8 us (0.7 of them the angles; the row's loads in front of the angles change nothing); one row 3.4 us, a launch and three dependent loads.
+// 32K, where an fp32 product position * frequency is 1e-3 rad off), once per row, and shared by the heads.  1536 rows of 28 and 4 heads of 128, 27 MB, 9.9 us
+// (2.7 TB/s): all workgroups are on the chip at once, and a row's chain of length, angle, projection, maximum, table and store is exposed once with nothing behind it (0.7 us of
+// it the angles; the row's loads in front of the angles change nothing).  One row 3.4 us, a launch and three dependent loads.
 template <typename T>
 __global__ __launch_bounds__(512) void kv8_write_k(const T* qkv, const T* __restrict__ bias, T* q_out, int64_t q_stride,   // (q_out may be qkv)
                                                    const int32_t* __restrict__ depth, int n, int n_q_heads, int lanes, double log2_theta, KV8Layer kv) {
@@ -714,7 +715,7 @@ struct KV8Out {
 // Few rows (NT tiles of 16): bound by memory.  A wave of the workgroup's four owns every fourth tile of the item's range with all rows, takes codes from
 // memory straight into the registers that the products want (no LDS, no barrier until the end) and keeps the next tile's in flight: keys once the
 // scores are done, values once the sums are.  The waves are joined through LDS.  64 sequences of ~8192 keys, 40 and 8 heads, one token: 1.08 GB in 177 us (6.1
-// TB/s); 16 of 8192, 28 and 4 heads: 135 MB in 28 us (4.8 TB/s, most of a fixed 5 us being planning and the first tile's way from memory); one: 6.9 us.
+// TB/s); 16 of 8192, 28 and 4 heads: 135 MB in 28.6 us (4.7 TB/s, most of a fixed 5 us being planning and the first tile's way from memory); one: 6.9 us.
 // Two waves per SIMD: three have no registers for the next tile (the same 64 sequences 205 us).
 template <int NT>
 __global__ __launch_bounds__(256, 2) void kv8_attn_few_k(KV8Split sp, int64_t q_stride, const uint16_t* __restrict__ q, KV8Rows rows, KV8Layer kv, KV8Out to,
@@ -861,12 +862,12 @@ __device__ __forceinline__ void dma_4(const uint8_t* base, uint32_t offset, uint
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t offset) { return (__attribute__((address_space(3))) T*)(uintptr_t)offset; }
 
-// More rows: bound by the matrix pipe and, side by side with it, the exponentials (32 sequences of ~4096 keys, 28 and 4 heads, 48 nodes, 91 GFLOP: 119 us, 63 % of
+// More rows: bound by the matrix pipe and, side by side with it, the exponentials (32 sequences of ~4096 keys, 28 and 4 heads, 48 nodes, 91 GFLOP: 119 us, 64 % of
 // the rate of a large product; the matrix pipes are busy 43 % of it).  One workgroup of eight waves, two per SIMD, streams the item's range once for up to 24
 // tiles of rows, dealt round-robin to the waves (NT each).  A tile of 64 keys passes through LDS twice: its codes come from memory by direct loads, kRaw tiles ahead,
 // a wave's eight keys (1 KB each of K and V) to a place that only this wave reads; the wave converts them to bf16 and stores them for all, K rows swizzled by
 // the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by twice the key (a transposing read takes two neighbouring places of each of 8
-// keys).  The two waves of a SIMD run half a period apart, so that one's softmax runs under the other's products: per tile a wave does [P V of the tile
+// keys; the stores of two neighbouring keys, though, meet in the 8 even places and then in the odd ones).  The two waves of a SIMD run half a period apart, so that one's softmax runs under the other's products: per tile a wave does [P V of the tile
 // before, Q K^T] and then [softmax, conversion of the next tile], and the early waves 0 .. 3 meet the tile's barrier in front of the first half, the
 // late ones 4 .. 7 between the two.  Between barriers `it` and `it + 1` all read K of tile it and V of it - 1, and write both of tile it + 1: two
 // stages of K and three of V.
@@ -1116,7 +1117,7 @@ __global__ __launch_bounds__(512) void kv8_attn_many_k(KV8Split sp, int64_t q_st
 // start under the other's work.  They stream the item's range for all tiles of rows, dealt round-robin to the waves (NT each).  A tile of 64 keys passes
 // through LDS twice: its codes come from memory by direct loads, two tiles ahead, a wave's page (2 KB each of K and V) to a place that only this wave reads;
 // the wave converts them to bf16 and stores them for all, K rows swizzled by the key (the 16-byte fragments of 16 keys hit 16 distinct places), V rows by
-// twice the key (a transposing read takes two neighbouring places of each of 8 keys).  There is one stage of either: V of a tile is converted
+// twice the key (a transposing read takes two neighbouring places of each of 8 keys; stores of two neighbouring keys meet).  There is one stage of either: V of a tile is converted
 // under Q K^T, K of the next one under P V.  16 sequences of 8192 keys, 28 and 4 heads, 16 nodes (7 tiles of rows, 30 GFLOP): 56 us; the matrix pipes are busy 29 % of
 // it, the chain of barrier, reads, products and exponentials is what takes the time (two workgroups per CU hide one another's only in part).
 constexpr int kMidRaw = 2, kMidLds = 2 * kStage + kMidRaw * kRawBytes + 64 * 8;
