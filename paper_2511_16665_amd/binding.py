@@ -502,7 +502,7 @@ class KV8:
     """8-bit paged KV cache of one model (tlt_kv8): codes [L, n_pages, Hkv, page, d] and exponent bytes [L, n_pages, Hkv, page] of keys and
     values (one byte per element: uint8, or float8_e4m3fn for the codes); the other fields as in KV.  Fields may be set one by one where their shapes
     stay, and together by replace(); they are checked against each other first, and one that does not fit leaves the cache as it was.  The tensors'
-    addresses are taken at every call."""
+    addresses are taken at every call, their shapes when they are set: one that has been resized in place is set again."""
     _TENSORS = ("k_pool", "v_pool", "k_exp", "v_exp", "block_table", "seq_len")
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, block_table: torch.Tensor,
