@@ -397,6 +397,109 @@ int tlt_kv8_commit(void *stream, int B, int n_layers, int n_kv_heads, int head_d
 int tlt_kv8_read(void *stream, int dtype, int n_layers, int B, int n, int n_kv_heads, int head_dim, int page_size,
                  const tlt_kv8 *kv, const int32_t *first, const int32_t *count, void *out_k, void *out_v);
 
+/* ---- pages of a paged cache -----------------------------------------------------------------------
+ * The block tables that every call on a cache takes, kept on the device: what a step adds to each sequence is known there (accepted
+ * lengths), and a table made on the host costs a round trip per step.  Free pages are a stack; growing pops from it, releasing pushes
+ * back, and a release of exactly what a growth took leaves stack and table as they were.  Page ids outside 0 .. n_pages - 1 are
+ * the caller's mistake: rows that meet one get slot -1, which tlt_rope_write does not write. */
+typedef struct tlt_pages {
+    int32_t *free_page;    /* DEVICE [n_pages]: entries 0 .. *n_free - 1 are the free pages, the last of them is taken first */
+    int32_t *n_free;       /* DEVICE [1] */
+    int32_t *page_count;   /* DEVICE [B]: sequence b holds pages block_table[b][0 .. page_count[b] - 1] */
+    int32_t *block_table;  /* DEVICE [B][max_pages], the table of tlt_kv and tlt_kv8 */
+    int64_t n_pages;
+    int32_t max_pages, page_size;
+} tlt_pages;
+
+/* Pages for n_new[b] rows behind the seq_len[b] of every sequence (DEVICE [B] both; negative counts as 0), and where those rows belong.
+ * A sequence needs the pages that seq_len + n_new fill beyond the ones it holds; sequences are served in order, lower table entries
+ * first, as long as everything that was needed so far is free: the first that does not fit and all behind it that need pages
+ * get none (granted 0).  A sequence that max_pages cannot hold, or whose page_count is not in 0 .. max_pages, is not granted either and takes nothing from the others.
+ * Rows of all sequences lie side by side: row_start[b] (DEVICE [B + 1]) is the first of sequence b's, row_start[B] their number (held at
+ * 2^31 - 1).  For row t = row_start[b] + i: row_seq[t] = b, position[t] = seq_len[b] + depth[t] (depth DEVICE [max_rows]; NULL: i), slot[t] =
+ * page * page_size + row in it of the sequence's token seq_len[b] + i, -1 where it was not granted.  Rows behind the last one, up to max_rows
+ * (the size of the four row arrays), are row_seq -1, position 0, slot -1, so that a captured step can run over max_rows rows; rows
+ * from max_rows on are not written.  Any output may be NULL.  B <= TLT_MAX_PAGED (TLT_ESHAPE). */
+enum { TLT_MAX_PAGED = 4096 };
+int tlt_pages_grow(void *stream, int B, const tlt_pages *pages, const int32_t *seq_len, const int32_t *n_new, const int32_t *depth, int max_rows,
+                   int32_t *row_start, int32_t *row_seq, int32_t *position, int64_t *slot, int32_t *granted);
+
+/* Gives back the pages behind the first keep_len[b] tokens of every sequence (DEVICE [B], negative counts as 0; NULL: all of them): their table
+ * entries become -1, page_count falls, and they go onto the stack, the last sequence's last page first.  A sequence that holds no
+ * more, or whose page_count is not in 0 .. max_pages, keeps what it has.  If the stack cannot hold them (*n_free + pages > n_pages: pages that were never taken) nothing changes. */
+int tlt_pages_release(void *stream, int B, const tlt_pages *pages, const int32_t *keep_len);
+
+/* ---- rotary positions -----------------------------------------------------------------------------
+ * The first rot_dim elements of every query and key head are turned in pairs: pair j by position * freq[j] radians (the product in
+ * double), (a, b) -> amplitude * (a cos - b sin, a sin + b cos); elements from rot_dim on stay as they are.  Pairs are elements
+ * (j, j + rot_dim / 2) (TLT_ROPE_HALF) or (2j, 2j + 1) (TLT_ROPE_INTERLEAVED). */
+enum { TLT_ROPE_HALF = 0, TLT_ROPE_INTERLEAVED = 1 };
+typedef struct tlt_rope {
+    const double *freq;        /* DEVICE [rot_dim / 2] */
+    int32_t rot_dim, layout;   /* rot_dim even, 2 .. head_dim */
+    float amplitude;           /* 1 but for scalings that ask for another */
+} tlt_rope;
+
+/* Frequencies (HOST, no GPU work): freq [rot_dim / 2] for a context `factor` >= 1 times as long as the original_len that the model was trained
+ * on, from f_j = theta^(-2j / rot_dim):
+ *   PLAIN   f_j                                    (factor, original_len, low, high unused)
+ *   LINEAR  f_j / factor
+ *   BASE    f_j of theta * factor^(rot_dim / (rot_dim - 2))
+ *   RAMP    (1 - s) f_j + s f_j / factor, s rising from 0 to 1 between the pairs that turn `high` and `low` times over original_len (the first
+ *           rounded down, the second up, held in 0 .. rot_dim - 1); *amplitude = 0.1 ln(factor) + 1
+ *   BANDS   the same sum with 1 - s = (turns - low) / (high - low) held in 0 .. 1, turns = original_len * f_j / 2 pi
+ * *amplitude (may be NULL) is 1 otherwise.  TLT_EINVAL: sizes, theta <= 1, factor < 1, RAMP and BANDS without 0 < low < high and original_len > 0. */
+enum { TLT_ROPE_PLAIN = 0, TLT_ROPE_LINEAR = 1, TLT_ROPE_BASE = 2, TLT_ROPE_RAMP = 3, TLT_ROPE_BANDS = 4 };
+int tlt_rope_freqs(int kind, int rot_dim, double theta, double factor, double original_len, double low, double high, double *freq, float *amplitude);
+
+/* `rows` new rows of one layer, from their projection qkv (DEVICE, dtype, rows of (Hq+2Hkv)*d elements qkv_stride apart): bqkv [(Hq+2Hkv)*d] is added
+ * (NULL: none), queries and keys are turned at position[r] (DEVICE [rows]), and
+ *   queries go to q_out, rows of Hq*d elements q_stride apart (NULL: nowhere),
+ *   keys and values to slot[r] (DEVICE [rows], as tlt_pages_grow gives them) of ONE layer's pools: kv's (dtype's type) or kv8's (as tlt_kv8_write
+ *   quantises; head_dim 64, 128, 192, 256), of which the pools and n_pages are read; rows whose slot is not in 0 .. n_pages * page_size - 1 are
+ *   not written,
+ *   keys and values to kv_out, rows of 2*Hkv*d elements kv_stride apart (NULL: nowhere).
+ * kv and kv8: one at most, with slot; at least one output.  q_out may be qkv with its stride, kv_out may be qkv + Hq*d with its stride; other
+ * overlaps, and two rows with one slot, are caller errors (such rows then hold a mixture).  head_dim even, <= 256; any page size; rows < 2^23; pointers and
+ * strides in whole elements (kv8's pools 16-byte aligned); 16-byte aligned rows of heads in whole 16-byte pieces are the fast case.  Sums and rotations are fp32, one rounding to dtype. */
+int tlt_rope_write(void *stream, int dtype, int rows, int n_q_heads, int n_kv_heads, int head_dim, int page_size, const tlt_rope *rope, const void *qkv,
+                   int64_t qkv_stride, const void *bqkv, const int32_t *position, const int64_t *slot, const tlt_kv *kv, const tlt_kv8 *kv8, void *q_out,
+                   int64_t q_stride, void *kv_out, int64_t kv_stride);
+
+/* ---- sampling -------------------------------------------------------------------------------------
+ * What every request asks for, DEVICE arrays with an entry per sequence, each NULL for none: temperature (NULL: 1), top_k (<= 0: off), top_p
+ * (off unless < 1), min_p (off unless > 0).
+ *
+ * A row of logits l gives whole-number weights W_j = floor(exp(l_j / temperature - max / temperature) * 2^32) (exp in double: tlt_accept's), so every sum
+ * is exact.  Tokens are ordered by falling logit, equal ones by rising index; tokens at -infinity are never kept.  Kept are
+ *   the first top_k of the order, weight S_k together;
+ *   of these the ones before which less than top_p * S_k lies (top_p in units of 2^-31, rounded down; the first one always);
+ *   of these the ones with W_j >= min_p * 2^32 (rounded down; the first one always).
+ * A temperature that is not positive keeps the first token of the order alone, weights as at temperature 1.  A row with a NaN, or with
+ * nothing above -infinity, keeps nothing; +infinity is a largest value like any other.  Logits of dtype TLT_F32 or TLT_BF16, rows `row_stride` elements apart (>= vocab); row r belongs
+ * to sequence r / rows_per_seq (the nodes of a tree lie side by side).  vocab <= 2^24, rows < 2^23.
+ * ws: DEVICE scratch (256-byte aligned) of tlt_sample_workspace_bytes(rows, vocab) bytes; it need not be cleared, and calls that may overlap in
+ * time need one each.  The function returns 0 for sizes that the calls refuse. */
+typedef struct tlt_filter {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+} tlt_filter;
+size_t tlt_sample_workspace_bytes(int rows, int vocab);
+
+/* One token per row: the first, by index, whose running sum of kept weights exceeds (u[r] * S) >> 32, S their whole sum and u (DEVICE [rows])
+ * the caller's 32-bit uniforms: the final draw of tlt_accept.  out_token [rows] (-1 where nothing is kept); out_logprob [rows][2] fp32, may be NULL: the
+ * token's log-probability in the distribution it was drawn from and in the row's whole one, l / temperature - max / temperature - ln(S 2^-32) with S
+ * the kept or the whole sum (-infinity where nothing is kept, NaN with a NaN in the row); out_kept [rows], may be NULL: number of tokens kept. */
+int tlt_sample(void *stream, int dtype, int rows, int rows_per_seq, int vocab, const void *logits, int64_t row_stride, const tlt_filter *filter,
+               const uint32_t *u, int32_t *out_token, float *out_logprob, int32_t *out_kept, void *ws, size_t ws_bytes);
+
+/* The kept tokens' logits, -infinity in the place of all others (rows that keep nothing are copied): what tlt_accept takes as target_logits so that
+ * a tree's tokens follow the FILTERED distribution of the target.  out (dtype, rows out_stride >= vocab elements apart) may be logits itself with the
+ * same stride; columns from vocab on are not touched. */
+int tlt_sample_filter(void *stream, int dtype, int rows, int rows_per_seq, int vocab, const void *logits, int64_t row_stride, const tlt_filter *filter,
+                      void *out, int64_t out_stride, int32_t *out_kept, void *ws, size_t ws_bytes);
+
 /* Attention kernel choice for cross-checks: -1 automatic (default), 0 wave-per-row kernel,
  * 1 MFMA split-KV kernel (bf16, head_dim 128 only; other shapes fall back to 0). */
 int tlt_set_attention_impl(tlt_ctx *ctx, int impl);

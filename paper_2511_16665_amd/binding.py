@@ -29,6 +29,7 @@ EXPORTS = [
     "tlt_template_build", "tlt_draft_sample", "tlt_gemm_argmax", "tlt_gemm_glu", "tlt_gemm_parts", "tlt_draft_pool", "tlt_set_oproj_rounding", "tlt_device_status", "tlt_accept_sample_static", "tlt_attention", "tlt_attention_workspace_bytes",
     "tlt_graph_pool_create", "tlt_graph_pool_destroy", "tlt_graph_pool_step", "tlt_graph_pool_count", "tlt_mfma_stream", "tlt_prefill", "tlt_step_report",
     "tlt_kv8_write", "tlt_kv8_attention", "tlt_kv8_attention_workspace_bytes", "tlt_kv8_commit", "tlt_kv8_read",
+    "tlt_pages_grow", "tlt_pages_release", "tlt_rope_freqs", "tlt_rope_write", "tlt_sample", "tlt_sample_filter", "tlt_sample_workspace_bytes",
 ]
 
 
@@ -64,6 +65,19 @@ class KVC(C.Structure):
 class KV8C(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("n_pages", C.c_int64),
                 ("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("max_pages", C.c_int32), ("seq_len_bound", C.c_int32)]
+
+
+class PagesC(C.Structure):
+    _fields_ = [("free_page", C.c_void_p), ("n_free", C.c_void_p), ("page_count", C.c_void_p), ("block_table", C.c_void_p), ("n_pages", C.c_int64),
+                ("max_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class RopeC(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float)]
+
+
+class FilterC(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("temperature", "top_k", "top_p", "min_p")]
 
 
 class TreeC(C.Structure):
@@ -128,6 +142,15 @@ def load() -> C.CDLL:
     lib.tlt_kv8_write.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.c_float] + [C.c_void_p] * 3 + [C.POINTER(KV8C), C.c_void_p, C.c_int64]
     lib.tlt_kv8_attention_workspace_bytes.restype = C.c_size_t
     lib.tlt_kv8_attention_workspace_bytes.argtypes = [C.c_int] * 6
+    lib.tlt_pages_grow.argtypes = [C.c_void_p, C.c_int, C.POINTER(PagesC)] + [C.c_void_p] * 3 + [C.c_int] + [C.c_void_p] * 5
+    lib.tlt_pages_release.argtypes = [C.c_void_p, C.c_int, C.POINTER(PagesC), C.c_void_p]
+    lib.tlt_rope_freqs.argtypes = [C.c_int] * 2 + [C.c_double] * 5 + [C.c_void_p, C.POINTER(C.c_float)]
+    lib.tlt_rope_write.argtypes = [C.c_void_p] + [C.c_int] * 6 + [C.POINTER(RopeC), C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + \
+        [C.POINTER(KVC), C.POINTER(KV8C), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
+    lib.tlt_sample_workspace_bytes.restype = C.c_size_t
+    lib.tlt_sample_workspace_bytes.argtypes = [C.c_int] * 2
+    lib.tlt_sample.argtypes = [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_int64, C.POINTER(FilterC)] + [C.c_void_p] * 5 + [C.c_size_t]
+    lib.tlt_sample_filter.argtypes = [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p, C.c_int64, C.POINTER(FilterC), C.c_void_p, C.c_int64] + [C.c_void_p] * 2 + [C.c_size_t]
     lib.tlt_kv8_attention.argtypes = [C.c_void_p] + [C.c_int] * 7 + [C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(KV8C), C.c_void_p, C.c_void_p,
                                                                    C.c_size_t, C.c_int]
     lib.tlt_kv8_commit.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.POINTER(KV8C), C.c_void_p, C.c_void_p, C.c_int]
@@ -630,6 +653,186 @@ def kv8_read(dtype_code, kv: KV8, first, count, out_k, out_v):
                              _addr(out_k, kv, shape, dt), _addr(out_v, kv, shape, dt))
     if rc:
         raise TltError(rc, "tlt_kv8_read")
+
+
+# ---- pages, rotary positions, sampling: what a step of a caller with a forward of its own needs around the attention calls
+
+def _here(device: int) -> int:
+    """The current stream of `device`, which has to be the current one."""
+    assert device == torch.cuda.current_device(), "the tensors lie on another device than the current one"
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _at(t: Optional[torch.Tensor], device: int, shape, dtype, name: str):
+    """The address of a contiguous device tensor of this shape and type; None stays None."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device, f"{name}: a contiguous {dtype} tensor {tuple(shape)} on the device of the others"
+    return t.data_ptr()
+
+
+def _row_step(t: torch.Tensor, device: int, rows: int, width: int, dtype, name: str) -> int:
+    """Elements between the rows of a tensor [..., width] whose leading dimensions are rows, evenly spaced; checks them."""
+    assert t.dtype is dtype and t.get_device() == device and t.shape[-1] == width and t.numel() == rows * width, f"{name}: {rows} rows of {width} {dtype} on the device of the others"
+    assert width == 1 or t.stride(-1) == 1, f"{name}: elements of a row lie side by side"
+    step, expect = width, None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:          # (a dimension of one element may have any stride)
+            continue
+        if expect is None:
+            step = stride
+        else:
+            assert stride == expect, f"{name}: rows must be evenly spaced"
+        expect = stride * size
+    assert step >= width, f"{name}: rows may not overlap"
+    return step
+
+
+class Pages:
+    """The pages of a paged cache (tlt_pages): free_page [n_pages], n_free [1], page_count [B], block_table [B, max_pages], int32 device tensors; block_table is the one
+    that the cache's handle (KV, KV8) holds.  The tensors' addresses and shapes are taken at every call."""
+
+    def __init__(self, free_page: torch.Tensor, n_free: torch.Tensor, page_count: torch.Tensor, block_table: torch.Tensor, page_size: int):
+        self.free_page, self.n_free, self.page_count, self.block_table, self.page_size = free_page, n_free, page_count, block_table, int(page_size)
+
+    @staticmethod
+    def empty(B, n_pages, max_pages, page_size, device="cuda") -> "Pages":
+        """All pages free, the lowest taken first; no sequence holds any."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return Pages(torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32), torch.zeros((B,), **i32), torch.full((B, max_pages), -1, **i32), page_size)
+
+    def c(self):
+        """(the C handle, sequences, device)"""
+        table = self.block_table
+        dev, (B, max_pages) = table.get_device(), table.shape
+        i32 = torch.int32
+        assert dev >= 0, "device tensors"
+        return PagesC(_at(self.free_page, dev, self.free_page.shape[:1], i32, "free_page"), _at(self.n_free, dev, (1,), i32, "n_free"),
+                      _at(self.page_count, dev, (B,), i32, "page_count"), _at(table, dev, (B, max_pages), i32, "block_table"), self.free_page.numel(), max_pages, self.page_size), B, dev
+
+
+def pages_grow(pages: Pages, seq_len, n_new, depth, row_start, row_seq, position, slot, granted):
+    """tlt_pages_grow: seq_len, n_new [B] int32; depth [rows] int32 or None; outputs (each may be None) row_start [B + 1], row_seq, position [rows] and granted [B] int32,
+    slot [rows] int64, all row tensors of one size."""
+    c, B, dev = pages.c()
+    row_tensors = [t for t in (depth, row_seq, position, slot) if t is not None]
+    rows, i32 = (row_tensors[0].numel() if row_tensors else 0), torch.int32
+    rc = load().tlt_pages_grow(_here(dev), B, c, _at(seq_len, dev, (B,), i32, "seq_len"), _at(n_new, dev, (B,), i32, "n_new"), _at(depth, dev, (rows,), i32, "depth"), rows,
+                               _at(row_start, dev, (B + 1,), i32, "row_start"), _at(row_seq, dev, (rows,), i32, "row_seq"), _at(position, dev, (rows,), i32, "position"),
+                               _at(slot, dev, (rows,), torch.int64, "slot"), _at(granted, dev, (B,), i32, "granted"))
+    if rc:
+        raise TltError(rc, "tlt_pages_grow")
+
+
+def pages_release(pages: Pages, keep_len):
+    """tlt_pages_release: keep_len [B] int32, or None: everything."""
+    c, B, dev = pages.c()
+    rc = load().tlt_pages_release(_here(dev), B, c, _at(keep_len, dev, (B,), torch.int32, "keep_len"))
+    if rc:
+        raise TltError(rc, "tlt_pages_release")
+
+
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+
+
+def rope_freqs(scaling: str, rot_dim: int, theta: float, factor: float = 1.0, original_len: float = 0.0, low: float = 1.0, high: float = 32.0):
+    """tlt_rope_freqs: (frequencies [rot_dim / 2] float64 on the host, amplitude)."""
+    freq, amplitude = np.empty(max(rot_dim // 2, 1), np.float64), C.c_float()
+    rc = load().tlt_rope_freqs(ROPE_SCALING[scaling], rot_dim, theta, factor, original_len, low, high, freq.ctypes.data, C.byref(amplitude))
+    if rc:
+        raise TltError(rc, "tlt_rope_freqs")
+    return freq, amplitude.value
+
+
+class Rope:
+    """tlt_rope: freq [rot_dim / 2] float64 device tensor (radians per position, as rope_freqs gives them), layout of the pairs, amplitude."""
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
+        assert freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous() and freq.get_device() >= 0, "freq: a contiguous float64 device tensor"
+        self.freq, self.interleaved, self.amplitude = freq, bool(interleaved), float(amplitude)
+
+
+def rope_write(dtype_code, n_q_heads, n_kv_heads, head_dim, rope: Rope, qkv, bias, position, slot, kv, layer, q_out, kv_out=None):
+    """tlt_rope_write: qkv rows [..., (Hq+2Hkv)*d], evenly spaced; bias [(Hq+2Hkv)*d] or None; position [rows] int32, slot [rows] int64 (None without a cache); kv a KV (pools
+    [layers, pages, Hkv, page, d] of dtype_code's type, or one layer's), a KV8 or None, `layer` of it; q_out rows [..., Hq*d] and kv_out rows [..., 2*Hkv*d], each or None."""
+    dev, dt, d = qkv.get_device(), torch_dtype(dtype_code), head_dim
+    width, rows = (n_q_heads + 2 * n_kv_heads) * d, position.numel()
+    step = _row_step(qkv, dev, rows, width, dt, "qkv")
+    q_step = _row_step(q_out, dev, rows, n_q_heads * d, dt, "q_out") if q_out is not None else 0
+    kv_step = _row_step(kv_out, dev, rows, 2 * n_kv_heads * d, dt, "kv_out") if kv_out is not None else 0
+    assert rope.freq.get_device() == dev, "freq lies on another device"
+    kvc = kv8c = None
+    page = 1
+    if isinstance(kv, KV8):
+        _, _, heads, page, pool_d = kv.dims
+        assert (heads, pool_d) == (n_kv_heads, d) and kv.k_pool.get_device() == dev, "the cache's shape and device"
+        kv8c = kv.c(layer)
+    elif kv is not None:
+        shape = tuple(kv.k_pool.shape)
+        assert kv.k_pool.dim() in (4, 5) and kv.v_pool.shape == kv.k_pool.shape and (shape[-3], shape[-1]) == (n_kv_heads, d), "the cache's shape"
+        assert all(t.dtype is dt and t.is_contiguous() and t.get_device() == dev for t in (kv.k_pool, kv.v_pool)), "contiguous pools of the model's type on the device of the others"
+        page = shape[-2]
+        if not 0 <= layer < (shape[0] if len(shape) == 5 else 1):
+            raise IndexError(f"layer {layer}")
+        at = layer * shape[-4] * n_kv_heads * page * d * kv.k_pool.element_size()
+        kvc = KVC(kv.k_pool.data_ptr() + at, kv.v_pool.data_ptr() + at, shape[-4], None, None, 0, 0)
+    rc = load().tlt_rope_write(_here(dev), dtype_code, rows, n_q_heads, n_kv_heads, d, page, RopeC(rope.freq.data_ptr(), 2 * rope.freq.numel(), int(rope.interleaved), rope.amplitude),
+                               qkv.data_ptr(), step, _at(bias, dev, (width,), dt, "bias"), _at(position, dev, (rows,), torch.int32, "position"),
+                               _at(slot, dev, (rows,), torch.int64, "slot"), kvc, kv8c, None if q_out is None else q_out.data_ptr(), q_step,
+                               None if kv_out is None else kv_out.data_ptr(), kv_step)
+    if rc:
+        raise TltError(rc, "tlt_rope_write")
+
+
+class SampleFilter:
+    """tlt_filter: what each sequence asks for, device tensors [B] or None: temperature, top_p, min_p float32, top_k int32."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
+
+    def c(self, B, device) -> FilterC:
+        f32 = torch.float32
+        return FilterC(_at(self.temperature, device, (B,), f32, "temperature"), _at(self.top_k, device, (B,), torch.int32, "top_k"), _at(self.top_p, device, (B,), f32, "top_p"),
+                       _at(self.min_p, device, (B,), f32, "min_p"))
+
+
+def sample_workspace(rows, vocab) -> torch.Tensor:
+    nbytes = load().tlt_sample_workspace_bytes(rows, vocab)
+    if nbytes == 0:
+        raise TltError(-1, "tlt_sample_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
+def _logit_rows(logits, dtype_code):
+    """(device, rows, rows per sequence, sequences, vocab, elements between rows) of logits [B, V] or [B, n, V]."""
+    assert logits.dim() in (2, 3), "logits [B, V] or [B, n, V]"
+    B, V, n = logits.shape[0], logits.shape[-1], logits.shape[1] if logits.dim() == 3 else 1
+    dev = logits.get_device()
+    return dev, B * n, n, B, V, _row_step(logits, dev, B * n, V, torch_dtype(dtype_code), "logits")
+
+
+def sample(dtype_code, logits, asked: SampleFilter, u, token, logprob, kept, ws):
+    """tlt_sample: logits [B, V] or [B, n, V] of dtype_code's type (rows evenly spaced, so a slice of wider rows will do), u like logits without V, int32 or uint32;
+    token and kept (may be None) int32 of u's shape, logprob (may be None) float32 [..., 2]."""
+    dev, rows, n, B, V, step = _logit_rows(logits, dtype_code)
+    shape = logits.shape[:-1]
+    assert ws.is_contiguous() and ws.get_device() == dev
+    rc = load().tlt_sample(_here(dev), dtype_code, rows, n, V, logits.data_ptr(), step, asked.c(B, dev), _at(u, dev, shape, u.dtype if u.dtype in (torch.int32, torch.uint32) else torch.int32, "u"),
+                           _at(token, dev, shape, torch.int32, "token"), _at(logprob, dev, (*shape, 2), torch.float32, "logprob"), _at(kept, dev, shape, torch.int32, "kept"),
+                           ws.data_ptr(), ws.numel() * ws.element_size())
+    if rc:
+        raise TltError(rc, "tlt_sample")
+
+
+def sample_filter(dtype_code, logits, asked: SampleFilter, out, kept, ws):
+    """tlt_sample_filter: out like logits (may be logits itself), kept (may be None) int32 of logits' shape without V."""
+    dev, rows, n, B, V, step = _logit_rows(logits, dtype_code)
+    assert out.shape == logits.shape and ws.is_contiguous() and ws.get_device() == dev
+    rc = load().tlt_sample_filter(_here(dev), dtype_code, rows, n, V, logits.data_ptr(), step, asked.c(B, dev), out.data_ptr(),
+                                  _row_step(out, dev, rows, V, torch_dtype(dtype_code), "out"), _at(kept, dev, logits.shape[:-1], torch.int32, "kept"), ws.data_ptr(), ws.numel() * ws.element_size())
+    if rc:
+        raise TltError(rc, "tlt_sample_filter")
 
 
 def gemm_argmax(A, W, ws, out):

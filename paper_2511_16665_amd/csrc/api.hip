@@ -1276,6 +1276,131 @@ int tlt_kv8_read(void* stream, int dtype, int n_layers, int B, int n, int n_kv_h
     return e == hipSuccess ? TLT_OK : TLT_EHIP;
 }
 
+static int check_pages(const tlt_pages* pages, int B) {
+    if (B < 1 || !pages || !pages->free_page || !pages->n_free || !pages->page_count || !pages->block_table || pages->n_pages < 1 || pages->n_pages > 0x7fffffff ||
+        pages->max_pages < 1 || pages->page_size < 1)
+        return TLT_EINVAL;
+    return B > TLT_MAX_PAGED ? TLT_ESHAPE : TLT_OK;
+}
+
+static PageState page_state(const tlt_pages* pages) {
+    PageState p;
+    p.free_page = pages->free_page;
+    p.n_free = pages->n_free;
+    p.page_count = pages->page_count;
+    p.block_table = pages->block_table;
+    p.n_pages = pages->n_pages;
+    p.max_pages = pages->max_pages;
+    p.page_size = pages->page_size;
+    return p;
+}
+
+int tlt_pages_grow(void* stream, int B, const tlt_pages* pages, const int32_t* seq_len, const int32_t* n_new, const int32_t* depth, int max_rows,
+                   int32_t* row_start, int32_t* row_seq, int32_t* position, int64_t* slot, int32_t* granted) {
+    if (!seq_len || !n_new || max_rows < 0) return TLT_EINVAL;
+    const int rc = check_pages(pages, B);
+    if (rc) return rc;
+    const hipError_t e = pages_grow((hipStream_t)stream, B, page_state(pages), seq_len, n_new, depth, max_rows, row_start, row_seq, position, slot, granted);
+    return e == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
+int tlt_pages_release(void* stream, int B, const tlt_pages* pages, const int32_t* keep_len) {
+    const int rc = check_pages(pages, B);
+    if (rc) return rc;
+    return pages_release((hipStream_t)stream, B, page_state(pages), keep_len) == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
+int tlt_rope_write(void* stream, int dtype, int rows, int n_q_heads, int n_kv_heads, int head_dim, int page_size, const tlt_rope* rope, const void* qkv,
+                   int64_t qkv_stride, const void* bqkv, const int32_t* position, const int64_t* slot, const tlt_kv* kv, const tlt_kv8* kv8, void* q_out,
+                   int64_t q_stride, void* kv_out, int64_t kv_stride) {
+    const int e = dtype == TLT_F32 ? 4 : 2;
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || rows < 1 || rows >= (1 << 23) || !heads_ok(n_q_heads, n_kv_heads) || head_dim < 2 || head_dim > 256 ||
+        head_dim % 2 || page_size < 1 || !rope || !rope->freq || rope->rot_dim < 2 || rope->rot_dim > head_dim || rope->rot_dim % 2 ||
+        (rope->layout != TLT_ROPE_HALF && rope->layout != TLT_ROPE_INTERLEAVED) || !qkv || !position)
+        return TLT_EINVAL;
+    const int64_t heads = n_q_heads + 2 * (int64_t)n_kv_heads;
+    // (a workgroup per four heads of a row, and 256 threads each, have to fit a grid)
+    if (qkv_stride < heads * head_dim || (double)rows * heads / 4 >= (double)(1 << 24) - 1) return TLT_EINVAL;
+    if ((((uintptr_t)qkv | (uintptr_t)bqkv | (uintptr_t)q_out | (uintptr_t)kv_out) & (e - 1)) != 0 || ((uintptr_t)rope->freq & 7) != 0) return TLT_EINVAL;
+    if ((kv && kv8) || (!kv && !kv8 && !q_out && !kv_out)) return TLT_EINVAL;
+    if ((q_out && q_stride < (int64_t)n_q_heads * head_dim) || (kv_out && kv_stride < 2 * (int64_t)n_kv_heads * head_dim)) return TLT_EINVAL;
+    RopeIn in;
+    in.qkv = qkv;
+    in.bias = bqkv;
+    in.stride = qkv_stride;
+    in.position = position;
+    in.slot = slot;
+    in.freq = rope->freq;
+    in.rot_dim = rope->rot_dim;
+    in.interleaved = rope->layout == TLT_ROPE_INTERLEAVED;
+    in.amplitude = rope->amplitude;
+    RopeOut out;
+    out.q = q_out;
+    out.q_stride = q_stride;
+    out.rows = kv_out;
+    out.rows_stride = kv_stride;
+    out.page_size = page_size;
+    out.n_kv = n_kv_heads;
+    out.d = head_dim;
+    if (kv || kv8) {
+        const int64_t n_pages = kv ? kv->n_pages : kv8->n_pages;
+        if (!slot || ((uintptr_t)slot & 7) != 0 || n_pages < 1 || n_pages > 0x7fffffff) return TLT_EINVAL;
+        out.k = kv ? kv->k_pool : kv8->k_pool;
+        out.v = kv ? kv->v_pool : kv8->v_pool;
+        if (!out.k || !out.v || (((uintptr_t)out.k | (uintptr_t)out.v) & (kv ? e - 1 : 15)) != 0) return TLT_EINVAL;
+        if (kv8) {
+            if (head_dim < 64 || head_dim % 64 || !kv8->k_exp || !kv8->v_exp) return TLT_EINVAL;
+            out.k_exp = (uint8_t*)kv8->k_exp;
+            out.v_exp = (uint8_t*)kv8->v_exp;
+        }
+        out.n_slots = n_pages * page_size;
+    }
+    return rope_write((hipStream_t)stream, dtype, rows, n_q_heads, in, out) == hipSuccess ? TLT_OK : TLT_EHIP;
+}
+
+constexpr int kMostVocab = 1 << 24;   // indices and counts of a row; its sum of weights stays below 2^56
+
+size_t tlt_sample_workspace_bytes(int rows, int vocab) {
+    if (rows < 1 || rows >= (1 << 23) || vocab < 1 || vocab > kMostVocab) return 0;
+    return pick_workspace_bytes(rows, vocab);
+}
+
+static int run_pick(void* stream, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const tlt_filter* filter,
+                    const PickOut& out, void* ws, size_t ws_bytes) {
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || rows < 1 || rows >= (1 << 23) || rows_per_seq < 1 || rows % rows_per_seq || vocab < 1 || vocab > kMostVocab ||
+        !logits || row_stride < vocab || !filter || !ws || ((uintptr_t)ws & 255) != 0)
+        return TLT_EINVAL;
+    if ((((uintptr_t)logits | (uintptr_t)out.rows) & (dtype == TLT_F32 ? 3 : 1)) != 0) return TLT_EINVAL;
+    PickFilter f;
+    f.temperature = filter->temperature;
+    f.top_k = filter->top_k;
+    f.top_p = filter->top_p;
+    f.min_p = filter->min_p;
+    const hipError_t e = pick((hipStream_t)stream, dtype, rows, rows_per_seq, vocab, logits, row_stride, f, out, ws, ws_bytes);
+    return e == hipSuccess ? TLT_OK : (e == hipErrorInvalidValue ? TLT_ESHAPE : TLT_EHIP);
+}
+
+int tlt_sample(void* stream, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const tlt_filter* filter,
+               const uint32_t* u, int32_t* out_token, float* out_logprob, int32_t* out_kept, void* ws, size_t ws_bytes) {
+    if (!u || !out_token) return TLT_EINVAL;
+    PickOut out;
+    out.u = u;
+    out.token = out_token;
+    out.logprob = out_logprob;
+    out.kept = out_kept;
+    return run_pick(stream, dtype, rows, rows_per_seq, vocab, logits, row_stride, filter, out, ws, ws_bytes);
+}
+
+int tlt_sample_filter(void* stream, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const tlt_filter* filter,
+                      void* out_rows, int64_t out_stride, int32_t* out_kept, void* ws, size_t ws_bytes) {
+    if (!out_rows || out_stride < vocab || (out_rows == logits && out_stride != row_stride)) return TLT_EINVAL;
+    PickOut out;
+    out.rows = out_rows;
+    out.rows_stride = out_stride;
+    out.kept = out_kept;
+    return run_pick(stream, dtype, rows, rows_per_seq, vocab, logits, row_stride, filter, out, ws, ws_bytes);
+}
+
 int tlt_gemm_glu(void* stream, int M, int N, int K, const void* A, const void* Wg, const void* Wu, void* act) {
     if (M < 1 || N < 1 || K < 1 || !A || !Wg || !Wu || !act) return TLT_EINVAL;
     if (!gemm_glu_supported(TLT_BF16, M, N, K, A, Wg, Wu) || ((uintptr_t)act & 7) != 0) return TLT_ENOTIMPL;   // (8-byte stores)

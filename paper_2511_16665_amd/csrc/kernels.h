@@ -183,6 +183,55 @@ size_t kv8_attention_workspace_bytes(int B, int n, int n_q_heads, int n_kv_heads
 hipError_t kv8_attention(hipStream_t s, int dtype, const KV8Rows& rows, const KV8Layer& kv, const void* q, int64_t q_stride, void* out, int n_q_heads, void* ws,
                          size_t ws_bytes, int impl);
 
+// ---- pages.hip
+struct PageState {
+    int32_t *free_page = nullptr, *n_free = nullptr, *page_count = nullptr, *block_table = nullptr;
+    int64_t n_pages = 0;
+    int max_pages = 0, page_size = 16;
+};
+// B <= 4096; outputs may be null
+hipError_t pages_grow(hipStream_t s, int B, const PageState& pg, const int32_t* seq_len, const int32_t* n_new, const int32_t* depth, int max_rows,
+                      int32_t* row_start, int32_t* row_seq, int32_t* position, int64_t* slot, int32_t* granted);
+hipError_t pages_release(hipStream_t s, int B, const PageState& pg, const int32_t* keep_len);
+
+// ---- rope.hip
+struct RopeIn {
+    const void *qkv = nullptr, *bias = nullptr;
+    int64_t stride = 0;
+    const int32_t* position = nullptr;
+    const int64_t* slot = nullptr;
+    const double* freq = nullptr;
+    int rot_dim = 0, interleaved = 0;
+    float amplitude = 1.f;
+};
+struct RopeOut {
+    void *q = nullptr, *rows = nullptr;               // null: nowhere
+    int64_t q_stride = 0, rows_stride = 0;
+    void *k = nullptr, *v = nullptr;                  // one layer's pools [n_pages][n_kv][page_size][d], null: nowhere
+    uint8_t *k_exp = nullptr, *v_exp = nullptr;       // of an 8-bit cache
+    int64_t n_slots = 0;
+    int page_size = 16, n_kv = 0, d = 0;
+};
+hipError_t rope_write(hipStream_t s, int dtype, int rows, int n_q_heads, const RopeIn& in, const RopeOut& out);
+
+// ---- pick.hip
+struct PickFilter {   // per sequence, null: none
+    const float* temperature = nullptr;
+    const int32_t* top_k = nullptr;
+    const float *top_p = nullptr, *min_p = nullptr;
+};
+struct PickOut {
+    const uint32_t* u = nullptr;
+    int32_t *token = nullptr, *kept = nullptr;   // token: a draw; otherwise rows
+    float* logprob = nullptr;
+    void* rows = nullptr;
+    int64_t rows_stride = 0;
+};
+size_t pick_workspace_bytes(int rows, int vocab);
+// (hipErrorInvalidValue: ws_bytes is too small)
+hipError_t pick(hipStream_t s, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const PickFilter& filter,
+                const PickOut& out, void* ws, size_t ws_bytes);
+
 // ---- sample.hip
 // (scratch, may be null: 8-byte aligned device memory the call may use, M * 256 bytes at most, to spread few rows over the chip)
 hipError_t row_argmax(hipStream_t s, int M, int V, const float* logits, int32_t* out, void* scratch = nullptr,
