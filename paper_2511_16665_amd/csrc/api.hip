@@ -1358,7 +1358,7 @@ int tlt_rope_write(void* stream, int dtype, int rows, int n_q_heads, int n_kv_he
     return rope_write((hipStream_t)stream, dtype, rows, n_q_heads, in, out) == hipSuccess ? TLT_OK : TLT_EHIP;
 }
 
-constexpr int kMostVocab = 1 << 24;   // indices and counts of a row; its sum of weights stays below 2^56
+constexpr int kMostVocab = 1 << 20;   // a row's sum of weights stays below 2^53, where doubles are exact
 
 size_t tlt_sample_workspace_bytes(int rows, int vocab) {
     if (rows < 1 || rows >= (1 << 23) || vocab < 1 || vocab > kMostVocab) return 0;
