@@ -5,13 +5,14 @@
 // (cut, last below), and of that what weighs enough.  Equal logits have equal weights.
 //
 // A row is cut into segments, a workgroup each, and read two or three times:
-//   pick_max_k     the largest logit, and 256 to 1024 sample maxima, which show how far down the most likely few hundred tokens reach
+//   pick_max_k     the largest logit, and how far down the most likely few hundred tokens reach
 //   pick_weigh_k   all weights; the likely few hundred tokens go to a list, and weights go to a histogram over the distance to the largest logit where the list may not reach the
-//                  prefix's end.  The last workgroup of a row orders the list and finds that end, or the histogram's bin that holds it
+//                  prefix's end.  The last workgroup of a row finds that end in the list, or the histogram's bin that holds it
 //   pick_gather_k  only where the list did not reach: the tokens of that bin (or all down to it) go to a list, what is above is summed up
 //   pick_mask_k    for filtered rows
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "kernels.h"
@@ -22,11 +23,15 @@ typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512;
-constexpr int kSegsMost = 32, kSamples = 1024;
-constexpr int kBins = 512;
-constexpr int kList = 2048, kLocalList = 1024;   // entries of a row's list of likely tokens, and of what a segment may add
-constexpr int kGather = 8192;                    // entries of the second list
-constexpr int kBatchRows = 256;                  // rows of one round: their logits stay in the last-level cache between the readings
+constexpr int kSegsMost = 32;                        // (a power of two)
+constexpr int kBins = 512;                           // of a row's histogram
+constexpr int kFindBins = 256;                       // and of a search in a list
+constexpr int kList = 1024;                          // entries of a row's list of likely tokens
+constexpr int kGather = 8192;                        // entries of the second list
+constexpr int kSmall = 4096;                         // vocabularies up to here are one list
+constexpr int kGroups = 2;                           // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
+constexpr int kInFlight = 4;                         // 16-byte pieces a lane asks for at once
+constexpr int kBatchRows = 256;                      // rows of one round: their logits stay in the last-level cache between the readings
 constexpr u64 kNoEntry = ~0ull;
 
 // order of logits as whole numbers; -0 and +0 are equal
@@ -49,7 +54,8 @@ struct Asked {
     __device__ __forceinline__ bool by_p() const { return top_p < (1u << 31); }
     __device__ __forceinline__ bool prefix() const { return top_k > 0 || by_p(); }
 };
-__device__ __forceinline__ Asked asked_of(const PickFilter& f, int seq, int V) {
+// tokens: of the row, above -infinity
+__device__ __forceinline__ Asked asked_of(const PickFilter& f, int seq, int tokens) {
     Asked a{1.0, 0, 1u << 31, 0.0};
     const float tau = f.temperature ? f.temperature[seq] : 1.f;
     if (!(tau > 0.f)) {
@@ -57,7 +63,7 @@ __device__ __forceinline__ Asked asked_of(const PickFilter& f, int seq, int V) {
         return a;
     }
     a.tau = (double)tau;
-    if (f.top_k) a.top_k = f.top_k[seq] < V ? max(f.top_k[seq], 0) : 0;
+    if (f.top_k) a.top_k = f.top_k[seq] < tokens ? max(f.top_k[seq], 0) : 0;
     if (f.top_p) {
         const float p = f.top_p[seq];
         if (p < 1.f) a.top_p = (uint32_t)(fmax((double)p, 0.0) * 2147483648.0);
@@ -123,34 +129,98 @@ struct RowView {
     __device__ __forceinline__ RowView(const T* row_, int V_) : row(row_), V(V_), off((int)(((uintptr_t)row_ & 15) / sizeof(T))) {}
     __device__ __forceinline__ int pieces() const { return (V + off + VEC - 1) / VEC; }
     __device__ __forceinline__ int first(int c) const { return c * VEC - off; }   // index of piece c's first element
+    __device__ __forceinline__ bool inside(int c) const { return first(c) >= 0 && first(c) + VEC <= V; }
+    __device__ __forceinline__ u32x4_t raw(int c) const { return *(const u32x4_t*)(row + first(c)); }
+    static __device__ __forceinline__ void values(u32x4_t w, float (&x)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) x[e] = __uint_as_float(w[e]);
+            else x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4_t packed(const float (&x)[VEC]) {   // (values of T: exact)
+        u32x4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(x[e]);
+            else w[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xffff0000u);
+        }
+        return w;
+    }
     // elements outside the row are -infinity
     __device__ __forceinline__ void load(int c, float (&x)[VEC]) const {
-        const int j = first(c);
-        if (j >= 0 && j + VEC <= V) {
-            const u32x4_t w = *(const u32x4_t*)(row + j);
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-            }
+        if (inside(c)) {
+            values(raw(c), x);
         } else {
+            const int j = first(c);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[e] = j + e >= 0 && j + e < V ? to_float(row[j + e]) : -INFINITY;
         }
     }
+    // f(piece, values) for pieces `from`, from + step, .. below `end`, kInFlight of them loaded at once; pieces at `end` and behind it come as -infinity (f is called by whole
+    // waves, whose lanes hold consecutive pieces).
+    template <typename F>
+    __device__ __forceinline__ void each(int from, int step, int end, F f) const {
+        const int lane = threadIdx.x & 63;
+        for (int c = from; c - lane < end; c += kInFlight * step) {
+            u32x4_t w[kInFlight];
+            const int last = c - lane + (kInFlight - 1) * step + 63;   // of the wave
+            if (last < end && inside(c - lane) && inside(last)) {
+#pragma unroll
+                for (int u = 0; u < kInFlight; ++u) w[u] = raw(c + u * step);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kInFlight; ++u) {
+                    float x[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) x[e] = -INFINITY;
+                    if (c + u * step < end) load(c + u * step, x);
+                    w[u] = packed(x);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                float x[VEC];
+                values(w[u], x);
+                f(c + u * step, x);
+            }
+        }
+    }
 };
 
-// ---- sums over a workgroup
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// ---- sums over a workgroup of NT threads, or over one wave (NT = 64), which needs no barrier
+template <int NT>
+__device__ __forceinline__ void together() {
+    if constexpr (NT == 64) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
+// sum over the lanes up to this one: within rows of 16 lanes by shifts, then from row to row (data-parallel moves; a shuffle is a trip through LDS)
+__device__ __forceinline__ double wave_incl(double v) {
+    auto add = [&](auto ctrl, auto rows) {
+        const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        v += __hiloint2double(hi, lo);
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31
     return v;
 }
+__device__ __forceinline__ double lane_63(double v) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 63), __builtin_amdgcn_readlane(__double2loint(v), 63));
+}
+__device__ __forceinline__ double wave_sum_d(double v) { return lane_63(wave_incl(v)); }
 template <int NT>
 __device__ __forceinline__ double block_sum(double v, double* tmp) {
     v = wave_sum_d(v);
+    if constexpr (NT == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -162,47 +232,103 @@ __device__ __forceinline__ double block_sum(double v, double* tmp) {
 // sum over the threads before this one
 template <int NT>
 __device__ __forceinline__ double block_excl_d(double v, double* tmp) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double incl = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double up = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += up;
-    }
+    const double incl = wave_incl(v);
+    if constexpr (NT == 64) return incl - v;
+    const int wave = threadIdx.x >> 6;
     __syncthreads();
-    if (lane == 63) tmp[wave] = incl;
+    if ((threadIdx.x & 63) == 63) tmp[wave] = incl;
     __syncthreads();
     double base = 0.0;
-    for (int w = 0; w < wave; ++w) base += tmp[w];
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) base += w < wave ? tmp[w] : 0.0;
     return base + incl - v;
 }
 
-// a[0 .. n - 1] in ascending order; n a power of two
-template <int NT>
-__device__ void sort_entries(u64* a, int n) {
-    for (int k = 2; k <= n; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < n / 2; i += NT) {
-                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-                const u64 x = a[lo], y = a[hi];
-                if ((x > y) == ((lo & k) == 0)) a[lo] = y, a[hi] = x;
+// ---- tokens in a list in LDS: entry_of (kNoEntry: none) and weights
+struct TokenList {
+    const u64* e;
+    const double* w;
+    int n;
+    __device__ __forceinline__ double weight(int i) const { return w[i]; }
+};
+struct FindLds {
+    u64 bins[kFindBins], order[256];
+    double value[256], base;
+    u64 found;
+    uint32_t n;
+    int bin;
+};
+// The first of the list's active tokens, in ascending order of `order` (all different, within lo .. hi), with which the running sum of `value` (whole numbers) reaches `aim`;
+// kNoEntry: none.  Bins over lo .. hi, then over the bin in which it happens, until that holds few tokens, which are compared with each other.
+template <int NT, typename O, typename A, typename F>
+__device__ u64 locate(int n, O order, A active, F value, double aim, u64 lo, u64 hi, FindLds& s, double* tmp) {
+    const int tid = threadIdx.x;
+    constexpr int B = NT < kFindBins ? kFindBins / NT : 1;
+    double base = 0.0;
+    for (;;) {
+        const double per = (double)kFindBins / ((double)(hi - lo) + 1.0) * (1.0 - 0x1p-40);
+        auto bin = [&](u64 o) { return (int)((double)(o - lo) * per); };
+        for (int i = tid; i < kFindBins; i += NT) s.bins[i] = 0;
+        if (tid == 0) s.n = 0, s.found = kNoEntry, s.bin = -1;
+        together<NT>();
+        for (int i = tid; i < n; i += NT) {
+            const u64 o = order(i);
+            if (o >= lo && o <= hi && active(i)) atomicAdd(&s.bins[bin(o)], (u64)__double_as_longlong(value(i) + 0x1p52) & 0xfffffffffffffull);
+        }
+        together<NT>();
+        double mine[B], sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < B; ++k) mine[k] = tid * B + k < kFindBins ? (double)s.bins[tid * B + k] : 0.0, sum += mine[k];
+        double run = base + block_excl_d<NT>(sum, tmp);
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            if (run < aim && aim <= run + mine[k]) s.bin = tid * B + k, s.base = run;
+            run += mine[k];
+        }
+        together<NT>();
+        const int at = s.bin;
+        if (at < 0) return kNoEntry;   // (uniform)
+        base = s.base;
+        for (int i = tid; i < n; i += NT) {
+            const u64 o = order(i);
+            if (o >= lo && o <= hi && active(i) && bin(o) == at) {
+                const uint32_t m = atomicAdd(&s.n, 1u);
+                if (m < 256) s.order[m] = o, s.value[m] = value(i);
             }
         }
-    __syncthreads();
-}
-__device__ __forceinline__ int power_above(int n) {
-    int p = 1;
-    while (p < n) p <<= 1;
-    return p;
+        together<NT>();
+        const uint32_t m = s.n;
+        if (m <= 256) {
+            for (uint32_t i = tid; i < m; i += NT) {
+                const u64 mine_at = s.order[i];
+                double before = base;
+                for (uint32_t j = 0; j < m; ++j) before += s.order[j] < mine_at ? s.value[j] : 0.0;
+                if (before < aim && aim <= before + s.value[i]) s.found = mine_at;
+            }
+            together<NT>();
+            const u64 found = s.found;
+            together<NT>();
+            return found;
+        }
+        // the range of the bin's tokens
+        if (tid == 0) s.order[0] = kNoEntry, s.order[1] = 0;
+        together<NT>();
+        for (int i = tid; i < n; i += NT) {
+            const u64 o = order(i);
+            if (o >= lo && o <= hi && active(i) && bin(o) == at) atomicMin(&s.order[0], o), atomicMax(&s.order[1], o);
+        }
+        together<NT>();
+        lo = s.order[0], hi = s.order[1];
+        together<NT>();
+    }
 }
 
 // ---- what the workgroups of a row share
-enum { kOpen = 0, kDone = 1, kBinAlone = 2, kAllDownTo = 3, kStepwise = 4 };
+enum { kOpen = 0, kDone = 1, kBinAlone = 2, kBinAloneN = 3, kAllDownTo = 4, kStepwise = 5 };
 struct PickRow {
     uint32_t list_n, gather_n, seen_weigh, seen_gather;
     int32_t state;
-    int32_t bin;                // kBinAlone: the bin that holds the end; kAllDownTo: the last one to take
+    int32_t bin;                // kBinAlone (by weight), kBinAloneN (by number): the bin that holds the end; kAllDownTo: the last one to take
     uint32_t cut;               // the result: kept are keys above it and those equal to it up to index `last`; 0: the row is copied
     int32_t last;
     double before_w, before_n;  // of the tokens above the gathered ones
@@ -210,7 +336,9 @@ struct PickRow {
 };
 struct PickWs {
     PickRow* row;
-    float *top, *sample;     // [rows][segs], [rows][samples]
+    float *top, *reach;      // [rows][segs], [rows][segs][kGroups]: the least of the largest logits of a segment's groups
+    uint32_t* groups;        // [rows][segs][kGroups]: how many of them have a token
+    uint32_t* tokens;        // [rows][segs]: tokens above -infinity
     double *whole, *part;    // [rows][segs], [rows][segs * 8]: sums of kept weights over the ranges of waves
     uint32_t* part_n;        // their counts
     u64 *list, *gather;      // [rows][kList], [rows][kGather]
@@ -218,9 +346,8 @@ struct PickWs {
     uint32_t* bin_n;
 };
 struct PickGeo {
-    int V, segs, pieces, per;   // pieces of a segment, and of a row at most
-    int samples;                // per segment
-    int rows_per_seq, row0;     // row0: first row of this round
+    int V, segs, per;         // per: pieces of a segment
+    int rows_per_seq, row0;   // row0: first row of this round
 };
 
 // The workgroup that is the last of `total` of a row to come here sees what all of them wrote (every wave waits for its stores, then one thread releases them).
@@ -248,11 +375,17 @@ __device__ __forceinline__ void put_nothing(const PickOut& out, int r, bool nan)
     if (out.logprob) out.logprob[2 * r] = out.logprob[2 * r + 1] = nan ? NAN : -INFINITY;
     if (out.kept) out.kept[r] = 0;
 }
-__device__ __forceinline__ void put_token(const PickOut& out, int r, const Weigh& w, int j, float x, double S, double whole) {
-    out.token[r] = j;
+// what a draw has found (in LDS), written out once
+struct Drawn {
+    double S;
+    int token;
+    float logit;
+};
+__device__ __forceinline__ void put_token(const PickOut& out, int r, const Weigh& w, const Drawn& d, double whole) {
+    out.token[r] = d.token;
     if (out.logprob) {
-        const double z = w.below(x);
-        out.logprob[2 * r] = (float)(z - log(S * 0x1p-32));
+        const double z = w.below(d.logit);
+        out.logprob[2 * r] = (float)(z - log(d.S * 0x1p-32));
         out.logprob[2 * r + 1] = (float)(z - log(whole * 0x1p-32));
     }
 }
@@ -263,13 +396,15 @@ struct Kept {
     double least;
     __device__ __forceinline__ bool operator()(const Weigh& w, int j, float x) const {
         const uint32_t k = key_of(x);
-        return (k > cut || (k == cut && j <= last)) && (least == 0.0 || w(x) >= least);
+        bool in = (k > cut) | ((k == cut) & (j <= last));
+        if (least != 0.0) in &= w(x) >= least;   // (the same for all lanes)
+        return in;
     }
 };
 
-// The first token of pieces [c0, c1) whose running sum, from `base` on, of kept weights exceeds `aim`; returns the sum over the pieces.
+// The first token of pieces [c0, c1) whose running sum, from `base` on, of kept weights exceeds what aim_of_sum gives for the sum over the pieces.
 template <int NT, typename T, typename F>
-__device__ double draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w, const Kept& kept, double base, F aim_of_sum, double* tmp, const PickOut& out, int r, double whole) {
+__device__ void draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w, const Kept& kept, double base, F aim_of_sum, double* tmp, Drawn* drawn) {
     constexpr int VEC = RowView<T>::VEC;
     const int per = (c1 - c0 + NT - 1) / NT, a = min(c1, c0 + (int)threadIdx.x * per), b = min(c1, a + per);
     double mine = 0.0;
@@ -277,8 +412,7 @@ __device__ double draw_from(const RowView<T>& row, int c0, int c1, const Weigh& 
         float x[VEC];
         row.load(c, x);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (kept(w, row.first(c) + e, x[e])) mine += w(x[e]);
+        for (int e = 0; e < VEC; ++e) mine += kept(w, row.first(c) + e, x[e]) ? w(x[e]) : 0.0;
     }
     const double all = block_sum<NT>(mine, tmp);
     double run = base + block_excl_d<NT>(mine, tmp), S;
@@ -290,109 +424,115 @@ __device__ double draw_from(const RowView<T>& row, int c0, int c1, const Weigh& 
             row.load(c, x);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                if (found || !kept(w, row.first(c) + e, x[e])) continue;
-                run += w(x[e]);
-                if (run > aim) {
-                    put_token(out, r, w, row.first(c) + e, x[e], S, whole);
-                    found = true;
-                }
+                const double add = !found && kept(w, row.first(c) + e, x[e]) ? w(x[e]) : 0.0;
+                run += add;
+                if (add > 0.0 && run > aim) drawn->S = S, drawn->token = row.first(c) + e, drawn->logit = x[e], found = true;
             }
         }
     }
-    return all;
+    __syncthreads();
 }
 
-// Where the prefix ends in an ordered list whose entries follow on before_n tokens of weight before_w: how many entries are in, or -1 if it ends behind them.
-// complete: no token above -infinity follows.  S: the weight that top_p is a share of, for rows without top_k.
-template <int NT>
-__device__ int end_in_list(const u64* a, int n, const Asked& ask, const Weigh& w, double before_w, double before_n, double S, bool complete, double* tmp, int* found) {
-    const double most = ask.top_k > 0 ? (double)ask.top_k - before_n : 1e18;
-    if (most > n && !complete && ask.top_k > 0) return -1;
-    const int nk = (int)fmin((double)n, most);
-    if (!ask.by_p()) return nk;
-    const int per = (nk + NT - 1) / NT, i0 = min(nk, (int)threadIdx.x * per), i1 = min(nk, i0 + per);
-    double mine = 0.0;
-    for (int i = i0; i < i1; ++i) mine += w(entry_logit(a[i]));
-    if (ask.top_k > 0) S = before_w + block_sum<NT>(mine, tmp);
-    const double aim = share_of(ask.top_p, S);
-    double run = before_w + block_excl_d<NT>(mine, tmp);
-    if (threadIdx.x == 0) *found = -1;
-    __syncthreads();
-    if (run < aim && aim <= run + mine)
-        for (int i = i0; i < i1; ++i) {
-            run += w(entry_logit(a[i]));
-            if (run >= aim) {
-                *found = i + 1;
-                break;
-            }
+// Where the prefix ends in a list whose tokens follow on before_n others of weight before_w: its last token, or kNoEntry if it ends behind them.  n of the list's entries are
+// tokens, between lo and hi.  S: the weight that top_p is a share of, for rows without top_k.
+template <int NT, typename L>
+__device__ u64 end_in_list(const L& l, int n, const Asked& ask, double before_w, double before_n, double S, u64 lo, u64 hi, FindLds& s, double* tmp) {
+    u64 end = kNoEntry - 1;   // (above every entry)
+    auto order = [&](int i) { return l.e[i]; };
+    if (ask.top_k > 0) {
+        const double aim = (double)ask.top_k - before_n;
+        if (aim > (double)n) return kNoEntry;
+        end = locate<NT>(l.n, order, [&](int) { return true; }, [](int) { return 1.0; }, aim, lo, hi, s, tmp);
+        if (ask.by_p()) {
+            double mine = 0.0;
+            for (int i = threadIdx.x; i < l.n; i += NT) mine += l.e[i] <= end ? l.weight(i) : 0.0;
+            S = before_w + block_sum<NT>(mine, tmp);
         }
-    __syncthreads();
-    return *found;
+    }
+    if (ask.by_p()) return locate<NT>(l.n, order, [&](int i) { return l.e[i] <= end; }, [&](int i) { return l.weight(i); }, share_of(ask.top_p, S) - before_w, lo, hi, s, tmp);
+    return end;
 }
 
-// Draws from the first n entries of an ordered list, which are all that is kept but for `least`.
-template <int NT>
-__device__ void draw_from_list(u64* a, int n, const Asked& ask, const Weigh& w, double* tmp, const PickOut& out, int r, double whole) {
-    // by index: entries too light, and those behind the end, go last
-    const int size = power_above(n);
+// Draws from the list's tokens up to `end`, which are all that is kept but for `least`.
+template <int NT, typename L>
+__device__ void draw_from_list(const L& l, u64 end, const Asked& ask, int V, FindLds& s, double* tmp, const PickOut& out, int r, Drawn* drawn) {
+    auto in = [&](int i) { return l.e[i] <= end && l.weight(i) >= ask.least; };
     double S = 0.0, count = 0.0;
-    for (int i = threadIdx.x; i < size; i += NT) {
-        u64 e = kNoEntry;
-        if (i < n) {
-            e = a[i];
-            const double x = w(entry_logit(e));
-            const bool in = ask.least == 0.0 || x >= ask.least;
-            S += in ? x : 0.0, count += in;
-            e = in ? e << 32 | e >> 32 : kNoEntry;
-        }
-        a[i] = e;
+    for (int i = threadIdx.x; i < l.n; i += NT) {
+        const bool k = in(i);
+        S += k ? l.weight(i) : 0.0, count += k;
     }
-    S = block_sum<NT>(S, tmp), count = block_sum<NT>(count, tmp);
+    S = block_sum<NT>(S, tmp);
+    count = block_sum<NT>(count, tmp);
     if (threadIdx.x == 0 && out.kept) out.kept[r] = (int32_t)count;
-    sort_entries<NT>(a, size);
-    const int m = (int)count, per = (m + NT - 1) / NT, i0 = min(m, (int)threadIdx.x * per), i1 = min(m, i0 + per);
-    auto logit = [&](u64 e) { return logit_of(~(uint32_t)e); };
-    double mine = 0.0;
-    for (int i = i0; i < i1; ++i) mine += w(logit(a[i]));
-    double run = block_excl_d<NT>(mine, tmp);
-    const double aim = aim_of(out.u[r], S);
-    if (run <= aim && aim < run + mine)
-        for (int i = i0; i < i1; ++i) {
-            run += w(logit(a[i]));
-            if (run > aim) {
-                put_token(out, r, w, (int)(a[i] >> 32), logit(a[i]), S, whole);
-                break;
-            }
-        }
+    const u64 token = locate<NT>(l.n, [&](int i) { return l.e[i] & 0xffffffffull; }, in, [&](int i) { return l.weight(i); }, aim_of(out.u[r], S) + 1.0, 0, (u64)(V - 1), s, tmp);
+    for (int i = threadIdx.x; i < l.n; i += NT)
+        if (in(i) && (l.e[i] & 0xffffffffull) == token) drawn->S = S, drawn->token = (int)token, drawn->logit = entry_logit(l.e[i]);
+    together<NT>();
 }
 
-// ---- the largest logit and the samples
+// The range of a wave, of those that a row's segments are cut into, in which the running sum of `part` passes aim (NT threads, at most one range each); -1: none.
+template <int NT>
+__device__ int range_of(double mine, double aim, double& base, FindLds& s, double* tmp) {
+    const double run = block_excl_d<NT>(mine, tmp);
+    if (threadIdx.x == 0) s.bin = -1;
+    __syncthreads();
+    if (run <= aim && aim < run + mine) s.bin = threadIdx.x, s.base = run;
+    __syncthreads();
+    base = s.base;
+    return s.bin;
+}
+
+// ---- the largest logit, and how far down the likely tokens reach: of 64 or 128 groups of a row's tokens each has one that is not below the least of the groups' largest, so at least so many
+// tokens reach that (some 300 or 620, if they are spread evenly).
 template <typename T>
 __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T* logits, int64_t row_stride, PickWs ws, PickOut out) {
-    constexpr int VEC = RowView<T>::VEC;
-    __shared__ float wave_top[kWeighThreads / 64];
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x;
+    constexpr int VEC = RowView<T>::VEC, NW = kWeighThreads / 64;
+    __shared__ float wave_top[NW], wave_reach[kGroups][NW];
+    __shared__ uint32_t wave_groups[kGroups][NW], wave_tokens[NW];
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, wave = tid >> 6;
     const RowView<T> row(logits + (int64_t)(geo.row0 + lr) * row_stride, geo.V);
-    const int c1 = min(row.pieces(), (g + 1) * geo.per);
     float top = -INFINITY;
     bool nan = false;
-    for (int c = g * geo.per + tid; c < c1; c += kWeighThreads) {
-        float x[VEC];
-        row.load(c, x);
+    uint32_t tokens = 0;
+    // (pieces of all parts of the row: where likely tokens have low indices, every group has its share of them)
+    row.each(g * kWeighThreads + tid, geo.segs * kWeighThreads, row.pieces(), [&](int, const float (&x)[VEC]) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) nan |= x[e] != x[e], top = fmaxf(top, x[e]);
-    }
-    const int lanes = kWeighThreads / geo.samples;   // that share a sample
+        for (int e = 0; e < VEC; ++e) nan |= x[e] != x[e], top = fmaxf(top, x[e]), tokens += x[e] > -INFINITY;
+    });
     float s = top;
-    for (int o = 1; o < lanes; o <<= 1) s = fmaxf(s, __shfl_xor(s, o, 64));
-    if (tid % lanes == 0) ws.sample[(int64_t)lr * kSamples + g * geo.samples + tid / lanes] = s;
+    int have = 1;   // lanes that share s
+#pragma unroll
+    for (int k = kGroups - 1; k >= 0; --k) {
+        const int lanes = min(64, kWeighThreads * geo.segs / (64 << k));   // (a power of two; 128 lanes are two waves, joined below)
+        for (; have < lanes; have <<= 1) s = fmaxf(s, __shfl_xor(s, have, 64));
+        const uint64_t full = __ballot(s > -INFINITY);
+        const float least = -wave_max(s > -INFINITY ? -s : -INFINITY);
+        if ((tid & 63) == 0) wave_reach[k][wave] = least, wave_groups[k][wave] = (uint32_t)(__popcll(full) / lanes);
+    }
     top = wave_max(top);
     if (__any(nan)) top = NAN;
-    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
+    tokens = (uint32_t)wave_sum_d((double)tokens);
+    if ((tid & 63) == 0) wave_top[wave] = top, wave_tokens[wave] = tokens;
     __syncthreads();
+    if (tid < kGroups) {
+        float least = INFINITY;
+        uint32_t n = 0;
+        const bool pairs = kWeighThreads * geo.segs / (64 << tid) > 64;
+        for (int v = 0; v < NW; v += pairs ? 2 : 1) {
+            float x = wave_reach[tid][v];
+            uint32_t m = wave_groups[tid][v];
+            if (pairs) x = wave_groups[tid][v + 1] == 0 ? x : (m == 0 ? wave_reach[tid][v + 1] : fmaxf(x, wave_reach[tid][v + 1])), m = max(m, wave_groups[tid][v + 1]);
+            if (m) least = fminf(least, x), n += m;
+        }
+        ws.reach[(lr * geo.segs + g) * kGroups + tid] = least, ws.groups[(lr * geo.segs + g) * kGroups + tid] = n;
+    }
     if (tid == 0) {
 #pragma unroll
-        for (int w = 0; w < kWeighThreads / 64; ++w) top = top != top || wave_top[w] != wave_top[w] ? NAN : fmaxf(top, wave_top[w]);
+        for (int v = 1; v < NW; ++v) tokens += wave_tokens[v];
+        ws.tokens[lr * geo.segs + g] = tokens;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) top = top != top || wave_top[v] != wave_top[v] ? NAN : fmaxf(top, wave_top[v]);
         ws.top[lr * geo.segs + g] = top;
         if (g == 0) {
             PickRow z{};
@@ -409,71 +549,41 @@ __device__ __forceinline__ float row_top(const PickGeo& geo, const PickWs& ws, i
     return __any(t != t) ? NAN : wave_max(t);
 }
 
-// A logit that at least `rank` of the row's samples, and so at least as many tokens, reach: from a histogram of the samples between the smallest and the largest.
-__device__ __forceinline__ float reached_by(int rank, int n, const float* sample, float top, uint32_t* bins, float* tmp) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    float lo = INFINITY;
-    for (int i = tid; i < n; i += kWeighThreads) {
-        const float s = sample[i];
-        if (s > -INFINITY) lo = fminf(lo, s);
-    }
-    lo = -wave_max(-lo);
-    for (int i = tid; i < 1024; i += kWeighThreads) bins[i] = 0;
-    if (lane == 0) tmp[wave] = lo;
-    __syncthreads();
-    lo = fminf(fminf(tmp[0], tmp[1]), fminf(tmp[2], tmp[3]));
-    const float width = (top - lo) / 1023.f, per = width > 0.f ? 1.f / width : 0.f;   // (infinite distances: every token is in)
-    for (int i = tid; i < n; i += kWeighThreads) {
-        const float s = sample[i];
-        if (s > -INFINITY) atomicAdd(&bins[min((int)fminf((top - s) * per, 1023.f), 1023)], 1u);
-    }
-    __syncthreads();
-    // the first bin down to which `rank` samples lie; all of them if there are fewer
-    uint32_t mine = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) mine += bins[4 * tid + k];
-    uint32_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t up = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += up;
-    }
-    uint32_t* sums = (uint32_t*)tmp + 8;
-    if (lane == 63) sums[wave] = incl;
-    if (tid == 0) sums[4] = 1024;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) incl += sums[w];
-    uint32_t run = incl - mine;
-    if (run < (uint32_t)rank && incl >= (uint32_t)rank)
-        for (int k = 0; k < 4; ++k) {
-            run += bins[4 * tid + k];
-            if (run >= (uint32_t)rank) {
-                sums[4] = 4 * tid + k;
-                break;
-            }
-        }
-    __syncthreads();
-    const int bin = (int)sums[4];
-    __syncthreads();
-    return bin >= 1023 ? -FLT_MAX : fmaxf(top - (float)(bin + 1) * width * 1.0001f, -FLT_MAX);
+__device__ __forceinline__ Asked asked_of_row(const PickGeo& geo, const PickWs& ws, int lr, const PickFilter& filter) {
+    const int lane = threadIdx.x & 63;
+    const float n = wave_sum(lane < geo.segs ? (float)ws.tokens[lr * geo.segs + lane] : 0.f);   // (2^20 at most: exact)
+    return asked_of(filter, (geo.row0 + lr) / geo.rows_per_seq, (int)n);
 }
 
-__device__ __forceinline__ int list_rank(const Asked& ask, int samples) {
-    const int want = ask.top_k > 0 ? max(ask.top_k + ask.top_k / 4, 64) : 256;
-    return min(want, samples * 3 / 4);
+// A logit that at least `rank` tokens reach, by the groups that fit what is asked for.
+__device__ __forceinline__ float reached(const PickGeo& geo, const PickWs& ws, int lr, const Asked& ask, int& rank) {
+    const int lane = threadIdx.x & 63, at = (lr * geo.segs + lane) * kGroups + (ask.top_k <= 64 ? 0 : 1);
+    const float least = lane < geo.segs ? ws.reach[at] : INFINITY;
+    rank = (int)wave_sum(lane < geo.segs ? (float)ws.groups[at] : 0.f);
+    return fmaxf(-wave_max(-least), -FLT_MAX);
 }
 
 // ---- weights, list, histogram
 template <typename T>
 __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kWeighThreads, NW = NT / 64;
-    __shared__ u64 buf[kList];          // first: histogram (weights, counts) and the segment's list; then the row's list
-    __shared__ double tmp[16];
+    __shared__ u64 local[kList];          // the segment's list, then the row's
+    __shared__ union {
+        struct {
+            u64 w[kBins];
+            uint32_t n[kBins];
+        } bin;                            // while the segment is read
+        struct {
+            FindLds find;
+            double w[kList];
+        } row;                            // then
+    } lds;
     __shared__ uint32_t local_n, base_n;
-    __shared__ int flag;
-    u64* bin_w = buf;
-    uint32_t* bin_n = (uint32_t*)(buf + kBins);
-    u64* local = buf + kBins + kBins / 2;
+    __shared__ double tmp[16];
+    __shared__ Drawn drawn;
+    __shared__ int flag, settled;
+    u64* bin_w = lds.bin.w;
+    uint32_t* bin_n = lds.bin.n;
     const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     PickRow* pr = ws.row + lr;
@@ -485,19 +595,13 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         }
         return;
     }
-    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);
+    const Asked ask = asked_of_row(geo, ws, lr, filter);
     const Weigh w(top, ask.tau);
     const bool prefix = ask.prefix();
-    const int n_samples = geo.samples * geo.segs;
     // tokens from `from` on go to the list
-    float from = INFINITY;
-    bool use_bins = false, count_bins = false;
-    if (prefix) {
-        const int rank = list_rank(ask, n_samples);
-        from = reached_by(rank, n_samples, ws.sample + (int64_t)lr * kSamples, top, (uint32_t*)buf, (float*)tmp);
-        count_bins = ask.top_k > rank;
-        use_bins = count_bins || ask.top_k == 0;
-    }
+    int rank = 0;
+    const float from = prefix ? reached(geo, ws, lr, ask, rank) : INFINITY;
+    const bool count_bins = ask.top_k > min(rank, 64), use_bins = prefix && (count_bins || ask.top_k == 0);
     const float per_logit = use_bins ? bins_per_logit(ask, geo.V) : 0.f;
     for (int i = tid; i < kBins; i += NT) bin_w[i] = 0, bin_n[i] = 0;
     if (tid == 0) local_n = 0;
@@ -506,13 +610,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     const int c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
     double whole = 0.0, kept = 0.0;
     uint32_t kept_n = 0;
-    for (int c = c0 + lane; c - lane < c1; c += 64) {   // (whole waves: the list is appended to together)
-        float x[VEC];
-        if (c < c1) row.load(c, x);
-        else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) x[e] = -INFINITY;
-        }
+    row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
         double weight[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -525,29 +623,17 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
                 const bool in = x[e] > -INFINITY && weight[e] >= ask.least;
                 kept += in ? weight[e] : 0.0, kept_n += in;
             }
-            continue;
+            return;
         }
         float best = x[0];
 #pragma unroll
         for (int e = 1; e < VEC; ++e) best = fmaxf(best, x[e]);
         if (__any(best >= from)) {
-            uint32_t n = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) n += x[e] >= from;
-            uint32_t at = n;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const uint32_t up = __shfl_up(at, o, 64);
-                if (lane >= o) at += up;
-            }
-            uint32_t start = 0;
-            if (lane == 63) start = atomicAdd(&local_n, at);
-            at += __shfl(start, 63, 64) - n;
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 if (x[e] >= from) {
-                    if (at < (uint32_t)kLocalList) local[at] = entry_of(x[e], row.first(c) + e);
-                    ++at;
+                    const uint32_t at = atomicAdd(&local_n, 1u);
+                    if (at < (uint32_t)kList) local[at] = entry_of(x[e], row.first(c) + e);
                 }
         }
         if (use_bins) {
@@ -560,7 +646,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
                 }
             }
         }
-    }
+    });
     whole = block_sum<NT>(whole, tmp);
     if (tid == 0) ws.whole[lr * geo.segs + g] = whole;
     if (!prefix) {
@@ -568,9 +654,9 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
         if (lane == 0) ws.part[(lr * geo.segs + g) * 8 + wave] = kept, ws.part_n[(lr * geo.segs + g) * 8 + wave] = kept_n;
     } else {
-        if (tid == 0) base_n = atomicAdd(&pr->list_n, local_n > (uint32_t)kLocalList ? 1u << 20 : local_n);
+        if (tid == 0) base_n = atomicAdd(&pr->list_n, local_n > (uint32_t)kList ? 1u << 20 : local_n);
         __syncthreads();
-        const uint32_t n = min(local_n, (uint32_t)kLocalList), base = base_n;
+        const uint32_t n = min(local_n, (uint32_t)kList), base = base_n;
         for (uint32_t i = tid; i < n; i += NT)
             if (base + i < (uint32_t)kList) ws.list[(int64_t)lr * kList + base + i] = local[i];
         if (use_bins)
@@ -582,56 +668,56 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     if (!last_here(&pr->seen_weigh, geo.segs, &flag)) return;
 
     // ---- the row's last workgroup
-    whole = 0.0;
-    for (int i = 0; i < geo.segs; ++i) whole += ws.whole[lr * geo.segs + i];
+    whole = wave_sum_d(lane < geo.segs ? ws.whole[lr * geo.segs + lane] : 0.0);
     if (tid == 0) pr->whole = whole;
+    FindLds& find = lds.row.find;
     if (!prefix) {
         if (tid == 0) pr->state = kDone, pr->cut = kKeyNothing, pr->last = -1;
         if (!out.token) return;
         // the wave's range that holds the draw
-        const int ranges = geo.segs * 8;
-        double S = 0.0, count = 0.0;
-        for (int i = 0; i < ranges; ++i)
-            if ((i & 7) < NW) S += ws.part[lr * ranges + i], count += ws.part_n[lr * ranges + i];
-        const double aim = aim_of(out.u[r], S);
-        double base = 0.0;
-        int at = -1;
-        for (int i = 0; i < ranges && at < 0; ++i) {
-            if ((i & 7) >= NW) continue;
-            const double add = ws.part[lr * ranges + i];
-            if (base + add > aim) at = i;
-            else base += add;
-        }
+        static_assert(kSegsMost * 8 <= NT, "a range per thread");
+        const bool is = tid < geo.segs * 8 && (tid & 7) < NW;
+        const double mine = is ? ws.part[lr * geo.segs * 8 + tid] : 0.0;
+        const double S = block_sum<NT>(mine, tmp), count = block_sum<NT>(is ? (double)ws.part_n[lr * geo.segs * 8 + tid] : 0.0, tmp);
         if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
+        const double aim = aim_of(out.u[r], S);
+        double base;
+        const int at = range_of<NT>(mine, aim, base, find, tmp);
         if (at < 0) return;   // (cannot be: S is the sum of the parts)
         const int end = min(row.pieces(), ((at >> 3) + 1) * geo.per), p0 = min(end, (at >> 3) * geo.per + (at & 7) * wper), p1 = min(end, p0 + wper);
-        const Kept in{kKeyNothing, -1, ask.least};
-        draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, out, r, whole);
+        draw_from<NT>(row, p0, p1, w, Kept{kKeyNothing, -1, ask.least}, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
+        if (tid == 0) put_token(out, r, w, drawn, whole);
         return;
     }
+    // the list, by one wave: no barriers
     const uint32_t n = pr->list_n;
-    int end = -1;
-    if (n <= (uint32_t)kList) {
-        const int size = power_above((int)n);
-        for (int i = tid; i < size; i += NT) buf[i] = i < (int)n ? ws.list[(int64_t)lr * kList + i] : kNoEntry;
-        sort_entries<NT>(buf, size);
-        end = end_in_list<NT>(buf, (int)n, ask, w, 0.0, 0.0, whole, from == -FLT_MAX, tmp, &flag);
-    }
-    if (end > 0) {
-        if (tid == 0) {
-            const u64 e = buf[end - 1];
-            pr->state = kDone, pr->cut = ~(uint32_t)(e >> 32), pr->last = (int32_t)(uint32_t)e;
+    if (wave == 0) {
+        u64 end = kNoEntry;
+        if (n <= (uint32_t)kList) {
+            for (uint32_t i = lane; i < n; i += 64) {
+                const u64 e = ws.list[(int64_t)lr * kList + i];
+                local[i] = e, lds.row.w[i] = w(entry_logit(e));
+            }
+            together<64>();
+            const TokenList l{local, lds.row.w, (int)n};
+            end = end_in_list<64>(l, (int)n, ask, 0.0, 0.0, whole, entry_of(top, 0), entry_of(from, -1), find, tmp);
+            if (end != kNoEntry) {
+                if (lane == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
+                if (out.token) {
+                    draw_from_list<64>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
+                    if (lane == 0) put_token(out, r, w, drawn, whole);
+                }
+            }
         }
-        __syncthreads();
-        if (out.token) draw_from_list<NT>(buf, end, ask, w, tmp, out, r, whole);
-        return;
+        if (lane == 0) settled = end != kNoEntry;
     }
+    __syncthreads();
+    if (settled) return;
     if (!use_bins) {
         if (tid == 0) pr->state = kStepwise;
         return;
     }
     // the bin that holds the end: thread t owns bins 2t and 2t + 1
-    __syncthreads();
     u64 bw[2] = {0, 0};
     uint32_t bn[2] = {0, 0};
     for (int i = 0; i < geo.segs; ++i) {
@@ -639,8 +725,10 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         bw[0] += ws.bin_w[at], bw[1] += ws.bin_w[at + 1];
         if (count_bins) bn[0] += ws.bin_n[at], bn[1] += ws.bin_n[at + 1];
     }
-    const double aim = count_bins ? (double)ask.top_k : share_of(ask.top_p, whole);
-    const double m0 = count_bins ? (double)bn[0] : (double)bw[0], m1 = count_bins ? (double)bn[1] : (double)bw[1];
+    // by numbers, unless top_k's tokens are more than the bins': then they hold all of the weight, and top_p decides alone
+    const bool by_n = count_bins && !(ask.by_p() && block_sum<NT>((double)bn[0] + (double)bn[1], tmp) < (double)ask.top_k);
+    const double aim = by_n ? (double)ask.top_k : share_of(ask.top_p, whole);
+    const double m0 = by_n ? (double)bn[0] : (double)bw[0], m1 = by_n ? (double)bn[1] : (double)bw[1];
     const double run = block_excl_d<NT>(m0 + m1, tmp);
     if (tid == 0) pr->state = kStepwise;   // (unless a bin is found)
     __syncthreads();
@@ -648,9 +736,9 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         const bool second = run + m0 < aim;
         const double before = second ? run + m0 : run;
         pr->bin = 2 * tid + second;
-        pr->before_w = count_bins ? 0.0 : before, pr->before_n = count_bins ? before : 0.0;
+        pr->before_w = by_n ? 0.0 : before, pr->before_n = by_n ? before : 0.0;
         // one limit: the bin's own tokens are enough.  Two: all tokens down to it, if a list holds them
-        if (!count_bins || !ask.by_p()) pr->state = kBinAlone;
+        if (!by_n || !ask.by_p()) pr->state = by_n ? kBinAloneN : kBinAlone;
         else if (before + (second ? m1 : m0) <= (double)kGather) pr->state = kAllDownTo, pr->before_n = 0.0;
     }
 }
@@ -751,31 +839,41 @@ __device__ void cut_stepwise(const RowView<T>& row, const Asked& ask, const Weig
     __syncthreads();
 }
 
-// ---- the second list
+// ---- the second list, whose weights are formed when they are asked for: with them in LDS there would be one workgroup on a CU
+struct LongTokenList {
+    const u64* e;
+    const Weigh& w;
+    int n;
+    __device__ __forceinline__ double weight(int i) const { return w(entry_logit(e[i])); }
+};
 template <typename T>
 __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kGatherThreads, NW = NT / 64;
-    __shared__ u64 buf[kGather];
+    __shared__ u64 local[kGather];        // the segment's list, then the row's
+    __shared__ FindLds find;
+    __shared__ Drawn drawn;
     __shared__ double tmp[16], part[kSegsMost * 8];
+    __shared__ uint32_t local_n, base_n;
     __shared__ int flag;
     const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
     PickRow* pr = ws.row + lr;
     const int state = pr->state;
     if (state == kDone || (state == kStepwise && g != 0)) return;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
-    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);
-    const Weigh w(row_top(geo, ws, lr), ask.tau);
+    Asked ask = asked_of_row(geo, ws, lr, filter);
+    const float top = row_top(geo, ws, lr);
+    const Weigh w(top, ask.tau);
     const double whole = pr->whole;
     const int wper = (geo.per + NW - 1) / NW, ranges = geo.segs * 8;
     if (state != kStepwise) {
         const float per_logit = bins_per_logit(ask, geo.V);
-        const int hi = pr->bin, lo = state == kBinAlone ? hi : 0;
+        const int hi = pr->bin, lo = state == kAllDownTo ? 0 : hi;
         const int seg_end = min(row.pieces(), (g + 1) * geo.per), c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
         double kept = 0.0;
         uint32_t kept_n = 0;
-        for (int c = c0 + lane; c < c1; c += 64) {
-            float x[VEC];
-            row.load(c, x);
+        if (tid == 0) local_n = 0;
+        __syncthreads();
+        row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int b = bin_of(w, x[e], per_logit);
@@ -786,62 +884,73 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
                         kept += in ? weight : 0.0, kept_n += in;
                     }
                 } else if (b <= hi && x[e] > -INFINITY) {
-                    const uint32_t at = atomicAdd(&pr->gather_n, 1u);
-                    if (at < (uint32_t)kGather) ws.gather[(int64_t)lr * kGather + at] = entry_of(x[e], row.first(c) + e);
+                    const uint32_t at = atomicAdd(&local_n, 1u);
+                    if (at < (uint32_t)kGather) local[at] = entry_of(x[e], row.first(c) + e);
                 }
             }
-        }
+        });
         kept = wave_sum_d(kept);
         for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
         if (lane == 0) ws.part[lr * ranges + g * 8 + wave] = kept, ws.part_n[lr * ranges + g * 8 + wave] = kept_n;
+        __syncthreads();
+        if (tid == 0) base_n = atomicAdd(&pr->gather_n, local_n > (uint32_t)kGather ? 1u << 20 : local_n);
+        __syncthreads();
+        const uint32_t mine_n = min(local_n, (uint32_t)kGather), at = base_n;
+        for (uint32_t i = tid; i < mine_n; i += NT)
+            if (at + i < (uint32_t)kGather) ws.gather[(int64_t)lr * kGather + at + i] = local[i];
         if (!last_here(&pr->seen_gather, geo.segs, &flag)) return;
         const uint32_t n = pr->gather_n;
-        int end = -1;
         if (n <= (uint32_t)kGather) {
-            const int size = power_above((int)n);
-            for (int i = tid; i < size; i += NT) buf[i] = i < (int)n ? ws.gather[(int64_t)lr * kGather + i] : kNoEntry;
-            sort_entries<NT>(buf, size);
-            end = end_in_list<NT>(buf, (int)n, ask, w, pr->before_w, pr->before_n, whole, false, tmp, &flag);
-        }
-        if (end > 0) {
-            const u64 e = buf[end - 1];
-            const Kept in{~(uint32_t)(e >> 32), (int)(uint32_t)e, ask.least};
-            if (tid == 0) pr->cut = in.cut, pr->last = in.last;
+            if (tid == 0) find.bins[0] = kNoEntry, find.bins[1] = 0;
             __syncthreads();
-            if (!out.token) return;
-            if (state == kAllDownTo) {
-                draw_from_list<NT>(buf, end, ask, w, tmp, out, r, whole);
+            for (uint32_t i = tid; i < n; i += NT) {
+                const u64 e = ws.gather[(int64_t)lr * kGather + i];
+                local[i] = e;
+                atomicMin(&find.bins[0], e), atomicMax(&find.bins[1], e);
+            }
+            __syncthreads();
+            const u64 first = find.bins[0], last = find.bins[1];
+            __syncthreads();
+            const LongTokenList l{local, w, (int)n};
+            if (state == kBinAlone) ask.top_k = 0;       // (the other limit is behind it)
+            if (state == kBinAloneN) ask.top_p = 1u << 31;
+            const u64 end = end_in_list<NT>(l, (int)n, ask, pr->before_w, pr->before_n, whole, first, last, find, tmp);
+            if (end != kNoEntry) {
+                const Kept in{~(uint32_t)(end >> 32), (int)(uint32_t)end, ask.least};
+                if (tid == 0) pr->cut = in.cut, pr->last = in.last;
+                if (!out.token) return;
+                if (state == kAllDownTo) {
+                    draw_from_list<NT>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
+                    if (tid == 0) put_token(out, r, w, drawn, whole);
+                    return;
+                }
+                // the listed ones join the sums of their ranges
+                static_assert(kSegsMost * 8 <= NT, "a range per thread");
+                if (tid < ranges) part[tid] = ws.part[lr * ranges + tid];
+                double count = tid < ranges ? (double)ws.part_n[lr * ranges + tid] : 0.0;
+                __syncthreads();
+                for (uint32_t i = tid; i < n; i += NT)
+                    if (local[i] <= end && l.weight(i) >= ask.least) {
+                        const int c = ((int)(uint32_t)local[i] + row.off) / VEC, seg = c / geo.per;
+                        atomicAdd(&part[seg * 8 + (c - seg * geo.per) / wper], l.weight(i));
+                        count += 1.0;
+                    }
+                count = block_sum<NT>(count, tmp);
+                if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
+                const double mine = tid < ranges ? part[tid] : 0.0, S = block_sum<NT>(mine, tmp), aim = aim_of(out.u[r], S);
+                double base;
+                const int range = range_of<NT>(mine, aim, base, find, tmp);
+                if (range < 0) return;   // (cannot be)
+                const int stop = min(row.pieces(), ((range >> 3) + 1) * geo.per), p0 = min(stop, (range >> 3) * geo.per + (range & 7) * wper), p1 = min(stop, p0 + wper);
+                draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
+                if (tid == 0) put_token(out, r, w, drawn, whole);
                 return;
             }
-            // the listed ones join the sums of their ranges
-            for (int i = tid; i < ranges; i += NT) part[i] = ws.part[lr * ranges + i];
-            double count = 0.0;
-            for (int i = tid; i < ranges; i += NT) count += ws.part_n[lr * ranges + i];
-            __syncthreads();
-            for (int i = tid; i < end; i += NT) {
-                const double x = w(entry_logit(buf[i]));
-                if (x < ask.least) continue;
-                const int c = ((int)(uint32_t)buf[i] + row.off) / VEC, seg = c / geo.per;
-                atomicAdd(&part[seg * 8 + (c - seg * geo.per) / wper], x);
-                count += 1.0;
-            }
-            count = block_sum<NT>(count, tmp);
-            if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
-            double S = 0.0, base = 0.0;
-            for (int i = 0; i < ranges; ++i) S += part[i];
-            const double aim = aim_of(out.u[r], S);
-            int at = -1;
-            for (int i = 0; i < ranges && at < 0; ++i) {
-                if (base + part[i] > aim) at = i;
-                else base += part[i];
-            }
-            if (at < 0) return;   // (cannot be)
-            const int stop = min(row.pieces(), ((at >> 3) + 1) * geo.per), p0 = min(stop, (at >> 3) * geo.per + (at & 7) * wper), p1 = min(stop, p0 + wper);
-            draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, out, r, whole);
-            return;
         }
+        ask = asked_of_row(geo, ws, lr, filter);
         __syncthreads();
     }
+    u64* buf = local;
     Kept in{0, 0, ask.least};
     cut_stepwise<NT>(row, ask, w, buf, tmp, in.cut, in.last);
     if (tid == 0) pr->cut = in.cut, pr->last = in.last;
@@ -857,7 +966,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         count = block_sum<NT>(count, tmp);
         if (tid == 0) out.kept[r] = (int32_t)count;
     }
-    draw_from<NT>(row, 0, row.pieces(), w, in, 0.0, [&](double all, double& sum) { sum = all; return aim_of(out.u[r], all); }, tmp, out, r, whole);
+    draw_from<NT>(row, 0, row.pieces(), w, in, 0.0, [&](double all, double& sum) { sum = all; return aim_of(out.u[r], all); }, tmp, &drawn);
+    if (tid == 0) put_token(out, r, w, drawn, whole);
 }
 
 // ---- filtered rows
@@ -867,7 +977,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
     __shared__ double tmp[16];
     const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, r = geo.row0 + lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
-    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);
+    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);   // (its least weight)
     const PickRow& pr = ws.row[lr];
     const bool copy = pr.cut == 0;
     const Weigh w(row_top(geo, ws, lr), ask.tau);
@@ -876,44 +986,99 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
     const bool wide = ((uintptr_t)o & 15) == ((uintptr_t)row.row & 15);
     const int c1 = min(row.pieces(), (g + 1) * geo.per);
     uint32_t count = 0;
-    for (int c = g * geo.per + tid; c < c1; c += NT) {
-        float x[VEC];
-        row.load(c, x);
+    row.each(g * geo.per + tid, NT, c1, [&](int c, const float (&x)[VEC]) {
         const int j = row.first(c);
+        float y[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (!copy) {
-                const bool keep = x[e] > -INFINITY && in(w, j + e, x[e]);
-                count += keep;
-                if (!keep) x[e] = -INFINITY;
-            }
-        if (wide && j >= 0 && j + VEC <= geo.V) {
-            u32x4_t v;
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xffff0000u);   // (values of T: exact)
-            }
-            *(u32x4_t*)(o + j) = v;
+        for (int e = 0; e < VEC; ++e) {
+            const bool keep = in(w, j + e, x[e]);
+            count += keep & !copy & (x[e] > -INFINITY);
+            y[e] = (keep | copy) ? x[e] : -INFINITY;
+        }
+        if (c >= c1) return;
+        if (wide && row.inside(c)) {
+            *(u32x4_t*)(o + j) = RowView<T>::packed(y);
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                if (j + e >= 0 && j + e < geo.V) o[j + e] = from_float<T>(x[e]);
+                if (j + e >= 0 && j + e < geo.V) o[j + e] = from_float<T>(y[e]);
         }
-    }
+    });
     if (!out.kept) return;
     const double all = block_sum<NT>((double)count, tmp);
     if (tid == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
 }
 
+// ---- small vocabularies: a row is one list, and one workgroup does everything
+template <typename T>
+__global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
+    constexpr int NT = kGatherThreads;
+    __shared__ u64 entry[kSmall];
+    __shared__ double weight[kSmall], tmp[16];
+    __shared__ FindLds find;
+    __shared__ Drawn drawn;
+    const int r = blockIdx.x, tid = threadIdx.x;
+    const T* row = logits + (int64_t)r * row_stride;
+    T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
+    float top = -INFINITY;
+    bool nan = false;
+    double tokens = 0.0;
+    for (int j = tid; j < V; j += NT) {
+        const float x = to_float(row[j]);
+        const bool is = x > -INFINITY;
+        nan |= x != x, top = fmaxf(top, x), tokens += is;
+        entry[j] = is ? entry_of(x, j) : kNoEntry;
+    }
+    top = wave_max(top);
+    if (__any(nan)) top = NAN;
+    if ((tid & 63) == 0) tmp[tid >> 6] = (double)top;
+    __syncthreads();
+    top = (float)tmp[0];
+#pragma unroll
+    for (int v = 1; v < NT / 64; ++v) top = top != top || tmp[v] != tmp[v] ? NAN : fmaxf(top, (float)tmp[v]);
+    if (top != top || top == -INFINITY) {   // (uniform)
+        if (o && o != row)
+            for (int j = tid; j < V; j += NT) o[j] = row[j];
+        if (tid == 0) put_nothing(out, r, top != top);
+        return;
+    }
+    tokens = block_sum<NT>(tokens, tmp);
+    const Asked ask = asked_of(filter, r / rows_per_seq, (int)tokens);
+    const Weigh w(top, ask.tau);
+    double whole = 0.0;
+    for (int j = tid; j < V; j += NT) {
+        const double x = entry[j] != kNoEntry ? w(entry_logit(entry[j])) : 0.0;
+        weight[j] = x, whole += x;
+    }
+    whole = block_sum<NT>(whole, tmp);   // (and all of both lists is there)
+    const TokenList l{entry, weight, V};
+    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, entry_of(top, 0), entry_of(-FLT_MAX, -1), find, tmp);
+    if (out.token) {
+        draw_from_list<NT>(l, end, ask, V, find, tmp, out, r, &drawn);
+        if (tid == 0) put_token(out, r, w, drawn, whole);
+        return;
+    }
+    double count = 0.0;
+    for (int j = tid; j < V; j += NT) {
+        const bool keep = entry[j] <= end && weight[j] >= ask.least;
+        count += keep;
+        const T x = row[j];
+        o[j] = keep ? x : from_float<T>(-INFINITY);
+    }
+    count = block_sum<NT>(count, tmp);
+    if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
+}
+
 // ---- host
 static int pick_segs(int rows, int vocab) {
-    // some 1024 workgroups, of 2048 tokens at least
-    return std::max(1, std::min({kSegsMost, 1024 / std::min(rows, kBatchRows), vocab / 2048}));
+    // some 1024 workgroups, of 4096 tokens at least (so that each of a segment's threads has some)
+    const int most = std::max(1, std::min(1024 / std::min(rows, kBatchRows), vocab / 4096));
+    int segs = 1;
+    while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
+    return segs;
 }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
+    if (vocab <= kSmall) return 256;
     const size_t R = (size_t)std::min(rows, kBatchRows), S = (size_t)pick_segs(rows, vocab);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -924,7 +1089,9 @@ static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
     PickWs w;
     w.row = (PickRow*)take(R * sizeof(PickRow));
     w.top = (float*)take(R * S * 4);
-    w.sample = (float*)take(R * kSamples * 4);
+    w.reach = (float*)take(R * S * kGroups * 4);
+    w.groups = (uint32_t*)take(R * S * kGroups * 4);
+    w.tokens = (uint32_t*)take(R * S * 4);
     w.whole = (double*)take(R * S * 8);
     w.part = (double*)take(R * S * 64);
     w.part_n = (uint32_t*)take(R * S * 32);
@@ -939,16 +1106,17 @@ size_t pick_workspace_bytes(int rows, int vocab) { return pick_carve(rows, vocab
 
 template <typename T>
 static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, const T* logits, int64_t row_stride, const PickFilter& filter, const PickOut& out, char* base) {
+    if (vocab <= kSmall) {
+        hipLaunchKernelGGL(pick_small_k<T>, dim3(rows), dim3(kGatherThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
+        return;
+    }
     PickWs ws;
     pick_carve(rows, vocab, base, &ws);
     PickGeo geo;
     geo.V = vocab;
     geo.segs = pick_segs(rows, vocab);
     constexpr int VEC = RowView<T>::VEC;
-    geo.pieces = (vocab + 2 * VEC - 2) / VEC;
-    geo.per = (geo.pieces + geo.segs - 1) / geo.segs;
-    geo.samples = kWeighThreads;
-    while (geo.samples * geo.segs > kSamples) geo.samples >>= 1;
+    geo.per = ((vocab + 2 * VEC - 2) / VEC + geo.segs - 1) / geo.segs;
     geo.rows_per_seq = rows_per_seq;
     for (int r0 = 0; r0 < rows; r0 += kBatchRows) {
         geo.row0 = r0;
