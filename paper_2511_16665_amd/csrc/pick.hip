@@ -25,11 +25,12 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 constexpr int kWeighThreads = 256, kGatherThreads = 512;
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
-constexpr int kFindBins = 256;                       // and of a search in a list
-constexpr int kList = 1024;                          // entries of a row's list of likely tokens
+constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
+constexpr int kList = 4096, kWaveList = 1024;        // entries of a row's list of likely tokens, and of what a wave may add (4096 in all: the row's list lies in their place)
 constexpr int kGather = 8192;                        // entries of the second list
 constexpr int kSmall = 4096;                         // vocabularies up to here are one list
-constexpr int kGroups = 2;                           // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
+// numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
+constexpr int kGroups = 3, kListed = 64 << (kGroups - 1);   // and the largest top_k that lists are made for
 constexpr int kInFlight = 4;                         // 16-byte pieces a lane asks for at once
 constexpr int kBatchRows = 256;                      // rows of one round: their logits stay in the last-level cache between the readings
 constexpr u64 kNoEntry = ~0ull;
@@ -56,22 +57,14 @@ struct Asked {
 };
 // tokens: of the row, above -infinity
 __device__ __forceinline__ Asked asked_of(const PickFilter& f, int seq, int tokens) {
-    Asked a{1.0, 0, 1u << 31, 0.0};
-    const float tau = f.temperature ? f.temperature[seq] : 1.f;
-    if (!(tau > 0.f)) {
-        a.top_k = 1;
-        return a;
-    }
+    const float tau = f.temperature ? f.temperature[seq] : 1.f, p = f.top_p ? f.top_p[seq] : 1.f, m = f.min_p ? f.min_p[seq] : 0.f;
+    const int k = f.top_k ? f.top_k[seq] : 0;
+    Asked a{1.0, 1, 1u << 31, 0.0};
+    if (!(tau > 0.f)) return a;
     a.tau = (double)tau;
-    if (f.top_k) a.top_k = f.top_k[seq] < tokens ? max(f.top_k[seq], 0) : 0;
-    if (f.top_p) {
-        const float p = f.top_p[seq];
-        if (p < 1.f) a.top_p = (uint32_t)(fmax((double)p, 0.0) * 2147483648.0);
-    }
-    if (f.min_p) {
-        const float m = f.min_p[seq];
-        if (m > 0.f) a.least = floor(fmin((double)m, 1.0) * 4294967296.0);
-    }
+    a.top_k = k < tokens ? max(k, 0) : 0;
+    if (p < 1.f) a.top_p = (uint32_t)(fmax((double)p, 0.0) * 2147483648.0);
+    if (m > 0.f) a.least = floor(fmin((double)m, 1.0) * 4294967296.0);
     return a;
 }
 // ceil(share * S / 2^31), at least 1
@@ -88,16 +81,17 @@ __device__ __forceinline__ double aim_of(uint32_t u, double S) { return (double)
 struct Weigh {
     double top, scale, tau;
     float top_f;
-    bool inf;   // the largest is +infinity: those tokens weigh 2^32, all others nothing
+    // (the largest is +infinity: 2^128 in its place, from which those tokens are cut to distance 0 and all others are far)
     __device__ __forceinline__ Weigh(float largest, double tau_) : tau(tau_) {
-        inf = largest == INFINITY;
-        top_f = inf ? 0.f : largest;
-        top = (double)top_f;
-        scale = 1.4426950408889634074 / tau_;
+        const bool inf = largest == INFINITY;
+        top_f = inf ? FLT_MAX : largest;
+        top = inf ? 0x1p128 : (double)largest;
+        scale = inf ? 1.0 : 1.4426950408889634074 / tau_;
     }
-    __device__ __forceinline__ float fix(float x) const { return inf ? (x == INFINITY ? 0.f : -INFINITY) : x; }
+    // how far below the largest, for bins: does not fall from a token to one with a smaller logit
+    __device__ __forceinline__ float distance(float x) const { return fmaxf(top_f - x, 0.f); }
     __device__ __forceinline__ double operator()(float x) const {
-        const double t = fmax(((double)fix(x) - top) * scale, -40.0);   // (-infinity, and what infinities leave undefined, weigh nothing)
+        const double t = fmin(fmax(((double)x - top) * scale, -40.0), 0.0);   // (-infinity, and what infinities leave undefined, weigh nothing)
         constexpr double kMagic = 6755399441055744.0 + 32.0;             // 1.5 * 2^52: the sum's low bits are n + 32
         const double s = t + kMagic;
         const double r = t - (s - kMagic);
@@ -116,7 +110,7 @@ struct Weigh {
         return floor(__hiloint2double(__double2hiint(p) + (n << 20), __double2loint(p)));
     }
     // l / tau - max / tau
-    __device__ __forceinline__ double below(float x) const { return fix(x) == top_f ? 0.0 : (double)fix(x) / tau - top / tau; }
+    __device__ __forceinline__ double below(float x) const { return (double)x >= top ? 0.0 : (double)x / tau - top / tau; }
     __device__ __forceinline__ u64 whole(double w) const { return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull; }
 };
 
@@ -158,23 +152,30 @@ struct RowView {
         }
     }
     // f(piece, values) for pieces `from`, from + step, .. below `end`, kInFlight of them loaded at once; pieces at `end` and behind it come as -infinity (f is called by whole
-    // waves, whose lanes hold consecutive pieces).
+    // waves, whose lanes hold consecutive pieces).  The row has a piece that lies inside.
     template <typename F>
     __device__ __forceinline__ void each(int from, int step, int end, F f) const {
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x & 63, in0 = off ? 1 : 0, in1 = (V + off) / VEC;   // pieces in0 .. in1 - 1 lie inside
         for (int c = from; c - lane < end; c += kInFlight * step) {
             u32x4_t w[kInFlight];
-            const int last = c - lane + (kInFlight - 1) * step + 63;   // of the wave
-            if (last < end && inside(c - lane) && inside(last)) {
 #pragma unroll
-                for (int u = 0; u < kInFlight; ++u) w[u] = raw(c + u * step);
-            } else {
+            for (int u = 0; u < kInFlight; ++u) w[u] = raw(min(max(c + u * step, in0), in1 - 1));
+            if (c - lane < in0 || c - lane + (kInFlight - 1) * step + 63 >= min(end, in1)) {   // (uniform over the wave)
+                const int behind = in1 * VEC < V + off ? in1 : -1;   // the piece behind the last whole one
+                u32x4_t part = {};
+                if (c == 0 && in0) w[0] = partly(0);
+                bool is = false;
+#pragma unroll
+                for (int u = 0; u < kInFlight; ++u) is |= c + u * step == behind;
+                if (is) part = partly(behind);
 #pragma unroll
                 for (int u = 0; u < kInFlight; ++u) {
+                    const int at = c + u * step;
+                    const bool in = at < end && (at < in1 || at == behind);
                     float x[VEC];
+                    values(at == behind ? part : w[u], x);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) x[e] = -INFINITY;
-                    if (c + u * step < end) load(c + u * step, x);
+                    for (int e = 0; e < VEC; ++e) x[e] = in ? x[e] : -INFINITY;
                     w[u] = packed(x);
                 }
             }
@@ -185,6 +186,12 @@ struct RowView {
                 f(c + u * step, x);
             }
         }
+    }
+    // a piece of which a part lies outside
+    __device__ __forceinline__ u32x4_t partly(int c) const {
+        float x[VEC];
+        load(c, x);
+        return packed(x);
     }
 };
 
@@ -251,29 +258,36 @@ struct TokenList {
     int n;
     __device__ __forceinline__ double weight(int i) const { return w[i]; }
 };
+// (weights formed when they are asked for: in LDS they would cost workgroups on a CU)
+struct LongTokenList {
+    const u64* e;
+    const Weigh& w;
+    int n;
+    __device__ __forceinline__ double weight(int i) const { return w(entry_logit(e[i])); }
+};
 struct FindLds {
-    u64 bins[kFindBins], order[256];
-    double value[256], base;
+    u64 bins[kFindBins], order[kFindFew];
+    double value[kFindFew], base;
     u64 found;
     uint32_t n;
     int bin;
 };
-// The first of the list's active tokens, in ascending order of `order` (all different, within lo .. hi), with which the running sum of `value` (whole numbers) reaches `aim`;
-// kNoEntry: none.  Bins over lo .. hi, then over the bin in which it happens, until that holds few tokens, which are compared with each other.
-template <int NT, typename O, typename A, typename F>
-__device__ u64 locate(int n, O order, A active, F value, double aim, u64 lo, u64 hi, FindLds& s, double* tmp) {
+// The first of the list's active tokens, in ascending order of `order` (all different), with which the running sum of `value` (whole numbers) reaches `aim`; kNoEntry: none.
+// Bins by `bin` (which does not fall in that order), then evenly over the orders of the bin in which it happens, until that holds few tokens, which are compared with each other.
+template <int NT, typename O, typename A, typename F, typename G>
+__device__ u64 locate(int n, O order, A active, F value, G bin, double aim, FindLds& s, double* tmp) {
     const int tid = threadIdx.x;
     constexpr int B = NT < kFindBins ? kFindBins / NT : 1;
-    double base = 0.0;
+    double base = 0.0, per = 0.0;
+    u64 lo = 0, hi = kNoEntry - 1;
+    auto bin_at = [&](int i, u64 o) { return per == 0.0 ? bin(i) : (int)((double)(o - lo) * per); };
     for (;;) {
-        const double per = (double)kFindBins / ((double)(hi - lo) + 1.0) * (1.0 - 0x1p-40);
-        auto bin = [&](u64 o) { return (int)((double)(o - lo) * per); };
         for (int i = tid; i < kFindBins; i += NT) s.bins[i] = 0;
         if (tid == 0) s.n = 0, s.found = kNoEntry, s.bin = -1;
         together<NT>();
         for (int i = tid; i < n; i += NT) {
             const u64 o = order(i);
-            if (o >= lo && o <= hi && active(i)) atomicAdd(&s.bins[bin(o)], (u64)__double_as_longlong(value(i) + 0x1p52) & 0xfffffffffffffull);
+            if (o >= lo && o <= hi && active(i)) atomicAdd(&s.bins[bin_at(i, o)], (u64)__double_as_longlong(value(i) + 0x1p52) & 0xfffffffffffffull);
         }
         together<NT>();
         double mine[B], sum = 0.0;
@@ -291,19 +305,20 @@ __device__ u64 locate(int n, O order, A active, F value, double aim, u64 lo, u64
         base = s.base;
         for (int i = tid; i < n; i += NT) {
             const u64 o = order(i);
-            if (o >= lo && o <= hi && active(i) && bin(o) == at) {
+            if (o >= lo && o <= hi && active(i) && bin_at(i, o) == at) {
                 const uint32_t m = atomicAdd(&s.n, 1u);
-                if (m < 256) s.order[m] = o, s.value[m] = value(i);
+                if (m < (uint32_t)kFindFew) s.order[m] = o, s.value[m] = value(i);
             }
         }
         together<NT>();
         const uint32_t m = s.n;
-        if (m <= 256) {
-            for (uint32_t i = tid; i < m; i += NT) {
-                const u64 mine_at = s.order[i];
+        if (m <= (uint32_t)kFindFew) {
+            if ((uint32_t)tid < m) {
+                const u64 mine_at = s.order[tid];
                 double before = base;
+#pragma unroll 4
                 for (uint32_t j = 0; j < m; ++j) before += s.order[j] < mine_at ? s.value[j] : 0.0;
-                if (before < aim && aim <= before + s.value[i]) s.found = mine_at;
+                if (before < aim && aim <= before + s.value[tid]) s.found = mine_at;
             }
             together<NT>();
             const u64 found = s.found;
@@ -313,25 +328,27 @@ __device__ u64 locate(int n, O order, A active, F value, double aim, u64 lo, u64
         // the range of the bin's tokens
         if (tid == 0) s.order[0] = kNoEntry, s.order[1] = 0;
         together<NT>();
+        u64 first = kNoEntry, last = 0;
         for (int i = tid; i < n; i += NT) {
             const u64 o = order(i);
-            if (o >= lo && o <= hi && active(i) && bin(o) == at) atomicMin(&s.order[0], o), atomicMax(&s.order[1], o);
+            if (o >= lo && o <= hi && active(i) && bin_at(i, o) == at) first = min(first, o), last = max(last, o);
         }
+        if (last) atomicMin(&s.order[0], first), atomicMax(&s.order[1], last);
         together<NT>();
         lo = s.order[0], hi = s.order[1];
+        per = (double)kFindBins / ((double)(hi - lo) + 1.0) * (1.0 - 0x1p-40);
         together<NT>();
     }
 }
 
 // ---- what the workgroups of a row share
-enum { kOpen = 0, kDone = 1, kBinAlone = 2, kBinAloneN = 3, kAllDownTo = 4, kStepwise = 5 };
+enum { kOpen = 0, kDone = 1, kByWeight = 2, kByNumber = 3, kAllDownTo = 4, kStepwise = 5 };
 struct PickRow {
     uint32_t list_n, gather_n, seen_weigh, seen_gather;
     int32_t state;
-    int32_t bin;                // kBinAlone (by weight), kBinAloneN (by number): the bin that holds the end; kAllDownTo: the last one to take
+    int32_t bin_lo, bin_hi;     // bins to gather: the one that the end lies in (kByWeight: of top_p; kByNumber: of top_k), or all down to it (kAllDownTo)
     uint32_t cut;               // the result: kept are keys above it and those equal to it up to index `last`; 0: the row is copied
     int32_t last;
-    double before_w, before_n;  // of the tokens above the gathered ones
     double whole;
 };
 struct PickWs {
@@ -342,8 +359,8 @@ struct PickWs {
     double *whole, *part;    // [rows][segs], [rows][segs * 8]: sums of kept weights over the ranges of waves
     uint32_t* part_n;        // their counts
     u64 *list, *gather;      // [rows][kList], [rows][kGather]
-    u64* bin_w;              // [rows][segs][kBins]
-    uint32_t* bin_n;
+    double* above;           // [rows][segs][2]: weight and number of the tokens above the gathered ones
+    u64* bins;               // [rows][segs][kBins]
 };
 struct PickGeo {
     int V, segs, per;         // per: pieces of a segment
@@ -367,7 +384,7 @@ __device__ __forceinline__ float bins_per_logit(const Asked& ask, int V) {
     if (ask.top_k == 0) reach = fmin(reach, 0.01 + log((double)V / fmax(1.0 - (double)ask.top_p * 0x1p-31, 1e-10)));
     return (float)fmin((double)kBins / (reach * ask.tau), 1e30);
 }
-__device__ __forceinline__ int bin_of(const Weigh& w, float x, float per_logit) { return (int)fminf((w.top_f - w.fix(x)) * per_logit, 1e6f); }
+__device__ __forceinline__ int bin_of(const Weigh& w, float x, float per_logit) { return (int)fminf(w.distance(x) * per_logit, 1e6f); }
 
 // ---- outputs
 __device__ __forceinline__ void put_nothing(const PickOut& out, int r, bool nan) {
@@ -434,22 +451,25 @@ __device__ void draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w,
 }
 
 // Where the prefix ends in a list whose tokens follow on before_n others of weight before_w: its last token, or kNoEntry if it ends behind them.  n of the list's entries are
-// tokens, between lo and hi.  S: the weight that top_p is a share of, for rows without top_k.
+// tokens, none below the logit `least`.  S: the weight that top_p is a share of, for rows without top_k.
 template <int NT, typename L>
-__device__ u64 end_in_list(const L& l, int n, const Asked& ask, double before_w, double before_n, double S, u64 lo, u64 hi, FindLds& s, double* tmp) {
+__device__ u64 end_in_list(const L& l, int n, const Asked& ask, double before_w, double before_n, double S, const Weigh& w, float least, FindLds& s, double* tmp) {
     u64 end = kNoEntry - 1;   // (above every entry)
     auto order = [&](int i) { return l.e[i]; };
+    // evenly over the distances to the largest logit
+    const float per = fminf((float)(kFindBins - 1) / w.distance(least), 1e30f);
+    auto bin = [&](int i) { return min((int)fminf(w.distance(entry_logit(l.e[i])) * per, 1e6f), kFindBins - 1); };
     if (ask.top_k > 0) {
         const double aim = (double)ask.top_k - before_n;
         if (aim > (double)n) return kNoEntry;
-        end = locate<NT>(l.n, order, [&](int) { return true; }, [](int) { return 1.0; }, aim, lo, hi, s, tmp);
+        end = locate<NT>(l.n, order, [](int) { return true; }, [](int) { return 1.0; }, bin, aim, s, tmp);
         if (ask.by_p()) {
             double mine = 0.0;
             for (int i = threadIdx.x; i < l.n; i += NT) mine += l.e[i] <= end ? l.weight(i) : 0.0;
             S = before_w + block_sum<NT>(mine, tmp);
         }
     }
-    if (ask.by_p()) return locate<NT>(l.n, order, [&](int i) { return l.e[i] <= end; }, [&](int i) { return l.weight(i); }, share_of(ask.top_p, S) - before_w, lo, hi, s, tmp);
+    if (ask.by_p()) return locate<NT>(l.n, order, [&](int i) { return l.e[i] <= end; }, [&](int i) { return l.weight(i); }, bin, share_of(ask.top_p, S) - before_w, s, tmp);
     return end;
 }
 
@@ -465,7 +485,9 @@ __device__ void draw_from_list(const L& l, u64 end, const Asked& ask, int V, Fin
     S = block_sum<NT>(S, tmp);
     count = block_sum<NT>(count, tmp);
     if (threadIdx.x == 0 && out.kept) out.kept[r] = (int32_t)count;
-    const u64 token = locate<NT>(l.n, [&](int i) { return l.e[i] & 0xffffffffull; }, in, [&](int i) { return l.weight(i); }, aim_of(out.u[r], S) + 1.0, 0, (u64)(V - 1), s, tmp);
+    const double per = (double)kFindBins / ((double)V + 1.0);
+    const u64 token = locate<NT>(l.n, [&](int i) { return l.e[i] & 0xffffffffull; }, in, [&](int i) { return l.weight(i); }, [&](int i) { return (int)((double)(uint32_t)l.e[i] * per); },
+                                 aim_of(out.u[r], S) + 1.0, s, tmp);
     for (int i = threadIdx.x; i < l.n; i += NT)
         if (in(i) && (l.e[i] & 0xffffffffull) == token) drawn->S = S, drawn->token = (int)token, drawn->logit = entry_logit(l.e[i]);
     together<NT>();
@@ -483,8 +505,8 @@ __device__ int range_of(double mine, double aim, double& base, FindLds& s, doubl
     return s.bin;
 }
 
-// ---- the largest logit, and how far down the likely tokens reach: of 64 or 128 groups of a row's tokens each has one that is not below the least of the groups' largest, so at least so many
-// tokens reach that (some 300 or 620, if they are spread evenly).
+// ---- the largest logit, and how far down the likely tokens reach: of 64, 128 or 256 groups of a row's tokens each has one that is not below the least of the groups' largest, so at least so many
+// tokens reach that (some 300, 620 or 1600, if they are spread evenly).
 template <typename T>
 __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T* logits, int64_t row_stride, PickWs ws, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NW = kWeighThreads / 64;
@@ -557,7 +579,7 @@ __device__ __forceinline__ Asked asked_of_row(const PickGeo& geo, const PickWs& 
 
 // A logit that at least `rank` tokens reach, by the groups that fit what is asked for.
 __device__ __forceinline__ float reached(const PickGeo& geo, const PickWs& ws, int lr, const Asked& ask, int& rank) {
-    const int lane = threadIdx.x & 63, at = (lr * geo.segs + lane) * kGroups + (ask.top_k <= 64 ? 0 : 1);
+    const int lane = threadIdx.x & 63, at = (lr * geo.segs + lane) * kGroups + (ask.top_k <= 64 ? 0 : ask.top_k <= 128 ? 1 : 2);
     const float least = lane < geo.segs ? ws.reach[at] : INFINITY;
     rank = (int)wave_sum(lane < geo.segs ? (float)ws.groups[at] : 0.f);
     return fmaxf(-wave_max(-least), -FLT_MAX);
@@ -569,21 +591,12 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     constexpr int VEC = RowView<T>::VEC, NT = kWeighThreads, NW = NT / 64;
     __shared__ u64 local[kList];          // the segment's list, then the row's
     __shared__ union {
-        struct {
-            u64 w[kBins];
-            uint32_t n[kBins];
-        } bin;                            // while the segment is read
-        struct {
-            FindLds find;
-            double w[kList];
-        } row;                            // then
+        u64 bins[kBins];                  // while the segment is read
+        FindLds find;                     // then
     } lds;
-    __shared__ uint32_t local_n, base_n;
     __shared__ double tmp[16];
     __shared__ Drawn drawn;
-    __shared__ int flag, settled;
-    u64* bin_w = lds.bin.w;
-    uint32_t* bin_n = lds.bin.n;
+    __shared__ int flag;
     const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     PickRow* pr = ws.row + lr;
@@ -600,22 +613,32 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     const bool prefix = ask.prefix();
     // tokens from `from` on go to the list
     int rank = 0;
-    const float from = prefix ? reached(geo, ws, lr, ask, rank) : INFINITY;
-    const bool count_bins = ask.top_k > min(rank, 64), use_bins = prefix && (count_bins || ask.top_k == 0);
+    float from = prefix ? reached(geo, ws, lr, ask, rank) : INFINITY;
+    const bool count_bins = ask.top_k > min(rank, kListed), use_bins = prefix && (count_bins || ask.top_k == 0);
+    if (count_bins) from = INFINITY;   // (no list reaches that far)
     const float per_logit = use_bins ? bins_per_logit(ask, geo.V) : 0.f;
-    for (int i = tid; i < kBins; i += NT) bin_w[i] = 0, bin_n[i] = 0;
-    if (tid == 0) local_n = 0;
+    const bool weigh_all = out.token ? !prefix || use_bins || out.logprob : use_bins;
+    if (!prefix && !weigh_all) {   // (a filtered row without a prefix: what it keeps is known)
+        if (g == 0 && tid == 0) pr->state = kDone, pr->cut = kKeyNothing, pr->last = -1;
+        return;
+    }
+    if (use_bins)
+        for (int i = tid; i < kBins; i += NT) lds.bins[i] = 0;
     __syncthreads();
     const int seg_end = min(row.pieces(), (g + 1) * geo.per), wper = (geo.per + NW - 1) / NW;
     const int c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
     double whole = 0.0, kept = 0.0;
     uint32_t kept_n = 0;
+    u64* listing = local + wave * kWaveList;   // the wave's own list: no counter is shared while the segment is read
+    uint32_t listed = 0;
     row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
         double weight[VEC];
+        if (weigh_all) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            weight[e] = w(x[e]);
-            whole += weight[e];
+            for (int e = 0; e < VEC; ++e) {
+                weight[e] = w(x[e]);
+                whole += weight[e];
+            }
         }
         if (!prefix) {
 #pragma unroll
@@ -630,20 +653,19 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         for (int e = 1; e < VEC; ++e) best = fmaxf(best, x[e]);
         if (__any(best >= from)) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (x[e] >= from) {
-                    const uint32_t at = atomicAdd(&local_n, 1u);
-                    if (at < (uint32_t)kList) local[at] = entry_of(x[e], row.first(c) + e);
-                }
+            for (int e = 0; e < VEC; ++e) {
+                const bool in = x[e] >= from;
+                const uint64_t all = __ballot(in);
+                const uint32_t at = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+                if (in && at < (uint32_t)kWaveList) listing[at] = entry_of(x[e], row.first(c) + e);
+                listed += (uint32_t)__popcll(all);
+            }
         }
         if (use_bins) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int b = bin_of(w, x[e], per_logit);
-                if (b < kBins) {
-                    atomicAdd(&bin_w[b], w.whole(weight[e]));
-                    if (count_bins) atomicAdd(&bin_n[b], 1u);
-                }
+                if (b < kBins) atomicAdd(&lds.bins[b], count_bins ? 1ull : w.whole(weight[e]));
             }
         }
     });
@@ -654,23 +676,22 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
         if (lane == 0) ws.part[(lr * geo.segs + g) * 8 + wave] = kept, ws.part_n[(lr * geo.segs + g) * 8 + wave] = kept_n;
     } else {
-        if (tid == 0) base_n = atomicAdd(&pr->list_n, local_n > (uint32_t)kList ? 1u << 20 : local_n);
-        __syncthreads();
-        const uint32_t n = min(local_n, (uint32_t)kList), base = base_n;
-        for (uint32_t i = tid; i < n; i += NT)
-            if (base + i < (uint32_t)kList) ws.list[(int64_t)lr * kList + base + i] = local[i];
+        uint32_t base = 0;
+        if (lane == 0) base = atomicAdd(&pr->list_n, listed > (uint32_t)kWaveList ? 1u << 20 : listed);
+        base = __builtin_amdgcn_readfirstlane(base);
+        listed = min(listed, (uint32_t)kWaveList);
+        for (uint32_t i = lane; i < listed; i += 64)
+            if (base + i < (uint32_t)kList) ws.list[(int64_t)lr * kList + base + i] = listing[i];
+        __syncthreads();   // (the bins)
         if (use_bins)
-            for (int i = tid; i < kBins; i += NT) {
-                ws.bin_w[((int64_t)lr * geo.segs + g) * kBins + i] = bin_w[i];
-                if (count_bins) ws.bin_n[((int64_t)lr * geo.segs + g) * kBins + i] = bin_n[i];
-            }
+            for (int i = tid; i < kBins; i += NT) ws.bins[((int64_t)lr * geo.segs + g) * kBins + i] = lds.bins[i];
     }
     if (!last_here(&pr->seen_weigh, geo.segs, &flag)) return;
 
     // ---- the row's last workgroup
     whole = wave_sum_d(lane < geo.segs ? ws.whole[lr * geo.segs + lane] : 0.0);
     if (tid == 0) pr->whole = whole;
-    FindLds& find = lds.row.find;
+    FindLds& find = lds.find;
     if (!prefix) {
         if (tid == 0) pr->state = kDone, pr->cut = kKeyNothing, pr->last = -1;
         if (!out.token) return;
@@ -689,57 +710,58 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         if (tid == 0) put_token(out, r, w, drawn, whole);
         return;
     }
-    // the list, by one wave: no barriers
     const uint32_t n = pr->list_n;
-    if (wave == 0) {
-        u64 end = kNoEntry;
-        if (n <= (uint32_t)kList) {
-            for (uint32_t i = lane; i < n; i += 64) {
-                const u64 e = ws.list[(int64_t)lr * kList + i];
-                local[i] = e, lds.row.w[i] = w(entry_logit(e));
+    if (n > 0 && n <= (uint32_t)kList) {
+#pragma unroll 4
+        for (uint32_t i = tid; i < n; i += NT) local[i] = ws.list[(int64_t)lr * kList + i];
+        __syncthreads();
+        const LongTokenList l{local, w, (int)n};
+        const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, w, from, find, tmp);
+        if (end != kNoEntry) {
+            if (tid == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
+            if (out.token) {
+                draw_from_list<NT>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
+                if (tid == 0) put_token(out, r, w, drawn, whole);
             }
-            together<64>();
-            const TokenList l{local, lds.row.w, (int)n};
-            end = end_in_list<64>(l, (int)n, ask, 0.0, 0.0, whole, entry_of(top, 0), entry_of(from, -1), find, tmp);
-            if (end != kNoEntry) {
-                if (lane == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
-                if (out.token) {
-                    draw_from_list<64>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
-                    if (lane == 0) put_token(out, r, w, drawn, whole);
-                }
-            }
+            return;
         }
-        if (lane == 0) settled = end != kNoEntry;
     }
-    __syncthreads();
-    if (settled) return;
     if (!use_bins) {
         if (tid == 0) pr->state = kStepwise;
         return;
     }
-    // the bin that holds the end: thread t owns bins 2t and 2t + 1
-    u64 bw[2] = {0, 0};
-    uint32_t bn[2] = {0, 0};
+    // The bin that the end lies in: thread t owns bins 2t and 2t + 1.
+    constexpr int OWN = kBins / NT;
+    u64 own[OWN] = {};
+#pragma unroll 8
     for (int i = 0; i < geo.segs; ++i) {
-        const int64_t at = ((int64_t)lr * geo.segs + i) * kBins + 2 * tid;
-        bw[0] += ws.bin_w[at], bw[1] += ws.bin_w[at + 1];
-        if (count_bins) bn[0] += ws.bin_n[at], bn[1] += ws.bin_n[at + 1];
+        const u64* from_seg = ws.bins + ((int64_t)lr * geo.segs + i) * kBins + OWN * tid;
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) own[k] += from_seg[k];
     }
-    // by numbers, unless top_k's tokens are more than the bins': then they hold all of the weight, and top_p decides alone
-    const bool by_n = count_bins && !(ask.by_p() && block_sum<NT>((double)bn[0] + (double)bn[1], tmp) < (double)ask.top_k);
-    const double aim = by_n ? (double)ask.top_k : share_of(ask.top_p, whole);
-    const double m0 = by_n ? (double)bn[0] : (double)bw[0], m1 = by_n ? (double)bn[1] : (double)bw[1];
-    const double run = block_excl_d<NT>(m0 + m1, tmp);
-    if (tid == 0) pr->state = kStepwise;   // (unless a bin is found)
+    double mine = 0.0;
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) mine += (double)own[k];
+    const double all = block_sum<NT>(mine, tmp), aim = count_bins ? (double)ask.top_k : share_of(ask.top_p, whole);
+    double run = block_excl_d<NT>(mine, tmp);
+    if (tid == 0) find.bin = -1;
     __syncthreads();
-    if (run < aim && aim <= run + m0 + m1) {
-        const bool second = run + m0 < aim;
-        const double before = second ? run + m0 : run;
-        pr->bin = 2 * tid + second;
-        pr->before_w = by_n ? 0.0 : before, pr->before_n = by_n ? before : 0.0;
-        // one limit: the bin's own tokens are enough.  Two: all tokens down to it, if a list holds them
-        if (!by_n || !ask.by_p()) pr->state = by_n ? kBinAloneN : kBinAlone;
-        else if (before + (second ? m1 : m0) <= (double)kGather) pr->state = kAllDownTo, pr->before_n = 0.0;
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+        if (run < aim && aim <= run + (double)own[k]) find.bin = OWN * tid + k, find.base = run + (double)own[k];
+        run += (double)own[k];
+    }
+    __syncthreads();
+    if (tid == 0) {
+        const bool found = find.bin >= 0;
+        int state = found ? (count_bins ? kByNumber : kByWeight) : kStepwise;
+        pr->bin_lo = pr->bin_hi = find.bin;
+        // two limits: all tokens down to the bin of the first, if a list holds them (all that weigh anything, if they are fewer than top_k)
+        if (count_bins && ask.by_p()) {
+            state = (found ? find.base : all) <= (double)kGather ? kAllDownTo : kStepwise;
+            pr->bin_lo = 0, pr->bin_hi = found ? find.bin : kBins - 1;
+        }
+        pr->state = state;
     }
 }
 
@@ -839,13 +861,7 @@ __device__ void cut_stepwise(const RowView<T>& row, const Asked& ask, const Weig
     __syncthreads();
 }
 
-// ---- the second list, whose weights are formed when they are asked for: with them in LDS there would be one workgroup on a CU
-struct LongTokenList {
-    const u64* e;
-    const Weigh& w;
-    int n;
-    __device__ __forceinline__ double weight(int i) const { return w(entry_logit(e[i])); }
-};
+// ---- the second list
 template <typename T>
 __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kGatherThreads, NW = NT / 64;
@@ -867,10 +883,10 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     const int wper = (geo.per + NW - 1) / NW, ranges = geo.segs * 8;
     if (state != kStepwise) {
         const float per_logit = bins_per_logit(ask, geo.V);
-        const int hi = pr->bin, lo = state == kAllDownTo ? 0 : hi;
+        const int lo = pr->bin_lo, hi = pr->bin_hi;
         const int seg_end = min(row.pieces(), (g + 1) * geo.per), c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
-        double kept = 0.0;
-        uint32_t kept_n = 0;
+        double kept = 0.0, above = 0.0;
+        uint32_t kept_n = 0, above_n = 0;
         if (tid == 0) local_n = 0;
         __syncthreads();
         row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
@@ -878,11 +894,10 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
             for (int e = 0; e < VEC; ++e) {
                 const int b = bin_of(w, x[e], per_logit);
                 if (b < lo) {
-                    if (out.token) {
-                        const double weight = w(x[e]);
-                        const bool in = weight >= ask.least;
-                        kept += in ? weight : 0.0, kept_n += in;
-                    }
+                    const double weight = w(x[e]);
+                    const bool in = weight >= ask.least;
+                    above += weight, ++above_n;
+                    kept += in ? weight : 0.0, kept_n += in;
                 } else if (b <= hi && x[e] > -INFINITY) {
                     const uint32_t at = atomicAdd(&local_n, 1u);
                     if (at < (uint32_t)kGather) local[at] = entry_of(x[e], row.first(c) + e);
@@ -892,6 +907,9 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         kept = wave_sum_d(kept);
         for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
         if (lane == 0) ws.part[lr * ranges + g * 8 + wave] = kept, ws.part_n[lr * ranges + g * 8 + wave] = kept_n;
+        above = block_sum<NT>(above, tmp);
+        const double n_above = block_sum<NT>((double)above_n, tmp);
+        if (tid == 0) ws.above[2 * (lr * geo.segs + g)] = above, ws.above[2 * (lr * geo.segs + g) + 1] = n_above;
         __syncthreads();
         if (tid == 0) base_n = atomicAdd(&pr->gather_n, local_n > (uint32_t)kGather ? 1u << 20 : local_n);
         __syncthreads();
@@ -900,21 +918,26 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
             if (at + i < (uint32_t)kGather) ws.gather[(int64_t)lr * kGather + at + i] = local[i];
         if (!last_here(&pr->seen_gather, geo.segs, &flag)) return;
         const uint32_t n = pr->gather_n;
-        if (n <= (uint32_t)kGather) {
-            if (tid == 0) find.bins[0] = kNoEntry, find.bins[1] = 0;
+        if (n > 0 && n <= (uint32_t)kGather) {
+            if (tid == 0) find.found = 0;
             __syncthreads();
+            u64 find_last = 0;
+#pragma unroll 4
             for (uint32_t i = tid; i < n; i += NT) {
                 const u64 e = ws.gather[(int64_t)lr * kGather + i];
                 local[i] = e;
-                atomicMin(&find.bins[0], e), atomicMax(&find.bins[1], e);
+                find_last = max(find_last, e);
             }
+            atomicMax(&find.found, find_last);
             __syncthreads();
-            const u64 first = find.bins[0], last = find.bins[1];
+            find_last = find.found;
             __syncthreads();
             const LongTokenList l{local, w, (int)n};
-            if (state == kBinAlone) ask.top_k = 0;       // (the other limit is behind it)
-            if (state == kBinAloneN) ask.top_p = 1u << 31;
-            const u64 end = end_in_list<NT>(l, (int)n, ask, pr->before_w, pr->before_n, whole, first, last, find, tmp);
+            if (state == kByNumber) ask.top_p = 1u << 31;
+            if (state == kAllDownTo && ask.top_k > (int)n) ask.top_k = 0;   // (tokens without weight fill it up)
+            const double before_w = wave_sum_d(lane < geo.segs ? ws.above[2 * (lr * geo.segs + lane)] : 0.0);
+            const double before_n = wave_sum_d(lane < geo.segs ? ws.above[2 * (lr * geo.segs + lane) + 1] : 0.0);
+            const u64 end = end_in_list<NT>(l, (int)n, ask, before_w, before_n, whole, w, entry_logit(find_last), find, tmp);
             if (end != kNoEntry) {
                 const Kept in{~(uint32_t)(end >> 32), (int)(uint32_t)end, ask.least};
                 if (tid == 0) pr->cut = in.cut, pr->last = in.last;
@@ -1020,13 +1043,14 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
     const int r = blockIdx.x, tid = threadIdx.x;
     const T* row = logits + (int64_t)r * row_stride;
     T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
-    float top = -INFINITY;
+    float top = -INFINITY, least = INFINITY;
     bool nan = false;
     double tokens = 0.0;
     for (int j = tid; j < V; j += NT) {
         const float x = to_float(row[j]);
         const bool is = x > -INFINITY;
         nan |= x != x, top = fmaxf(top, x), tokens += is;
+        if (is) least = fminf(least, x);
         entry[j] = is ? entry_of(x, j) : kNoEntry;
     }
     top = wave_max(top);
@@ -1043,6 +1067,12 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
         return;
     }
     tokens = block_sum<NT>(tokens, tmp);
+    least = -wave_max(-least);
+    __syncthreads();
+    if ((tid & 63) == 0) tmp[tid >> 6] = (double)least;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < NT / 64; ++v) least = fminf(least, (float)tmp[v]);
     const Asked ask = asked_of(filter, r / rows_per_seq, (int)tokens);
     const Weigh w(top, ask.tau);
     double whole = 0.0;
@@ -1052,7 +1082,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
     }
     whole = block_sum<NT>(whole, tmp);   // (and all of both lists is there)
     const TokenList l{entry, weight, V};
-    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, entry_of(top, 0), entry_of(-FLT_MAX, -1), find, tmp);
+    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, w, least, find, tmp);
     if (out.token) {
         draw_from_list<NT>(l, end, ask, V, find, tmp, out, r, &drawn);
         if (tid == 0) put_token(out, r, w, drawn, whole);
@@ -1097,8 +1127,8 @@ static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
     w.part_n = (uint32_t*)take(R * S * 32);
     w.list = (u64*)take(R * kList * 8);
     w.gather = (u64*)take(R * kGather * 8);
-    w.bin_w = (u64*)take(R * S * kBins * 8);
-    w.bin_n = (uint32_t*)take(R * S * kBins * 4);
+    w.above = (double*)take(R * S * 16);
+    w.bins = (u64*)take(R * S * kBins * 8);
     if (ws) *ws = w;
     return at;
 }
