@@ -22,7 +22,8 @@ namespace tlt {
 typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
-constexpr int kWeighThreads = 256, kGatherThreads = 512;
+constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
+constexpr int kManyRows = 96;                        // from here on a row is one workgroup's
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
@@ -994,22 +995,13 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
 }
 
 // ---- filtered rows
+// Pieces first, first + step, .. of a row below `end`, with what is not kept at -infinity (copy: as they are); returns this thread's number of kept tokens.
 template <typename T>
-__global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
-    constexpr int VEC = RowView<T>::VEC, NT = kWeighThreads;
-    __shared__ double tmp[16];
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, r = geo.row0 + lr;
-    const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
-    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);   // (its least weight)
-    const PickRow& pr = ws.row[lr];
-    const bool copy = pr.cut == 0;
-    const Weigh w(row_top(geo, ws, lr), ask.tau);
-    const Kept in{pr.cut, pr.last, ask.least};
-    T* o = (T*)out.rows + (int64_t)r * out.rows_stride;
+__device__ __forceinline__ uint32_t mask_row(const RowView<T>& row, T* o, int first, int step, int end, const Weigh& w, const Kept& in, bool copy) {
+    constexpr int VEC = RowView<T>::VEC;
     const bool wide = ((uintptr_t)o & 15) == ((uintptr_t)row.row & 15);
-    const int c1 = min(row.pieces(), (g + 1) * geo.per);
     uint32_t count = 0;
-    row.each(g * geo.per + tid, NT, c1, [&](int c, const float (&x)[VEC]) {
+    row.each(first, step, end, [&](int c, const float (&x)[VEC]) {
         const int j = row.first(c);
         float y[VEC];
 #pragma unroll
@@ -1018,18 +1010,261 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
             count += keep & !copy & (x[e] > -INFINITY);
             y[e] = (keep | copy) ? x[e] : -INFINITY;
         }
-        if (c >= c1) return;
+        if (c >= end) return;
         if (wide && row.inside(c)) {
             *(u32x4_t*)(o + j) = RowView<T>::packed(y);
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                if (j + e >= 0 && j + e < geo.V) o[j + e] = from_float<T>(y[e]);
+                if (j + e >= 0 && j + e < row.V) o[j + e] = from_float<T>(y[e]);
         }
     });
+    return count;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
+    constexpr int NT = kWeighThreads;
+    __shared__ double tmp[16];
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, r = geo.row0 + lr;
+    const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
+    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);   // (its least weight)
+    const PickRow& pr = ws.row[lr];
+    const Weigh w(row_top(geo, ws, lr), ask.tau);
+    const uint32_t count = mask_row<T>(row, (T*)out.rows + (int64_t)r * out.rows_stride, g * geo.per + threadIdx.x, NT, min(row.pieces(), (g + 1) * geo.per), w,
+                                       Kept{pr.cut, pr.last, ask.least}, pr.cut == 0);
     if (!out.kept) return;
     const double all = block_sum<NT>((double)count, tmp);
-    if (tid == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
+    if (threadIdx.x == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
+}
+
+// ---- many rows: a workgroup each, which does everything without meeting another one
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
+    constexpr int VEC = RowView<T>::VEC, NT = kRowThreads, NW = NT / 64, kWaveList = kGather / NW;
+    __shared__ u64 list[kGather];         // waves' lists of likely tokens, then the bin's tokens
+    __shared__ u64 bins[kBins];
+    __shared__ FindLds find;
+    __shared__ double tmp[16], part[16];
+    __shared__ float wave_top[NW], wave_reach[kGroups][NW];
+    __shared__ uint32_t wave_groups[kGroups][NW], wave_n[NW], count_n;
+    __shared__ Drawn drawn;
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const RowView<T> row(logits + (int64_t)r * row_stride, V);
+    const int pieces = row.pieces();
+    // the largest logit, the number of tokens, and how far the likely ones reach
+    float top = -INFINITY;
+    bool nan = false;
+    uint32_t tokens = 0;
+    row.each(tid, NT, pieces, [&](int, const float (&x)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) nan |= x[e] != x[e], top = fmaxf(top, x[e]), tokens += x[e] > -INFINITY;
+    });
+    float s = top;
+    int have = 1;
+#pragma unroll
+    for (int k = kGroups - 1; k >= 0; --k) {
+        constexpr int most = NT / 64;
+        const int lanes = most >> k;   // of a group
+        for (; have < lanes; have <<= 1) s = fmaxf(s, __shfl_xor(s, have, 64));
+        const uint64_t full = __ballot(s > -INFINITY);
+        const float least = -wave_max(s > -INFINITY ? -s : -INFINITY);
+        if (lane == 0) wave_reach[k][wave] = least, wave_groups[k][wave] = (uint32_t)(__popcll(full) / lanes);
+    }
+    top = wave_max(top);
+    if (__any(nan)) top = NAN;
+    tokens = (uint32_t)wave_sum_d((double)tokens);
+    if (lane == 0) wave_top[wave] = top, wave_n[wave] = tokens;
+    __syncthreads();
+    top = wave_top[0], tokens = wave_n[0];
+#pragma unroll
+    for (int v = 1; v < NW; ++v) top = top != top || wave_top[v] != wave_top[v] ? NAN : fmaxf(top, wave_top[v]), tokens += wave_n[v];
+    T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
+    if (top != top || top == -INFINITY) {   // (uniform)
+        if (o && o != row.row) mask_row<T>(row, o, tid, NT, pieces, Weigh(0.f, 1.0), Kept{0, 0, 0.0}, true);
+        if (tid == 0) put_nothing(out, r, top != top);
+        return;
+    }
+    const Asked ask = asked_of(filter, r / rows_per_seq, (int)tokens);
+    const Weigh w(top, ask.tau);
+    const bool prefix = ask.prefix();
+    Kept in{kKeyNothing, -1, ask.least};   // (all, unless a prefix is asked for)
+    const int wper = (pieces + NW - 1) / NW, c0 = min(pieces, wave * wper), c1 = min(pieces, c0 + wper);   // a wave's range, where ranges matter
+    double whole = 0.0;
+    bool by_ranges = !prefix;              // the draw goes by the sums over the waves' ranges
+    double kept = 0.0, count = 0.0;
+    if (prefix) {
+        const int level = ask.top_k <= 64 ? 0 : ask.top_k <= 128 ? 1 : 2;
+        int rank = 0;
+        float from = INFINITY;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) rank += wave_groups[level][v], from = fminf(from, wave_reach[level][v]);
+        from = fmaxf(from, -FLT_MAX);
+        const bool count_bins = ask.top_k > min(rank, kListed), use_bins = count_bins || ask.top_k == 0;
+        if (count_bins) from = INFINITY;
+        const float per_logit = use_bins ? bins_per_logit(ask, V) : 0.f;
+        const bool weigh_all = use_bins || out.logprob;
+        if (use_bins)
+            for (int i = tid; i < kBins; i += NT) bins[i] = 0;
+        if (tid == 0) count_n = 0;
+        __syncthreads();
+        u64* listing = list + wave * kWaveList;
+        uint32_t listed = 0;
+        row.each(tid, NT, pieces, [&](int c, const float (&x)[VEC]) {   // (waves take turns, so that neighbouring tokens go to several lists)
+            double weight[VEC];
+            if (weigh_all) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    weight[e] = w(x[e]);
+                    whole += weight[e];
+                }
+            }
+            float best = x[0];
+#pragma unroll
+            for (int e = 1; e < VEC; ++e) best = fmaxf(best, x[e]);
+            if (__any(best >= from)) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const bool is = x[e] >= from;
+                    const uint64_t all = __ballot(is);
+                    const uint32_t at = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+                    if (is && at < (uint32_t)kWaveList) listing[at] = entry_of(x[e], row.first(c) + e);
+                    listed += (uint32_t)__popcll(all);
+                }
+            }
+            if (use_bins) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int b = bin_of(w, x[e], per_logit);
+                    if (b < kBins) atomicAdd(&bins[b], count_bins ? 1ull : w.whole(weight[e]));
+                }
+            }
+        });
+        for (uint32_t i = listed + lane; i < (uint32_t)kWaveList; i += 64) listing[i] = kNoEntry;
+        if (lane == 0) atomicAdd(&count_n, listed > (uint32_t)kWaveList ? 1u << 20 : listed);
+        whole = block_sum<NT>(whole, tmp);
+        const LongTokenList l{list, w, kGather};
+        uint32_t n = count_n;
+        u64 end = kNoEntry;
+        if (n > 0 && n <= (uint32_t)kGather) end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, w, from, find, tmp);
+        int lo = 0, hi = 0;
+        int state = end != kNoEntry ? kDone : kStepwise;
+        if (state != kDone && use_bins) {
+            // the bin that the end lies in
+            const double mine = tid < kBins ? (double)bins[tid] : 0.0;
+            const double all = block_sum<NT>(mine, tmp), aim = count_bins ? (double)ask.top_k : share_of(ask.top_p, whole), run = block_excl_d<NT>(mine, tmp);
+            if (tid == 0) find.bin = -1;
+            __syncthreads();
+            if (run < aim && aim <= run + mine) find.bin = tid, find.base = run + mine;
+            __syncthreads();
+            const bool found = find.bin >= 0;
+            lo = hi = find.bin;
+            if (found) state = count_bins ? kByNumber : kByWeight;
+            if (count_bins && ask.by_p()) {
+                state = (found ? find.base : all) <= (double)kGather ? kAllDownTo : kStepwise;
+                lo = 0, hi = found ? hi : kBins - 1;
+            }
+            __syncthreads();
+        }
+        if (state == kByNumber || state == kByWeight || state == kAllDownTo) {
+            double above = 0.0;
+            uint32_t above_n = 0, kept_n = 0;
+            if (tid == 0) count_n = 0;
+            __syncthreads();
+            row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int b = bin_of(w, x[e], per_logit);
+                    if (b < lo) {
+                        const double weight = w(x[e]);
+                        const bool is = weight >= ask.least;
+                        above += weight, ++above_n;
+                        kept += is ? weight : 0.0, kept_n += is;
+                    }
+                    const bool is = b >= lo && b <= hi;
+                    const uint64_t all = __ballot(is);
+                    if (all) {
+                        uint32_t first = 0;
+                        if (lane == 0) first = atomicAdd(&count_n, (uint32_t)__popcll(all));
+                        const uint32_t at = __builtin_amdgcn_readfirstlane(first) + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+                        if (is && at < (uint32_t)kGather) list[at] = entry_of(x[e], row.first(c) + e);
+                    }
+                }
+            });
+            above = block_sum<NT>(above, tmp);
+            const double before_n = block_sum<NT>((double)above_n, tmp);
+            count = (double)kept_n;
+            n = count_n;
+            if (n > 0 && n <= (uint32_t)kGather) {
+                const LongTokenList m{list, w, (int)n};
+                Asked one = ask;
+                if (state == kByNumber) one.top_p = 1u << 31;
+                if (state == kAllDownTo && one.top_k > (int)n) one.top_k = 0;   // (tokens without weight fill it up)
+                end = end_in_list<NT>(m, (int)n, one, above, before_n, whole, w, top - (float)(hi + 1) / per_logit, find, tmp);
+            }
+            if (end == kNoEntry) state = kStepwise;
+        }
+        if (state == kStepwise) {
+            __syncthreads();
+            cut_stepwise<NT>(row, ask, w, list, tmp, in.cut, in.last);
+            by_ranges = true;
+        } else {
+            in.cut = ~(uint32_t)(end >> 32), in.last = (int)(uint32_t)end;
+        }
+        if (out.token && (state == kDone || state == kAllDownTo)) {
+            draw_from_list<NT>(LongTokenList{list, w, state == kDone ? kGather : (int)n}, end, ask, V, find, tmp, out, r, &drawn);
+            if (tid == 0) put_token(out, r, w, drawn, whole);
+            return;
+        }
+        if (out.token && !by_ranges) {
+            // what the bin's list keeps joins the sums of its ranges
+            kept = wave_sum_d(kept);
+            if (lane == 0) part[wave] = kept;
+            __syncthreads();
+            for (uint32_t i = tid; i < n; i += NT) {
+                const double x = list[i] <= end ? w(entry_logit(list[i])) : -1.0;
+                if (x >= ask.least && x >= 0.0) {
+                    atomicAdd(&part[(((int)(uint32_t)list[i] + row.off) / VEC) / wper], x);
+                    count += 1.0;
+                }
+            }
+            __syncthreads();
+        }
+    }
+    if (!out.token) {
+        const uint32_t mine = mask_row<T>(row, o, tid, NT, pieces, w, in, false);
+        const double all = block_sum<NT>((double)mine, tmp);
+        if (tid == 0 && out.kept) out.kept[r] = (int32_t)all;
+        return;
+    }
+    if (by_ranges) {
+        // sums over the waves' ranges; without a prefix they are those of all weights too
+        count = 0.0, kept = 0.0;
+        double all = 0.0;
+        uint32_t kept_n = 0;
+        row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const double weight = w(x[e]);
+                const bool is = in(w, row.first(c) + e, x[e]) && x[e] > -INFINITY;
+                all += weight, kept += is ? weight : 0.0, kept_n += is;
+            }
+        });
+        whole = block_sum<NT>(all, tmp);
+        count = (double)kept_n;
+        kept = wave_sum_d(kept);
+        if (lane == 0) part[wave] = kept;
+        __syncthreads();
+    }
+    count = block_sum<NT>(count, tmp);
+    if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
+    const double mine = tid < NW ? part[tid] : 0.0, S = block_sum<NT>(mine, tmp), aim = aim_of(out.u[r], S);
+    double base;
+    const int range = range_of<NT>(mine, aim, base, find, tmp);
+    if (range < 0) return;   // (cannot be)
+    const int p0 = min(pieces, range * wper), p1 = min(pieces, p0 + wper);
+    draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
+    if (tid == 0) put_token(out, r, w, drawn, whole);
 }
 
 // ---- small vocabularies: a row is one list, and one workgroup does everything
@@ -1108,7 +1343,7 @@ static int pick_segs(int rows, int vocab) {
     return segs;
 }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
-    if (vocab <= kSmall) return 256;
+    if (vocab <= kSmall || rows >= kManyRows) return 256;
     const size_t R = (size_t)std::min(rows, kBatchRows), S = (size_t)pick_segs(rows, vocab);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -1138,6 +1373,10 @@ template <typename T>
 static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, const T* logits, int64_t row_stride, const PickFilter& filter, const PickOut& out, char* base) {
     if (vocab <= kSmall) {
         hipLaunchKernelGGL(pick_small_k<T>, dim3(rows), dim3(kGatherThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
+        return;
+    }
+    if (rows >= kManyRows) {
+        hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
         return;
     }
     PickWs ws;
