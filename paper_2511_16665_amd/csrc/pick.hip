@@ -24,6 +24,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
 constexpr int kManyRows = 96;                        // from here on a row is one workgroup's
+constexpr int kMostRows = 256;                       // up to here its long prefixes are shared out among several (one row on each CU)
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
@@ -33,7 +34,6 @@ constexpr int kSmall = 4096;                         // vocabularies up to here 
 // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
 constexpr int kGroups = 3, kListed = 64 << (kGroups - 1);   // and the largest top_k that lists are made for
 constexpr int kInFlight = 4;                         // 16-byte pieces a lane asks for at once
-constexpr int kBatchRows = 256;                      // rows of one round: their logits stay in the last-level cache between the readings
 constexpr u64 kNoEntry = ~0ull;
 
 // order of logits as whole numbers; -0 and +0 are equal
@@ -56,18 +56,23 @@ struct Asked {
     __device__ __forceinline__ bool by_p() const { return top_p < (1u << 31); }
     __device__ __forceinline__ bool prefix() const { return top_k > 0 || by_p(); }
 };
-// tokens: of the row, above -infinity
-__device__ __forceinline__ Asked asked_of(const PickFilter& f, int seq, int tokens) {
-    const float tau = f.temperature ? f.temperature[seq] : 1.f, p = f.top_p ? f.top_p[seq] : 1.f, m = f.min_p ? f.min_p[seq] : 0.f;
-    const int k = f.top_k ? f.top_k[seq] : 0;
-    Asked a{1.0, 1, 1u << 31, 0.0};
-    if (!(tau > 0.f)) return a;
-    a.tau = (double)tau;
-    a.top_k = k < tokens ? max(k, 0) : 0;
-    if (p < 1.f) a.top_p = (uint32_t)(fmax((double)p, 0.0) * 2147483648.0);
-    if (m > 0.f) a.least = floor(fmin((double)m, 1.0) * 4294967296.0);
-    return a;
-}
+// the request's numbers as they are (loaded before they are needed)
+struct Wish {
+    float tau, p, m;
+    int k;
+    __device__ __forceinline__ Wish(const PickFilter& f, int seq)
+        : tau(f.temperature ? f.temperature[seq] : 1.f), p(f.top_p ? f.top_p[seq] : 1.f), m(f.min_p ? f.min_p[seq] : 0.f), k(f.top_k ? f.top_k[seq] : 0) {}
+    // tokens: of the row, above -infinity
+    __device__ __forceinline__ Asked asked(int tokens) const {
+        Asked a{1.0, 1, 1u << 31, 0.0};
+        if (!(tau > 0.f)) return a;
+        a.tau = (double)tau;
+        a.top_k = k < tokens ? max(k, 0) : 0;
+        if (p < 1.f) a.top_p = (uint32_t)(fmax((double)p, 0.0) * 2147483648.0);
+        if (m > 0.f) a.least = floor(fmin((double)m, 1.0) * 4294967296.0);
+        return a;
+    }
+};
 // ceil(share * S / 2^31), at least 1
 __device__ __forceinline__ double share_of(uint32_t share, double S) {
     const unsigned __int128 x = (unsigned __int128)share * (u64)S + 0x7fffffffu;
@@ -196,6 +201,46 @@ struct RowView {
     }
 };
 
+// Places in a list for the wave's lanes with `is`, from a counter in LDS
+__device__ __forceinline__ uint32_t place(bool is, uint32_t* n) {
+    const uint64_t all = __ballot(is);
+    if (all == 0) return 0;
+    uint32_t first = 0;
+    if ((threadIdx.x & 63) == 0) first = atomicAdd(n, (uint32_t)__popcll(all));
+    return __builtin_amdgcn_readfirstlane(first) + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+}
+
+// Weights of a wave's scattered tokens: their logits are put side by side first, 64 at a time, so that the lanes of the arithmetic are full (buf: 128 floats of LDS).
+struct SparseSum {
+    float* buf;
+    double least, sum = 0.0;   // of this lane: to be added up over the wave
+    uint32_t count = 0, n = 0;
+    __device__ __forceinline__ void take(const Weigh& w, uint32_t many) {
+        const int lane = threadIdx.x & 63;
+        const double x = (uint32_t)lane < many ? w(buf[lane]) : -1.0;
+        const bool in = x >= least && x >= 0.0;
+        sum += in ? x : 0.0, count += in;
+    }
+    __device__ __forceinline__ void add(const Weigh& w, bool is, float x) {
+        const uint64_t all = __ballot(is);
+        if (all == 0) return;
+        const int lane = threadIdx.x & 63;
+        if (is) buf[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = x;
+        n += (uint32_t)__popcll(all);
+        if (n < 64) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        take(w, 64);
+        const float rest = buf[64 + lane];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        buf[lane] = rest;
+        n -= 64;
+    }
+    __device__ __forceinline__ void finish(const Weigh& w) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (n) take(w, n);
+    }
+};
+
 // ---- sums over a workgroup of NT threads, or over one wave (NT = 64), which needs no barrier
 template <int NT>
 __device__ __forceinline__ void together() {
@@ -252,19 +297,13 @@ __device__ __forceinline__ double block_excl_d(double v, double* tmp) {
     return base + incl - v;
 }
 
-// ---- tokens in a list in LDS: entry_of (kNoEntry: none) and weights
+// ---- tokens in a list in LDS: entry_of, and the weights where there is room for them (they are formed when they are asked for otherwise)
 struct TokenList {
     const u64* e;
-    const double* w;
+    const double* stored;
+    Weigh w;
     int n;
-    __device__ __forceinline__ double weight(int i) const { return w[i]; }
-};
-// (weights formed when they are asked for: in LDS they would cost workgroups on a CU)
-struct LongTokenList {
-    const u64* e;
-    const Weigh& w;
-    int n;
-    __device__ __forceinline__ double weight(int i) const { return w(entry_logit(e[i])); }
+    __device__ __forceinline__ double weight(int i) const { return stored ? stored[i] : w(entry_logit(e[i])); }
 };
 struct FindLds {
     u64 bins[kFindBins], order[kFindFew];
@@ -350,7 +389,7 @@ struct PickRow {
     int32_t bin_lo, bin_hi;     // bins to gather: the one that the end lies in (kByWeight: of top_p; kByNumber: of top_k), or all down to it (kAllDownTo)
     uint32_t cut;               // the result: kept are keys above it and those equal to it up to index `last`; 0: the row is copied
     int32_t last;
-    double whole;
+    double before, whole;       // weight (kByWeight) or number (kByNumber) of the tokens above those bins
 };
 struct PickWs {
     PickRow* row;
@@ -360,12 +399,11 @@ struct PickWs {
     double *whole, *part;    // [rows][segs], [rows][segs * 8]: sums of kept weights over the ranges of waves
     uint32_t* part_n;        // their counts
     u64 *list, *gather;      // [rows][kList], [rows][kGather]
-    double* above;           // [rows][segs][2]: weight and number of the tokens above the gathered ones
     u64* bins;               // [rows][segs][kBins]
 };
 struct PickGeo {
     int V, segs, per;         // per: pieces of a segment
-    int rows_per_seq, row0;   // row0: first row of this round
+    int rows_per_seq;
 };
 
 // The workgroup that is the last of `total` of a row to come here sees what all of them wrote (every wave waits for its stores, then one thread releases them).
@@ -399,12 +437,12 @@ struct Drawn {
     int token;
     float logit;
 };
-__device__ __forceinline__ void put_token(const PickOut& out, int r, const Weigh& w, const Drawn& d, double whole) {
-    out.token[r] = d.token;
-    if (out.logprob) {
+__device__ __forceinline__ void put_token(int32_t* token, float* logprob, const Weigh w, const Drawn& d, double whole) {
+    *token = d.token;
+    if (logprob) {
         const double z = w.below(d.logit);
-        out.logprob[2 * r] = (float)(z - log(d.S * 0x1p-32));
-        out.logprob[2 * r + 1] = (float)(z - log(whole * 0x1p-32));
+        logprob[0] = (float)(z - log(d.S * 0x1p-32));
+        logprob[1] = (float)(z - log(whole * 0x1p-32));
     }
 }
 
@@ -420,9 +458,9 @@ struct Kept {
     }
 };
 
-// The first token of pieces [c0, c1) whose running sum, from `base` on, of kept weights exceeds what aim_of_sum gives for the sum over the pieces.
-template <int NT, typename T, typename F>
-__device__ void draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w, const Kept& kept, double base, F aim_of_sum, double* tmp, Drawn* drawn) {
+// The first token of pieces [c0, c1) whose running sum, from `base` on, of kept weights exceeds (u * S) >> 32.  S < 0: the sum over the pieces.
+template <int NT, typename T>
+__device__ __forceinline__ void draw_from(const RowView<T> row, int c0, int c1, const Weigh w, const Kept kept, double base, double S, uint32_t u, double* tmp, Drawn* drawn) {
     constexpr int VEC = RowView<T>::VEC;
     const int per = (c1 - c0 + NT - 1) / NT, a = min(c1, c0 + (int)threadIdx.x * per), b = min(c1, a + per);
     double mine = 0.0;
@@ -432,9 +470,9 @@ __device__ void draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w,
 #pragma unroll
         for (int e = 0; e < VEC; ++e) mine += kept(w, row.first(c) + e, x[e]) ? w(x[e]) : 0.0;
     }
-    const double all = block_sum<NT>(mine, tmp);
-    double run = base + block_excl_d<NT>(mine, tmp), S;
-    const double aim = aim_of_sum(all, S);
+    if (S < 0.0) S = block_sum<NT>(mine, tmp);
+    double run = base + block_excl_d<NT>(mine, tmp);
+    const double aim = aim_of(u, S);
     if (run <= aim && aim < run + mine) {
         bool found = false;
         for (int c = a; c < b && !found; ++c) {
@@ -452,14 +490,14 @@ __device__ void draw_from(const RowView<T>& row, int c0, int c1, const Weigh& w,
 }
 
 // Where the prefix ends in a list whose tokens follow on before_n others of weight before_w: its last token, or kNoEntry if it ends behind them.  n of the list's entries are
-// tokens, none below the logit `least`.  S: the weight that top_p is a share of, for rows without top_k.
-template <int NT, typename L>
-__device__ u64 end_in_list(const L& l, int n, const Asked& ask, double before_w, double before_n, double S, const Weigh& w, float least, FindLds& s, double* tmp) {
+// tokens, nearly all between the logits `best` and `least`.  S: the weight that top_p is a share of, for rows without top_k.
+template <int NT>
+__device__ __forceinline__ u64 end_in_list(const TokenList l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
     u64 end = kNoEntry - 1;   // (above every entry)
     auto order = [&](int i) { return l.e[i]; };
-    // evenly over the distances to the largest logit
-    const float per = fminf((float)(kFindBins - 1) / w.distance(least), 1e30f);
-    auto bin = [&](int i) { return min((int)fminf(w.distance(entry_logit(l.e[i])) * per, 1e6f), kFindBins - 1); };
+    // evenly over the distances from `best`
+    const float near = l.w.distance(best), per = fminf((float)(kFindBins - 1) / (l.w.distance(least) - near), 1e30f);
+    auto bin = [&](int i) { return min((int)fminf(fmaxf(l.w.distance(entry_logit(l.e[i])) - near, 0.f) * per, 1e6f), kFindBins - 1); };
     if (ask.top_k > 0) {
         const double aim = (double)ask.top_k - before_n;
         if (aim > (double)n) return kNoEntry;
@@ -475,9 +513,9 @@ __device__ u64 end_in_list(const L& l, int n, const Asked& ask, double before_w,
 }
 
 // Draws from the list's tokens up to `end`, which are all that is kept but for `least`.
-template <int NT, typename L>
-__device__ void draw_from_list(const L& l, u64 end, const Asked& ask, int V, FindLds& s, double* tmp, const PickOut& out, int r, Drawn* drawn) {
-    auto in = [&](int i) { return l.e[i] <= end && l.weight(i) >= ask.least; };
+template <int NT>
+__device__ __forceinline__ void draw_from_list(const TokenList l, u64 end, double least, int V, FindLds& s, double* tmp, int32_t* kept, uint32_t u, Drawn* drawn) {
+    auto in = [&](int i) { return l.e[i] <= end && l.weight(i) >= least; };
     double S = 0.0, count = 0.0;
     for (int i = threadIdx.x; i < l.n; i += NT) {
         const bool k = in(i);
@@ -485,10 +523,10 @@ __device__ void draw_from_list(const L& l, u64 end, const Asked& ask, int V, Fin
     }
     S = block_sum<NT>(S, tmp);
     count = block_sum<NT>(count, tmp);
-    if (threadIdx.x == 0 && out.kept) out.kept[r] = (int32_t)count;
+    if (threadIdx.x == 0 && kept) *kept = (int32_t)count;
     const double per = (double)kFindBins / ((double)V + 1.0);
     const u64 token = locate<NT>(l.n, [&](int i) { return l.e[i] & 0xffffffffull; }, in, [&](int i) { return l.weight(i); }, [&](int i) { return (int)((double)(uint32_t)l.e[i] * per); },
-                                 aim_of(out.u[r], S) + 1.0, s, tmp);
+                                 aim_of(u, S) + 1.0, s, tmp);
     for (int i = threadIdx.x; i < l.n; i += NT)
         if (in(i) && (l.e[i] & 0xffffffffull) == token) drawn->S = S, drawn->token = (int)token, drawn->logit = entry_logit(l.e[i]);
     together<NT>();
@@ -514,7 +552,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T
     __shared__ float wave_top[NW], wave_reach[kGroups][NW];
     __shared__ uint32_t wave_groups[kGroups][NW], wave_tokens[NW];
     const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, wave = tid >> 6;
-    const RowView<T> row(logits + (int64_t)(geo.row0 + lr) * row_stride, geo.V);
+    const RowView<T> row(logits + (int64_t)lr * row_stride, geo.V);
     float top = -INFINITY;
     bool nan = false;
     uint32_t tokens = 0;
@@ -560,7 +598,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T
         if (g == 0) {
             PickRow z{};
             ws.row[lr] = z;
-            if (out.rows && out.kept) out.kept[geo.row0 + lr] = 0;
+            if (out.rows && out.kept) out.kept[lr] = 0;
         }
     }
 }
@@ -573,9 +611,10 @@ __device__ __forceinline__ float row_top(const PickGeo& geo, const PickWs& ws, i
 }
 
 __device__ __forceinline__ Asked asked_of_row(const PickGeo& geo, const PickWs& ws, int lr, const PickFilter& filter) {
+    const Wish wish(filter, (lr) / geo.rows_per_seq);
     const int lane = threadIdx.x & 63;
     const float n = wave_sum(lane < geo.segs ? (float)ws.tokens[lr * geo.segs + lane] : 0.f);   // (2^20 at most: exact)
-    return asked_of(filter, (geo.row0 + lr) / geo.rows_per_seq, (int)n);
+    return wish.asked((int)n);
 }
 
 // A logit that at least `rank` tokens reach, by the groups that fit what is asked for.
@@ -598,7 +637,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     __shared__ double tmp[16];
     __shared__ Drawn drawn;
     __shared__ int flag;
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     PickRow* pr = ws.row + lr;
     const float top = row_top(geo, ws, lr);
@@ -707,8 +746,8 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         const int at = range_of<NT>(mine, aim, base, find, tmp);
         if (at < 0) return;   // (cannot be: S is the sum of the parts)
         const int end = min(row.pieces(), ((at >> 3) + 1) * geo.per), p0 = min(end, (at >> 3) * geo.per + (at & 7) * wper), p1 = min(end, p0 + wper);
-        draw_from<NT>(row, p0, p1, w, Kept{kKeyNothing, -1, ask.least}, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
-        if (tid == 0) put_token(out, r, w, drawn, whole);
+        draw_from<NT, T>(row, p0, p1, w, Kept{kKeyNothing, -1, ask.least}, base, S, out.u[r], tmp, &drawn);
+        if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
         return;
     }
     const uint32_t n = pr->list_n;
@@ -716,13 +755,13 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
 #pragma unroll 4
         for (uint32_t i = tid; i < n; i += NT) local[i] = ws.list[(int64_t)lr * kList + i];
         __syncthreads();
-        const LongTokenList l{local, w, (int)n};
-        const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, w, from, find, tmp);
+        const TokenList l{local, nullptr, w, (int)n};
+        const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
         if (end != kNoEntry) {
             if (tid == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
             if (out.token) {
-                draw_from_list<NT>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
-                if (tid == 0) put_token(out, r, w, drawn, whole);
+                draw_from_list<NT>(l, end, ask.least, geo.V, find, tmp, out.kept ? out.kept + r : nullptr, out.u[r], &drawn);
+                if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
             }
             return;
         }
@@ -749,18 +788,18 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-        if (run < aim && aim <= run + (double)own[k]) find.bin = OWN * tid + k, find.base = run + (double)own[k];
+        if (run < aim && aim <= run + (double)own[k]) find.bin = OWN * tid + k, find.base = run, find.value[0] = run + (double)own[k];
         run += (double)own[k];
     }
     __syncthreads();
     if (tid == 0) {
         const bool found = find.bin >= 0;
         int state = found ? (count_bins ? kByNumber : kByWeight) : kStepwise;
-        pr->bin_lo = pr->bin_hi = find.bin;
+        pr->bin_lo = pr->bin_hi = find.bin, pr->before = find.base;
         // two limits: all tokens down to the bin of the first, if a list holds them (all that weigh anything, if they are fewer than top_k)
         if (count_bins && ask.by_p()) {
-            state = (found ? find.base : all) <= (double)kGather ? kAllDownTo : kStepwise;
-            pr->bin_lo = 0, pr->bin_hi = found ? find.bin : kBins - 1;
+            state = (found ? find.value[0] : all) <= (double)kGather ? kAllDownTo : kStepwise;
+            pr->before = 0.0, pr->bin_lo = 0, pr->bin_hi = found ? find.bin : kBins - 1;
         }
         pr->state = state;
     }
@@ -768,7 +807,9 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
 
 // ---- rows that neither list nor bins settle: digit by digit over the keys, one workgroup, every step a pass over the row
 template <int NT, typename T>
-__device__ void cut_stepwise(const RowView<T>& row, const Asked& ask, const Weigh& w, u64* lds, double* tmp, uint32_t& cut, int& last) {
+__device__ __forceinline__ u64 cut_stepwise(const RowView<T> row, const Asked ask, const Weigh w, u64* lds, double* tmp) {
+    uint32_t cut;
+    int last;
     constexpr int VEC = RowView<T>::VEC;
     u64 *bins = lds, *counts = lds + 256, *found = lds + 512;
     const int tid = threadIdx.x, pieces = row.pieces();
@@ -860,6 +901,7 @@ __device__ void cut_stepwise(const RowView<T>& row, const Asked& ask, const Weig
     __syncthreads();
     last = (int)(uint32_t)found[0];
     __syncthreads();
+    return (u64)cut << 32 | (uint32_t)last;
 }
 
 // ---- the second list
@@ -870,9 +912,10 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     __shared__ FindLds find;
     __shared__ Drawn drawn;
     __shared__ double tmp[16], part[kSegsMost * 8];
+    __shared__ float sparse[NW][128];
     __shared__ uint32_t local_n, base_n;
     __shared__ int flag;
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lr;
     PickRow* pr = ws.row + lr;
     const int state = pr->state;
     if (state == kDone || (state == kStepwise && g != 0)) return;
@@ -886,31 +929,22 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         const float per_logit = bins_per_logit(ask, geo.V);
         const int lo = pr->bin_lo, hi = pr->bin_hi;
         const int seg_end = min(row.pieces(), (g + 1) * geo.per), c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
-        double kept = 0.0, above = 0.0;
-        uint32_t kept_n = 0, above_n = 0;
         if (tid == 0) local_n = 0;
         __syncthreads();
+        SparseSum above{sparse[wave], ask.least};
         row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int b = bin_of(w, x[e], per_logit);
-                if (b < lo) {
-                    const double weight = w(x[e]);
-                    const bool in = weight >= ask.least;
-                    above += weight, ++above_n;
-                    kept += in ? weight : 0.0, kept_n += in;
-                } else if (b <= hi && x[e] > -INFINITY) {
-                    const uint32_t at = atomicAdd(&local_n, 1u);
-                    if (at < (uint32_t)kGather) local[at] = entry_of(x[e], row.first(c) + e);
-                }
+                if (out.token) above.add(w, b < lo, x[e]);
+                const bool is = b >= lo && b <= hi;
+                const uint32_t at = place(is, &local_n);
+                if (is && at < (uint32_t)kGather) local[at] = entry_of(x[e], row.first(c) + e);
             }
         });
-        kept = wave_sum_d(kept);
-        for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
-        if (lane == 0) ws.part[lr * ranges + g * 8 + wave] = kept, ws.part_n[lr * ranges + g * 8 + wave] = kept_n;
-        above = block_sum<NT>(above, tmp);
-        const double n_above = block_sum<NT>((double)above_n, tmp);
-        if (tid == 0) ws.above[2 * (lr * geo.segs + g)] = above, ws.above[2 * (lr * geo.segs + g) + 1] = n_above;
+        above.finish(w);
+        const double kept = wave_sum_d(above.sum), kept_n = wave_sum_d((double)above.count);
+        if (lane == 0) ws.part[lr * ranges + g * 8 + wave] = kept, ws.part_n[lr * ranges + g * 8 + wave] = (uint32_t)kept_n;
         __syncthreads();
         if (tid == 0) base_n = atomicAdd(&pr->gather_n, local_n > (uint32_t)kGather ? 1u << 20 : local_n);
         __syncthreads();
@@ -920,32 +954,33 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         if (!last_here(&pr->seen_gather, geo.segs, &flag)) return;
         const uint32_t n = pr->gather_n;
         if (n > 0 && n <= (uint32_t)kGather) {
-            if (tid == 0) find.found = 0;
+            if (tid == 0) find.bins[0] = kNoEntry, find.bins[1] = 0;
             __syncthreads();
-            u64 find_last = 0;
+            double* stored = n <= kGather / 2 ? (double*)(local + kGather / 2) : nullptr;
+            u64 first = kNoEntry, last = 0;
 #pragma unroll 4
             for (uint32_t i = tid; i < n; i += NT) {
                 const u64 e = ws.gather[(int64_t)lr * kGather + i];
                 local[i] = e;
-                find_last = max(find_last, e);
+                if (stored) stored[i] = w(entry_logit(e));
+                first = min(first, e), last = max(last, e);
             }
-            atomicMax(&find.found, find_last);
+            if (last) atomicMin(&find.bins[0], first), atomicMax(&find.bins[1], last);
             __syncthreads();
-            find_last = find.found;
+            first = find.bins[0], last = find.bins[1];
             __syncthreads();
-            const LongTokenList l{local, w, (int)n};
+            const TokenList l{local, stored, w, (int)n};
             if (state == kByNumber) ask.top_p = 1u << 31;
             if (state == kAllDownTo && ask.top_k > (int)n) ask.top_k = 0;   // (tokens without weight fill it up)
-            const double before_w = wave_sum_d(lane < geo.segs ? ws.above[2 * (lr * geo.segs + lane)] : 0.0);
-            const double before_n = wave_sum_d(lane < geo.segs ? ws.above[2 * (lr * geo.segs + lane) + 1] : 0.0);
-            const u64 end = end_in_list<NT>(l, (int)n, ask, before_w, before_n, whole, w, entry_logit(find_last), find, tmp);
+            const double before = pr->before;
+            const u64 end = end_in_list<NT>(l, (int)n, ask, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, entry_logit(first), entry_logit(last), find, tmp);
             if (end != kNoEntry) {
                 const Kept in{~(uint32_t)(end >> 32), (int)(uint32_t)end, ask.least};
                 if (tid == 0) pr->cut = in.cut, pr->last = in.last;
                 if (!out.token) return;
                 if (state == kAllDownTo) {
-                    draw_from_list<NT>(l, end, ask, geo.V, find, tmp, out, r, &drawn);
-                    if (tid == 0) put_token(out, r, w, drawn, whole);
+                    draw_from_list<NT>(l, end, ask.least, geo.V, find, tmp, out.kept ? out.kept + r : nullptr, out.u[r], &drawn);
+                    if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
                     return;
                 }
                 // the listed ones join the sums of their ranges
@@ -966,8 +1001,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
                 const int range = range_of<NT>(mine, aim, base, find, tmp);
                 if (range < 0) return;   // (cannot be)
                 const int stop = min(row.pieces(), ((range >> 3) + 1) * geo.per), p0 = min(stop, (range >> 3) * geo.per + (range & 7) * wper), p1 = min(stop, p0 + wper);
-                draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
-                if (tid == 0) put_token(out, r, w, drawn, whole);
+                draw_from<NT, T>(row, p0, p1, w, in, base, S, out.u[r], tmp, &drawn);
+                if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
                 return;
             }
         }
@@ -976,7 +1011,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     }
     u64* buf = local;
     Kept in{0, 0, ask.least};
-    cut_stepwise<NT>(row, ask, w, buf, tmp, in.cut, in.last);
+    const u64 found = cut_stepwise<NT, T>(row, ask, w, buf, tmp);
+    in.cut = (uint32_t)(found >> 32), in.last = (int)(uint32_t)found;
     if (tid == 0) pr->cut = in.cut, pr->last = in.last;
     if (!out.token) return;
     if (out.kept) {
@@ -990,8 +1026,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         count = block_sum<NT>(count, tmp);
         if (tid == 0) out.kept[r] = (int32_t)count;
     }
-    draw_from<NT>(row, 0, row.pieces(), w, in, 0.0, [&](double all, double& sum) { sum = all; return aim_of(out.u[r], all); }, tmp, &drawn);
-    if (tid == 0) put_token(out, r, w, drawn, whole);
+    draw_from<NT, T>(row, 0, row.pieces(), w, in, 0.0, -1.0, out.u[r], tmp, &drawn);
+    if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
 }
 
 // ---- filtered rows
@@ -1026,9 +1062,9 @@ template <typename T>
 __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
     constexpr int NT = kWeighThreads;
     __shared__ double tmp[16];
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, r = geo.row0 + lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, r = lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
-    const Asked ask = asked_of(filter, r / geo.rows_per_seq, geo.V);   // (its least weight)
+    const Asked ask = Wish(filter, r / geo.rows_per_seq).asked(geo.V);   // (its least weight)
     const PickRow& pr = ws.row[lr];
     const Weigh w(row_top(geo, ws, lr), ask.tau);
     const uint32_t count = mask_row<T>(row, (T*)out.rows + (int64_t)r * out.rows_stride, g * geo.per + threadIdx.x, NT, min(row.pieces(), (g + 1) * geo.per), w,
@@ -1038,20 +1074,44 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
     if (threadIdx.x == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
 }
 
-// ---- many rows: a workgroup each, which does everything without meeting another one
+// The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (filtered rows 32 x 48 770 us, 975 with them inlined; the kernels with fewer threads are better
+// off inlined).
+template <int NT>
+__device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
+    return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, s, tmp);
+}
+template <int NT>
+__device__ __attribute__((noinline)) void draw_from_list_apart(const TokenList l, u64 end, double least, int V, FindLds& s, double* tmp, int32_t* kept, uint32_t u, Drawn* drawn) {
+    draw_from_list<NT>(l, end, least, V, s, tmp, kept, u, drawn);
+}
+template <int NT, typename T>
+__device__ __attribute__((noinline)) void draw_from_apart(const RowView<T> row, int c0, int c1, const Weigh w, const Kept kept, double base, double S, uint32_t u, double* tmp, Drawn* drawn) {
+    draw_from<NT, T>(row, c0, c1, w, kept, base, S, u, tmp, drawn);
+}
+template <int NT, typename T>
+__device__ __attribute__((noinline)) u64 cut_stepwise_apart(const RowView<T> row, const Asked ask, const Weigh w, u64* lds, double* tmp) {
+    return cut_stepwise<NT, T>(row, ask, w, lds, tmp);
+}
+__device__ __attribute__((noinline)) void put_token_apart(int32_t* token, float* logprob, const Weigh w, const Drawn& d, double whole) { put_token(token, logprob, w, d, whole); }
+
+// ---- many rows: a workgroup each, which does everything without meeting another one.  segs > 0: but for rows whose prefix the list does not hold, which are left to
+// pick_gather_k, with what it needs to know in ws.
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
+__global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out, int segs, PickWs ws) {
     constexpr int VEC = RowView<T>::VEC, NT = kRowThreads, NW = NT / 64, kWaveList = kGather / NW;
-    __shared__ u64 list[kGather];         // waves' lists of likely tokens, then the bin's tokens
+    __shared__ u64 list[kGather];         // waves' lists of likely tokens, put together; then the bin's tokens
     __shared__ u64 bins[kBins];
     __shared__ FindLds find;
     __shared__ double tmp[16], part[16];
+    __shared__ float sparse[NW][128];
     __shared__ float wave_top[NW], wave_reach[kGroups][NW];
     __shared__ uint32_t wave_groups[kGroups][NW], wave_n[NW], count_n;
     __shared__ Drawn drawn;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const RowView<T> row(logits + (int64_t)r * row_stride, V);
     const int pieces = row.pieces();
+    const Wish wish(filter, r / rows_per_seq);
+    const uint32_t u = out.token ? out.u[r] : 0u;
     // the largest logit, the number of tokens, and how far the likely ones reach
     float top = -INFINITY;
     bool nan = false;
@@ -1080,12 +1140,14 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
 #pragma unroll
     for (int v = 1; v < NW; ++v) top = top != top || wave_top[v] != wave_top[v] ? NAN : fmaxf(top, wave_top[v]), tokens += wave_n[v];
     T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
+    PickRow* pr = ws.row + r;
+    if (segs && tid == 0) pr->state = kDone, pr->gather_n = pr->seen_gather = 0;
     if (top != top || top == -INFINITY) {   // (uniform)
         if (o && o != row.row) mask_row<T>(row, o, tid, NT, pieces, Weigh(0.f, 1.0), Kept{0, 0, 0.0}, true);
         if (tid == 0) put_nothing(out, r, top != top);
         return;
     }
-    const Asked ask = asked_of(filter, r / rows_per_seq, (int)tokens);
+    const Asked ask = wish.asked((int)tokens);
     const Weigh w(top, ask.tau);
     const bool prefix = ask.prefix();
     Kept in{kKeyNothing, -1, ask.least};   // (all, unless a prefix is asked for)
@@ -1140,80 +1202,89 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                 }
             }
         });
-        for (uint32_t i = listed + lane; i < (uint32_t)kWaveList; i += 64) listing[i] = kNoEntry;
-        if (lane == 0) atomicAdd(&count_n, listed > (uint32_t)kWaveList ? 1u << 20 : listed);
-        whole = block_sum<NT>(whole, tmp);
-        const LongTokenList l{list, w, kGather};
-        uint32_t n = count_n;
+        if (lane == 0) wave_n[wave] = listed > (uint32_t)kWaveList ? 1u << 20 : listed;
+        whole = block_sum<NT>(whole, tmp);   // (the lists are whole, too)
+        uint32_t n = 0, at = 0;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) at += v < wave ? wave_n[v] : 0, n += wave_n[v];
+        if (n <= (uint32_t)kGather) {
+            u64 held[kWaveList / 64];
+#pragma unroll
+            for (int i = 0; i < kWaveList / 64; ++i) held[i] = listing[i * 64 + lane];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kWaveList / 64; ++i)
+                if ((uint32_t)(i * 64 + lane) < listed) list[at + i * 64 + lane] = held[i];
+            __syncthreads();
+        }
+        TokenList l{list, nullptr, w, (int)n};
         u64 end = kNoEntry;
-        if (n > 0 && n <= (uint32_t)kGather) end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, w, from, find, tmp);
+        if (n > 0 && n <= (uint32_t)kGather) end = end_in_list_apart<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
         int lo = 0, hi = 0;
+        double before = 0.0;
         int state = end != kNoEntry ? kDone : kStepwise;
         if (state != kDone && use_bins) {
             // the bin that the end lies in
+            static_assert(kBins <= NT, "a bin per thread");
             const double mine = tid < kBins ? (double)bins[tid] : 0.0;
             const double all = block_sum<NT>(mine, tmp), aim = count_bins ? (double)ask.top_k : share_of(ask.top_p, whole), run = block_excl_d<NT>(mine, tmp);
             if (tid == 0) find.bin = -1;
             __syncthreads();
-            if (run < aim && aim <= run + mine) find.bin = tid, find.base = run + mine;
+            if (run < aim && aim <= run + mine) find.bin = tid, find.base = run, find.value[0] = run + mine;
             __syncthreads();
             const bool found = find.bin >= 0;
-            lo = hi = find.bin;
+            lo = hi = find.bin, before = find.base;
             if (found) state = count_bins ? kByNumber : kByWeight;
             if (count_bins && ask.by_p()) {
-                state = (found ? find.base : all) <= (double)kGather ? kAllDownTo : kStepwise;
-                lo = 0, hi = found ? hi : kBins - 1;
+                state = (found ? find.value[0] : all) <= (double)kGather ? kAllDownTo : kStepwise;
+                before = 0.0, lo = 0, hi = found ? hi : kBins - 1;
             }
             __syncthreads();
         }
+        if (segs && state != kDone) {
+            if (tid < segs) ws.top[r * segs + tid] = top, ws.tokens[r * segs + tid] = tid == 0 ? tokens : 0;
+            if (tid == 0) pr->state = state, pr->bin_lo = lo, pr->bin_hi = hi, pr->before = before, pr->whole = whole;
+            return;
+        }
         if (state == kByNumber || state == kByWeight || state == kAllDownTo) {
-            double above = 0.0;
-            uint32_t above_n = 0, kept_n = 0;
             if (tid == 0) count_n = 0;
             __syncthreads();
+            SparseSum above{sparse[wave], ask.least};
             row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const int b = bin_of(w, x[e], per_logit);
-                    if (b < lo) {
-                        const double weight = w(x[e]);
-                        const bool is = weight >= ask.least;
-                        above += weight, ++above_n;
-                        kept += is ? weight : 0.0, kept_n += is;
-                    }
+                    if (out.token) above.add(w, b < lo, x[e]);
                     const bool is = b >= lo && b <= hi;
-                    const uint64_t all = __ballot(is);
-                    if (all) {
-                        uint32_t first = 0;
-                        if (lane == 0) first = atomicAdd(&count_n, (uint32_t)__popcll(all));
-                        const uint32_t at = __builtin_amdgcn_readfirstlane(first) + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
-                        if (is && at < (uint32_t)kGather) list[at] = entry_of(x[e], row.first(c) + e);
-                    }
+                    const uint32_t at = place(is, &count_n);
+                    if (is && at < (uint32_t)kGather) list[at] = entry_of(x[e], row.first(c) + e);
                 }
             });
-            above = block_sum<NT>(above, tmp);
-            const double before_n = block_sum<NT>((double)above_n, tmp);
-            count = (double)kept_n;
+            above.finish(w);
+            kept = above.sum, count = (double)above.count;
+            __syncthreads();
             n = count_n;
             if (n > 0 && n <= (uint32_t)kGather) {
-                const LongTokenList m{list, w, (int)n};
+                l.n = (int)n;
                 Asked one = ask;
                 if (state == kByNumber) one.top_p = 1u << 31;
                 if (state == kAllDownTo && one.top_k > (int)n) one.top_k = 0;   // (tokens without weight fill it up)
-                end = end_in_list<NT>(m, (int)n, one, above, before_n, whole, w, top - (float)(hi + 1) / per_logit, find, tmp);
+                end = end_in_list_apart<NT>(l, (int)n, one, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit,
+                                      find, tmp);
             }
             if (end == kNoEntry) state = kStepwise;
         }
         if (state == kStepwise) {
             __syncthreads();
-            cut_stepwise<NT>(row, ask, w, list, tmp, in.cut, in.last);
+            const u64 cut = cut_stepwise_apart<NT, T>(row, ask, w, list, tmp);
+            in.cut = (uint32_t)(cut >> 32), in.last = (int)(uint32_t)cut;
             by_ranges = true;
         } else {
             in.cut = ~(uint32_t)(end >> 32), in.last = (int)(uint32_t)end;
         }
         if (out.token && (state == kDone || state == kAllDownTo)) {
-            draw_from_list<NT>(LongTokenList{list, w, state == kDone ? kGather : (int)n}, end, ask, V, find, tmp, out, r, &drawn);
-            if (tid == 0) put_token(out, r, w, drawn, whole);
+            draw_from_list_apart<NT>(l, end, ask.least, V, find, tmp, out.kept ? out.kept + r : nullptr, u, &drawn);
+            if (tid == 0) put_token_apart(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
             return;
         }
         if (out.token && !by_ranges) {
@@ -1222,7 +1293,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
             if (lane == 0) part[wave] = kept;
             __syncthreads();
             for (uint32_t i = tid; i < n; i += NT) {
-                const double x = list[i] <= end ? w(entry_logit(list[i])) : -1.0;
+                const double x = list[i] <= end ? l.weight((int)i) : -1.0;
                 if (x >= ask.least && x >= 0.0) {
                     atomicAdd(&part[(((int)(uint32_t)list[i] + row.off) / VEC) / wper], x);
                     count += 1.0;
@@ -1258,13 +1329,13 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
     }
     count = block_sum<NT>(count, tmp);
     if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
-    const double mine = tid < NW ? part[tid] : 0.0, S = block_sum<NT>(mine, tmp), aim = aim_of(out.u[r], S);
+    const double mine = tid < NW ? part[tid] : 0.0, S = block_sum<NT>(mine, tmp), aim = aim_of(u, S);
     double base;
     const int range = range_of<NT>(mine, aim, base, find, tmp);
     if (range < 0) return;   // (cannot be)
     const int p0 = min(pieces, range * wper), p1 = min(pieces, p0 + wper);
-    draw_from<NT>(row, p0, p1, w, in, base, [&](double, double& sum) { sum = S; return aim; }, tmp, &drawn);
-    if (tid == 0) put_token(out, r, w, drawn, whole);
+    draw_from_apart<NT, T>(row, p0, p1, w, in, base, S, u, tmp, &drawn);
+    if (tid == 0) put_token_apart(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
 }
 
 // ---- small vocabularies: a row is one list, and one workgroup does everything
@@ -1278,6 +1349,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
     const int r = blockIdx.x, tid = threadIdx.x;
     const T* row = logits + (int64_t)r * row_stride;
     T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
+    const Wish wish(filter, r / rows_per_seq);
+    const uint32_t u = out.token ? out.u[r] : 0u;
     float top = -INFINITY, least = INFINITY;
     bool nan = false;
     double tokens = 0.0;
@@ -1308,7 +1381,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < NT / 64; ++v) least = fminf(least, (float)tmp[v]);
-    const Asked ask = asked_of(filter, r / rows_per_seq, (int)tokens);
+    const Asked ask = wish.asked((int)tokens);
     const Weigh w(top, ask.tau);
     double whole = 0.0;
     for (int j = tid; j < V; j += NT) {
@@ -1316,11 +1389,11 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
         weight[j] = x, whole += x;
     }
     whole = block_sum<NT>(whole, tmp);   // (and all of both lists is there)
-    const TokenList l{entry, weight, V};
-    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, w, least, find, tmp);
+    const TokenList l{entry, weight, w, V};
+    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, top, least, find, tmp);
     if (out.token) {
-        draw_from_list<NT>(l, end, ask, V, find, tmp, out, r, &drawn);
-        if (tid == 0) put_token(out, r, w, drawn, whole);
+        draw_from_list<NT>(l, end, ask.least, V, find, tmp, out.kept ? out.kept + r : nullptr, u, &drawn);
+        if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
         return;
     }
     double count = 0.0;
@@ -1336,15 +1409,16 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 
 // ---- host
 static int pick_segs(int rows, int vocab) {
+    if (rows >= kManyRows) return std::max(1, std::min(8, 1 << (31 - __builtin_clz(std::max(1, vocab / 4096)))));   // (of the second list)
     // some 1024 workgroups, of 4096 tokens at least (so that each of a segment's threads has some)
-    const int most = std::max(1, std::min(1024 / std::min(rows, kBatchRows), vocab / 4096));
+    const int most = std::max(1, std::min(1024 / rows, vocab / 4096));
     int segs = 1;
     while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
     return segs;
 }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
-    if (vocab <= kSmall || rows >= kManyRows) return 256;
-    const size_t R = (size_t)std::min(rows, kBatchRows), S = (size_t)pick_segs(rows, vocab);
+    if (vocab <= kSmall || rows > kMostRows) return 256;
+    const size_t R = (size_t)rows, S = (size_t)pick_segs(rows, vocab);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         char* p = base + at;
@@ -1362,7 +1436,6 @@ static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
     w.part_n = (uint32_t*)take(R * S * 32);
     w.list = (u64*)take(R * kList * 8);
     w.gather = (u64*)take(R * kGather * 8);
-    w.above = (double*)take(R * S * 16);
     w.bins = (u64*)take(R * S * kBins * 8);
     if (ws) *ws = w;
     return at;
@@ -1375,10 +1448,6 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
         hipLaunchKernelGGL(pick_small_k<T>, dim3(rows), dim3(kGatherThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
         return;
     }
-    if (rows >= kManyRows) {
-        hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
-        return;
-    }
     PickWs ws;
     pick_carve(rows, vocab, base, &ws);
     PickGeo geo;
@@ -1387,14 +1456,17 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
     constexpr int VEC = RowView<T>::VEC;
     geo.per = ((vocab + 2 * VEC - 2) / VEC + geo.segs - 1) / geo.segs;
     geo.rows_per_seq = rows_per_seq;
-    for (int r0 = 0; r0 < rows; r0 += kBatchRows) {
-        geo.row0 = r0;
-        const dim3 grid((unsigned)(std::min(kBatchRows, rows - r0) * geo.segs));
-        hipLaunchKernelGGL(pick_max_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, ws, out);
-        hipLaunchKernelGGL(pick_weigh_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
-        hipLaunchKernelGGL(pick_gather_k<T>, grid, dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
-        if (out.rows) hipLaunchKernelGGL(pick_mask_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+    if (rows >= kManyRows) {
+        const int segs = out.token && rows <= kMostRows ? geo.segs : 0;
+        hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out, segs, ws);
+        if (segs) hipLaunchKernelGGL(pick_gather_k<T>, dim3((unsigned)(rows * geo.segs)), dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+        return;
     }
+    const dim3 grid((unsigned)(rows * geo.segs));
+    hipLaunchKernelGGL(pick_max_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, ws, out);
+    hipLaunchKernelGGL(pick_weigh_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+    hipLaunchKernelGGL(pick_gather_k<T>, grid, dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+    if (out.rows) hipLaunchKernelGGL(pick_mask_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
 }
 
 hipError_t pick(hipStream_t s, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const PickFilter& filter,

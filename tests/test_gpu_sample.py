@@ -127,12 +127,27 @@ def test_batches_and_trees(B, n, V):
     check_rows(values, asked, n, u, *got)
 
 
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,V", [(112, 5003), (280, 4099), (28, 33000), (3, 33001)])
+def test_rows_by_one_or_several_workgroups(code, kind, rows, V):
+    """Few rows are cut into segments, more of them are a workgroup's, the longest prefixes of up to 256 such rows are cut up again; every setting on every kind of row."""
+    rng = np.random.default_rng(rows + len(kind))
+    x = logits_of(kind, rows, V, rng)
+    u = rng.integers(0, 2 ** 32, rows)
+    asked = asks(rng, 28) * 10
+    values, *got = run(code, x, asked[:rows], 1, u, pad=V % 4)
+    check_rows(values, asked[:rows], 1, u, *got)
+
+
 def test_values_at_the_ends():
     """NaN, infinities, the type's lowest value as a mask, denormals, differences past the weights' range."""
     low, tiny = float(np.finfo(np.float32).min), 1e-42
     rows = [[math.nan, 1.0, 2.0], [1.0, 2.0, math.nan], [INF, 1.0, INF], [-INF, -INF, -INF], [low, low, low], [low, 3.0, low], [tiny, -tiny, 0.0], [3e38, -3e38, 3e38], [0.0, -22.0, -22.5],
             [-INF, 5.0, -INF], [INF, INF, INF], [-INF, low, -INF]]
-    for V in (3, 900, 9000):
+    few = rows
+    for V, times in ((3, 1), (900, 1), (9000, 1), (9000, 9), (9000, 22)):
+        rows = few * times
         x = np.full((len(rows), V), -INF, np.float32)
         x[:, [0, V // 2, V - 1]] = rows
         for ask in (dict(), dict(top_k=2), dict(top_p=0.6), dict(min_p=0.2), dict(tau=0.0), dict(top_k=2, top_p=0.99, min_p=0.01), dict(tau=INF, top_p=0.5), dict(tau=1e-38)):
