@@ -656,25 +656,31 @@ def kv8_read(dtype_code, kv: KV8, first, count, out_k, out_v):
 
 
 # ---- pages, rotary positions, sampling: what a step of a caller with a forward of its own needs around the attention calls
+# (Small calls are bound by the host, so checks are few and cheap: a launch costs 2.6 us, a tensor's check 0.3.)
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 
 def _here(device: int) -> int:
     """The current stream of `device`, which has to be the current one."""
-    assert device == torch.cuda.current_device(), "the tensors lie on another device than the current one"
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+    assert device == _current_device(), "the tensors lie on another device than the current one"
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
-def _at(t: Optional[torch.Tensor], device: int, shape, dtype, name: str):
-    """The address of a contiguous device tensor of this shape and type; None stays None."""
+def _at(t: Optional[torch.Tensor], device: int, count: int, dtype, name: str):
+    """The address of a contiguous device tensor of so many elements of this type; None stays None."""
     if t is None:
         return None
-    assert t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device, f"{name}: a contiguous {dtype} tensor {tuple(shape)} on the device of the others"
+    assert t.dtype is dtype and t.numel() == count and t.is_contiguous() and t.get_device() == device, f"{name}: a contiguous {dtype} tensor of {count} on the device of the others"
     return t.data_ptr()
 
 
 def _row_step(t: torch.Tensor, device: int, rows: int, width: int, dtype, name: str) -> int:
     """Elements between the rows of a tensor [..., width] whose leading dimensions are rows, evenly spaced; checks them."""
-    assert t.dtype is dtype and t.get_device() == device and t.shape[-1] == width and t.numel() == rows * width, f"{name}: {rows} rows of {width} {dtype} on the device of the others"
+    assert t.dtype is dtype and t.get_device() == device and t.size(-1) == width and t.numel() == rows * width, f"{name}: {rows} rows of {width} {dtype} on the device of the others"
+    if t.is_contiguous():
+        return width
     assert width == 1 or t.stride(-1) == 1, f"{name}: elements of a row lie side by side"
     step, expect = width, None
     for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
@@ -691,10 +697,18 @@ def _row_step(t: torch.Tensor, device: int, rows: int, width: int, dtype, name: 
 
 class Pages:
     """The pages of a paged cache (tlt_pages): free_page [n_pages], n_free [1], page_count [B], block_table [B, max_pages], int32 device tensors; block_table is the one
-    that the cache's handle (KV, KV8) holds.  The tensors' addresses and shapes are taken at every call."""
+    that the cache's handle (KV, KV8) holds.  The tensors are checked here and kept; their addresses are taken at every call."""
 
     def __init__(self, free_page: torch.Tensor, n_free: torch.Tensor, page_count: torch.Tensor, block_table: torch.Tensor, page_size: int):
-        self.free_page, self.n_free, self.page_count, self.block_table, self.page_size = free_page, n_free, page_count, block_table, int(page_size)
+        dev = block_table.get_device()
+        assert dev >= 0 and block_table.dim() == 2, "block_table: a device tensor [B, max_pages]"
+        B, max_pages = block_table.shape
+        for name, x, count in (("free_page", free_page, free_page.numel()), ("n_free", n_free, 1), ("page_count", page_count, B), ("block_table", block_table, B * max_pages)):
+            _at(x, dev, count, torch.int32, name)
+        self._tensors, self._sizes, self.device, self.batch = (free_page, n_free, page_count, block_table), (free_page.numel(), max_pages, int(page_size)), dev, B
+
+    free_page, n_free, page_count, block_table = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
+    page_size = property(lambda self: self._sizes[2])
 
     @staticmethod
     def empty(B, n_pages, max_pages, page_size, device="cuda") -> "Pages":
@@ -702,33 +716,30 @@ class Pages:
         i32 = dict(dtype=torch.int32, device=device)
         return Pages(torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32), torch.zeros((B,), **i32), torch.full((B, max_pages), -1, **i32), page_size)
 
-    def c(self):
-        """(the C handle, sequences, device)"""
-        table = self.block_table
-        dev, (B, max_pages) = table.get_device(), table.shape
-        i32 = torch.int32
-        assert dev >= 0, "device tensors"
-        return PagesC(_at(self.free_page, dev, self.free_page.shape[:1], i32, "free_page"), _at(self.n_free, dev, (1,), i32, "n_free"),
-                      _at(self.page_count, dev, (B,), i32, "page_count"), _at(table, dev, (B, max_pages), i32, "block_table"), self.free_page.numel(), max_pages, self.page_size), B, dev
+    def c(self) -> PagesC:
+        free, n_free, count, table = self._tensors
+        return PagesC(free.data_ptr(), n_free.data_ptr(), count.data_ptr(), table.data_ptr(), *self._sizes)
 
 
 def pages_grow(pages: Pages, seq_len, n_new, depth, row_start, row_seq, position, slot, granted):
     """tlt_pages_grow: seq_len, n_new [B] int32; depth [rows] int32 or None; outputs (each may be None) row_start [B + 1], row_seq, position [rows] and granted [B] int32,
     slot [rows] int64, all row tensors of one size."""
-    c, B, dev = pages.c()
-    row_tensors = [t for t in (depth, row_seq, position, slot) if t is not None]
-    rows, i32 = (row_tensors[0].numel() if row_tensors else 0), torch.int32
-    rc = load().tlt_pages_grow(_here(dev), B, c, _at(seq_len, dev, (B,), i32, "seq_len"), _at(n_new, dev, (B,), i32, "n_new"), _at(depth, dev, (rows,), i32, "depth"), rows,
-                               _at(row_start, dev, (B + 1,), i32, "row_start"), _at(row_seq, dev, (rows,), i32, "row_seq"), _at(position, dev, (rows,), i32, "position"),
-                               _at(slot, dev, (rows,), torch.int64, "slot"), _at(granted, dev, (B,), i32, "granted"))
+    dev, B, i32, rows = pages.device, pages.batch, torch.int32, 0
+    for t in (slot, position, row_seq, depth):
+        if t is not None:
+            rows = t.numel()
+            break
+    rc = load().tlt_pages_grow(_here(dev), B, pages.c(), _at(seq_len, dev, B, i32, "seq_len"), _at(n_new, dev, B, i32, "n_new"), _at(depth, dev, rows, i32, "depth"), rows,
+                               _at(row_start, dev, B + 1, i32, "row_start"), _at(row_seq, dev, rows, i32, "row_seq"), _at(position, dev, rows, i32, "position"),
+                               _at(slot, dev, rows, torch.int64, "slot"), _at(granted, dev, B, i32, "granted"))
     if rc:
         raise TltError(rc, "tlt_pages_grow")
 
 
 def pages_release(pages: Pages, keep_len):
     """tlt_pages_release: keep_len [B] int32, or None: everything."""
-    c, B, dev = pages.c()
-    rc = load().tlt_pages_release(_here(dev), B, c, _at(keep_len, dev, (B,), torch.int32, "keep_len"))
+    dev, B = pages.device, pages.batch
+    rc = load().tlt_pages_release(_here(dev), B, pages.c(), _at(keep_len, dev, B, torch.int32, "keep_len"))
     if rc:
         raise TltError(rc, "tlt_pages_release")
 
@@ -750,51 +761,65 @@ class Rope:
 
     def __init__(self, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
         assert freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous() and freq.get_device() >= 0, "freq: a contiguous float64 device tensor"
-        self.freq, self.interleaved, self.amplitude = freq, bool(interleaved), float(amplitude)
+        self._freq, self._rest, self.device = freq, (2 * freq.numel(), int(bool(interleaved)), float(amplitude)), freq.get_device()
+
+    freq = property(lambda self: self._freq)
+    interleaved = property(lambda self: bool(self._rest[1]))
+    amplitude = property(lambda self: self._rest[2])
+
+    def c(self) -> RopeC:
+        return RopeC(self._freq.data_ptr(), *self._rest)
 
 
 def rope_write(dtype_code, n_q_heads, n_kv_heads, head_dim, rope: Rope, qkv, bias, position, slot, kv, layer, q_out, kv_out=None):
     """tlt_rope_write: qkv rows [..., (Hq+2Hkv)*d], evenly spaced; bias [(Hq+2Hkv)*d] or None; position [rows] int32, slot [rows] int64 (None without a cache); kv a KV (pools
     [layers, pages, Hkv, page, d] of dtype_code's type, or one layer's), a KV8 or None, `layer` of it; q_out rows [..., Hq*d] and kv_out rows [..., 2*Hkv*d], each or None."""
-    dev, dt, d = qkv.get_device(), torch_dtype(dtype_code), head_dim
+    dev, dt, d = rope.device, torch_dtype(dtype_code), head_dim
     width, rows = (n_q_heads + 2 * n_kv_heads) * d, position.numel()
     step = _row_step(qkv, dev, rows, width, dt, "qkv")
-    q_step = _row_step(q_out, dev, rows, n_q_heads * d, dt, "q_out") if q_out is not None else 0
-    kv_step = _row_step(kv_out, dev, rows, 2 * n_kv_heads * d, dt, "kv_out") if kv_out is not None else 0
-    assert rope.freq.get_device() == dev, "freq lies on another device"
-    kvc = kv8c = None
-    page = 1
+    q, q_step = (None, 0) if q_out is None else (q_out.data_ptr(), _row_step(q_out, dev, rows, n_q_heads * d, dt, "q_out"))
+    o, o_step = (None, 0) if kv_out is None else (kv_out.data_ptr(), _row_step(kv_out, dev, rows, 2 * n_kv_heads * d, dt, "kv_out"))
+    kvc, kv8c, page = None, None, 1
     if isinstance(kv, KV8):
         _, _, heads, page, pool_d = kv.dims
-        assert (heads, pool_d) == (n_kv_heads, d) and kv.k_pool.get_device() == dev, "the cache's shape and device"
+        assert heads == n_kv_heads and pool_d == d and kv.k_pool.get_device() == dev, "the cache's shape and device"
         kv8c = kv.c(layer)
     elif kv is not None:
-        shape = tuple(kv.k_pool.shape)
-        assert kv.k_pool.dim() in (4, 5) and kv.v_pool.shape == kv.k_pool.shape and (shape[-3], shape[-1]) == (n_kv_heads, d), "the cache's shape"
-        assert all(t.dtype is dt and t.is_contiguous() and t.get_device() == dev for t in (kv.k_pool, kv.v_pool)), "contiguous pools of the model's type on the device of the others"
-        page = shape[-2]
-        if not 0 <= layer < (shape[0] if len(shape) == 5 else 1):
-            raise IndexError(f"layer {layer}")
-        at = layer * shape[-4] * n_kv_heads * page * d * kv.k_pool.element_size()
-        kvc = KVC(kv.k_pool.data_ptr() + at, kv.v_pool.data_ptr() + at, shape[-4], None, None, 0, 0)
-    rc = load().tlt_rope_write(_here(dev), dtype_code, rows, n_q_heads, n_kv_heads, d, page, RopeC(rope.freq.data_ptr(), 2 * rope.freq.numel(), int(rope.interleaved), rope.amplitude),
-                               qkv.data_ptr(), step, _at(bias, dev, (width,), dt, "bias"), _at(position, dev, (rows,), torch.int32, "position"),
-                               _at(slot, dev, (rows,), torch.int64, "slot"), kvc, kv8c, None if q_out is None else q_out.data_ptr(), q_step,
-                               None if kv_out is None else kv_out.data_ptr(), kv_step)
+        k, v = kv.k_pool, kv.v_pool
+        shape = k.shape
+        layers, (n_pages, heads, page, pool_d) = (shape[0] if len(shape) == 5 else 1), shape[-4:]
+        assert len(shape) in (4, 5) and v.shape == shape and heads == n_kv_heads and pool_d == d, "the cache's shape"
+        assert k.dtype is dt and v.dtype is dt and k.is_contiguous() and v.is_contiguous() and k.get_device() == dev and v.get_device() == dev, \
+            "contiguous pools of the model's type on the device of the others"
+        if not 0 <= layer < layers:
+            raise IndexError(f"layer {layer} of {layers}")
+        at = layer * n_pages * heads * page * d * (4 if dtype_code == TLT_F32 else 2)
+        kvc = KVC(k.data_ptr() + at, v.data_ptr() + at, n_pages, None, None, 0, 0)
+    rc = load().tlt_rope_write(_here(dev), dtype_code, rows, n_q_heads, n_kv_heads, d, page, rope.c(), qkv.data_ptr(), step, _at(bias, dev, width, dt, "bias"),
+                               _at(position, dev, rows, torch.int32, "position"), _at(slot, dev, rows, torch.int64, "slot"), kvc, kv8c, q, q_step, o, o_step)
     if rc:
         raise TltError(rc, "tlt_rope_write")
 
 
 class SampleFilter:
-    """tlt_filter: what each sequence asks for, device tensors [B] or None: temperature, top_p, min_p float32, top_k int32."""
+    """tlt_filter: what each sequence asks for, device tensors [B] or None: temperature, top_p, min_p float32, top_k int32.  Checked here and kept; addresses are taken at every call."""
 
     def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
-        self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
+        tensors, self.device, self.batch = (temperature, top_k, top_p, min_p), None, None
+        for name, t, dt in zip(("temperature", "top_k", "top_p", "min_p"), tensors, (torch.float32, torch.int32, torch.float32, torch.float32)):
+            if t is not None:
+                assert t.dim() == 1 and t.get_device() >= 0, f"{name}: a device tensor [B]"
+                if self.batch is None:
+                    self.device, self.batch = t.get_device(), t.numel()
+                _at(t, self.device, self.batch, dt, name)
+        self._tensors = tensors
+
+    temperature, top_k, top_p, min_p = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
     def c(self, B, device) -> FilterC:
-        f32 = torch.float32
-        return FilterC(_at(self.temperature, device, (B,), f32, "temperature"), _at(self.top_k, device, (B,), torch.int32, "top_k"), _at(self.top_p, device, (B,), f32, "top_p"),
-                       _at(self.min_p, device, (B,), f32, "min_p"))
+        assert self.batch is None or (self.batch == B and self.device == device), f"settings of {B} sequences on the device of the others"
+        a, b, c, d = self._tensors
+        return FilterC(a.data_ptr() if a is not None else None, b.data_ptr() if b is not None else None, c.data_ptr() if c is not None else None, d.data_ptr() if d is not None else None)
 
 
 def sample_workspace(rows, vocab) -> torch.Tensor:
@@ -806,31 +831,31 @@ def sample_workspace(rows, vocab) -> torch.Tensor:
 
 def _logit_rows(logits, dtype_code):
     """(device, rows, rows per sequence, sequences, vocab, elements between rows) of logits [B, V] or [B, n, V]."""
-    assert logits.dim() in (2, 3), "logits [B, V] or [B, n, V]"
-    B, V, n = logits.shape[0], logits.shape[-1], logits.shape[1] if logits.dim() == 3 else 1
+    shape = logits.shape
+    assert len(shape) in (2, 3), "logits [B, V] or [B, n, V]"
+    B, V, n = shape[0], shape[-1], shape[1] if len(shape) == 3 else 1
     dev = logits.get_device()
     return dev, B * n, n, B, V, _row_step(logits, dev, B * n, V, torch_dtype(dtype_code), "logits")
 
 
 def sample(dtype_code, logits, asked: SampleFilter, u, token, logprob, kept, ws):
     """tlt_sample: logits [B, V] or [B, n, V] of dtype_code's type (rows evenly spaced, so a slice of wider rows will do), u like logits without V, int32 or uint32;
-    token and kept (may be None) int32 of u's shape, logprob (may be None) float32 [..., 2]."""
+    token and kept (may be None) int32 of u's size, logprob (may be None) float32 [..., 2]."""
     dev, rows, n, B, V, step = _logit_rows(logits, dtype_code)
-    shape = logits.shape[:-1]
-    assert ws.is_contiguous() and ws.get_device() == dev
-    rc = load().tlt_sample(_here(dev), dtype_code, rows, n, V, logits.data_ptr(), step, asked.c(B, dev), _at(u, dev, shape, u.dtype if u.dtype in (torch.int32, torch.uint32) else torch.int32, "u"),
-                           _at(token, dev, shape, torch.int32, "token"), _at(logprob, dev, (*shape, 2), torch.float32, "logprob"), _at(kept, dev, shape, torch.int32, "kept"),
+    assert ws.is_contiguous() and ws.get_device() == dev, "the workspace"
+    rc = load().tlt_sample(_here(dev), dtype_code, rows, n, V, logits.data_ptr(), step, asked.c(B, dev), _at(u, dev, rows, torch.uint32 if u.dtype is torch.uint32 else torch.int32, "u"),
+                           _at(token, dev, rows, torch.int32, "token"), _at(logprob, dev, 2 * rows, torch.float32, "logprob"), _at(kept, dev, rows, torch.int32, "kept"),
                            ws.data_ptr(), ws.numel() * ws.element_size())
     if rc:
         raise TltError(rc, "tlt_sample")
 
 
 def sample_filter(dtype_code, logits, asked: SampleFilter, out, kept, ws):
-    """tlt_sample_filter: out like logits (may be logits itself), kept (may be None) int32 of logits' shape without V."""
+    """tlt_sample_filter: out like logits (may be logits itself), kept (may be None) int32 of logits' size without V."""
     dev, rows, n, B, V, step = _logit_rows(logits, dtype_code)
-    assert out.shape == logits.shape and ws.is_contiguous() and ws.get_device() == dev
+    assert out.shape == logits.shape and ws.is_contiguous() and ws.get_device() == dev, "out like logits, and the workspace"
     rc = load().tlt_sample_filter(_here(dev), dtype_code, rows, n, V, logits.data_ptr(), step, asked.c(B, dev), out.data_ptr(),
-                                  _row_step(out, dev, rows, V, torch_dtype(dtype_code), "out"), _at(kept, dev, logits.shape[:-1], torch.int32, "kept"), ws.data_ptr(), ws.numel() * ws.element_size())
+                                  _row_step(out, dev, rows, V, torch_dtype(dtype_code), "out"), _at(kept, dev, rows, torch.int32, "kept"), ws.data_ptr(), ws.numel() * ws.element_size())
     if rc:
         raise TltError(rc, "tlt_sample_filter")
 
