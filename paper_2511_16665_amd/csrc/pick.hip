@@ -752,10 +752,15 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     }
     const uint32_t n = pr->list_n;
     if (n > 0 && n <= (uint32_t)kList) {
+        double* stored = n <= kList / 2 ? (double*)(local + kList / 2) : nullptr;
 #pragma unroll 4
-        for (uint32_t i = tid; i < n; i += NT) local[i] = ws.list[(int64_t)lr * kList + i];
+        for (uint32_t i = tid; i < n; i += NT) {
+            const u64 e = ws.list[(int64_t)lr * kList + i];
+            local[i] = e;
+            if (stored) stored[i] = w(entry_logit(e));
+        }
         __syncthreads();
-        const TokenList l{local, nullptr, w, (int)n};
+        const TokenList l{local, stored, w, (int)n};
         const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
         if (end != kNoEntry) {
             if (tid == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
@@ -1410,8 +1415,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 // ---- host
 static int pick_segs(int rows, int vocab) {
     if (rows >= kManyRows) return std::max(1, std::min(8, 1 << (31 - __builtin_clz(std::max(1, vocab / 4096)))));   // (of the second list)
-    // some 1024 workgroups, of 4096 tokens at least (so that each of a segment's threads has some)
-    const int most = std::max(1, std::min(1024 / rows, vocab / 4096));
+    // some 512 workgroups (each costs some 10 us of beginning, meeting and end: 64 x 152064 96 us with 1024, 86 with 512, 92 with 256), of 4096 tokens at least (so that each of a segment's threads has some)
+    const int most = std::max(1, std::min(512 / rows, vocab / 4096));
     int segs = 1;
     while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
     return segs;

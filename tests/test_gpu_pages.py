@@ -80,8 +80,8 @@ def test_many_rows_by_many_workgroups(B):
 
 def test_many_pages_given_back():
     rng = np.random.default_rng(1)
-    lens = rng.integers(1, 400, 500)
-    s = Both(pm.state(rng, 500, 1, lens, 401, 3), 1)
+    lens = rng.integers(1, 800, 500)
+    s = Both(pm.state(rng, 500, 1, lens, 801, 3), 1)
     s.release(lens // 3)
     s.release(None)
 
