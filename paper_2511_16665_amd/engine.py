@@ -102,12 +102,14 @@ class Engine:
         self.have_pending = True
 
     # -- one speculative-decoding step
-    def step(self, topk, depth, n_verify, sync=True, logits_out=None, sample=None):
+    def step(self, topk, depth, n_verify, sync=True, logits_out=None, sample=None, asked=None):
         """Runs the four calls.  With sync=True returns (accept_len [B], out_tokens [B, stride]) as
         numpy arrays and keeps the host-side length bounds exact; with sync=False nothing is read
         back and the bounds advance by the largest possible accept length.
         sample = (temperature, u_accept [B, n], u_final [B]) switches the acceptance from greedy to
-        the target-only sampling rule (the drafter's top-k tree stays as it is)."""
+        the target-only sampling rule (the drafter's top-k tree stays as it is); asked (a SampleFilter of B sequences, with
+        `sample` only) reduces the target's distribution to what top-k, top-p and min-p keep of it at the temperature: its own, which is
+        that of `sample`.  Tokens then follow the reduced distribution; the logits kept are the reduced ones."""
         B = self.B
         pool = topk + (depth - 1) * topk * topk if depth >= 1 else 0
         n = min(n_verify, 1 + pool)
@@ -128,6 +130,7 @@ class Engine:
             temperature, u_accept, u_final = sample
             logits = logits_out if logits_out is not None else self.logits(n)
             self.ctx.verify_forward(B, t, self.kv, out_logits=logits, out_argmax=None, out_hidden=hid)
+            self._reduce(logits, n, asked)
             self.ctx.accept(B, 2, temperature, t, logits, None, None, u_accept, u_final, self.stride, self.accept_len,
                             self.path_idx, self.out_tokens, self.n_out)
         self.ctx.kv_commit(B, self.kv, self.accept_len, self.path_idx, self.stride)
@@ -144,11 +147,12 @@ class Engine:
         return al, out
 
     # -- one sampled speculative-decoding step (static template, rejection-sampling acceptance)
-    def step_sampled(self, topk, depth, n_verify, temperature, u_draw, u_accept, u_final):
+    def step_sampled(self, topk, depth, n_verify, temperature, u_draw, u_accept, u_final, asked=None):
         """u_draw, u_accept [B, n] and u_final [B]: uint32 device tensors (as int32 storage) with the
         step's random numbers, n = node count of the template.  Returns (accept_len [B], out_tokens
         [B, stride]) as numpy arrays; the tree, the draft distributions and the target logits of the
-        step stay available as self.tree(n), self.draft_q(n), self.logits(n)."""
+        step stay available as self.tree(n), self.draft_q(n), self.logits(n).  asked (a SampleFilter of B sequences):
+        as in step; rejection sampling against the reduced distribution stays lossless whatever the drafts were drawn from."""
         B = self.B
         n = len(tlt.template_build(topk, depth, n_verify)[0])
         t, q, logits = self.tree(n), self.draft_q(n), self.logits(n)
@@ -161,6 +165,7 @@ class Engine:
                                   u_draw, t, q)
         hid = self._buf("hid", n)
         self.ctx.verify_forward(B, t, self.kv, out_logits=logits, out_argmax=None, out_hidden=hid)
+        self._reduce(logits, n, asked)
         self.ctx.accept(B, 1, temperature, t, logits, None, q, u_accept, u_final, self.stride, self.accept_len,
                         self.path_idx, self.out_tokens, self.n_out)
         self.ctx.kv_commit(B, self.kv, self.accept_len, self.path_idx, self.stride)
@@ -171,6 +176,15 @@ class Engine:
         self.kv.seq_len_bound += inc
         self.pending_max_new = inc
         return al, out
+
+    def _reduce(self, logits, n, asked):
+        """What is not kept of the target's logits [B, n, V] becomes -infinity, in place."""
+        if asked is None:
+            return
+        key = ("reduce", n)
+        if key not in self._trees:
+            self._trees[key] = tlt.sample_workspace(self.B * n, self.cfg.vocab)
+        tlt.sample_filter(tlt.TLT_F32, logits, asked, logits, None, self._trees[key])
 
     def _read_result(self):
         """(accept_len [B], out_tokens [B, stride]) as numpy arrays, in the step's one synchronisation; raises when a kernel saw
