@@ -477,7 +477,7 @@ int tlt_rope_write(void *stream, int dtype, int rows, int n_q_heads, int n_kv_he
  *   of these the ones with W_j >= min_p * 2^32 (rounded down; the first one always).
  * A temperature that is not positive keeps the first token of the order alone, weights as at temperature 1.  A row with a NaN, or with
  * nothing above -infinity, keeps nothing; +infinity is a largest value like any other.  Logits of dtype TLT_F32 or TLT_BF16, rows `row_stride` elements apart (>= vocab); row r belongs
- * to sequence r / rows_per_seq (the nodes of a tree lie side by side).  vocab <= 2^20, rows < 2^23.
+ * to sequence r / rows_per_seq (the nodes of a tree lie side by side).  vocab <= 2^20, rows < 2^22.
  * ws: DEVICE scratch (256-byte aligned) of tlt_sample_workspace_bytes(rows, vocab) bytes; it need not be cleared, and calls that may overlap in
  * time need one each.  The function returns 0 for sizes that the calls refuse. */
 typedef struct tlt_filter {
@@ -496,7 +496,7 @@ int tlt_sample(void *stream, int dtype, int rows, int rows_per_seq, int vocab, c
 
 /* The kept tokens' logits, -infinity in the place of all others (rows that keep nothing are copied): what tlt_accept takes as target_logits so that
  * a tree's tokens follow the FILTERED distribution of the target.  out (dtype, rows out_stride >= vocab elements apart) may be logits itself with the
- * same stride; columns from vocab on are not touched. */
+ * same stride, other overlaps are caller errors; columns from vocab on are not touched. */
 int tlt_sample_filter(void *stream, int dtype, int rows, int rows_per_seq, int vocab, const void *logits, int64_t row_stride, const tlt_filter *filter,
                       void *out, int64_t out_stride, int32_t *out_kept, void *ws, size_t ws_bytes);
 

@@ -1359,15 +1359,16 @@ int tlt_rope_write(void* stream, int dtype, int rows, int n_q_heads, int n_kv_he
 }
 
 constexpr int kMostVocab = 1 << 20;   // a row's sum of weights stays below 2^53, where doubles are exact
+constexpr int kMostPickRows = 1 << 22;   // (a workgroup of 1024 threads each: a launch holds fewer than 2^32 threads)
 
 size_t tlt_sample_workspace_bytes(int rows, int vocab) {
-    if (rows < 1 || rows >= (1 << 23) || vocab < 1 || vocab > kMostVocab) return 0;
+    if (rows < 1 || rows >= kMostPickRows || vocab < 1 || vocab > kMostVocab) return 0;
     return pick_workspace_bytes(rows, vocab);
 }
 
 static int run_pick(void* stream, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const tlt_filter* filter,
                     const PickOut& out, void* ws, size_t ws_bytes) {
-    if ((dtype != TLT_F32 && dtype != TLT_BF16) || rows < 1 || rows >= (1 << 23) || rows_per_seq < 1 || rows % rows_per_seq || vocab < 1 || vocab > kMostVocab ||
+    if ((dtype != TLT_F32 && dtype != TLT_BF16) || rows < 1 || rows >= kMostPickRows || rows_per_seq < 1 || rows % rows_per_seq || vocab < 1 || vocab > kMostVocab ||
         !logits || row_stride < vocab || !filter || !ws || ((uintptr_t)ws & 255) != 0)
         return TLT_EINVAL;
     if ((((uintptr_t)logits | (uintptr_t)out.rows) & (dtype == TLT_F32 ? 3 : 1)) != 0) return TLT_EINVAL;

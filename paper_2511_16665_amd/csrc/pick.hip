@@ -23,7 +23,7 @@ typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
-constexpr int kManyRows = 96;                        // from here on a row is one workgroup's
+constexpr int kManyRows = 129;                       // from here on a row is one workgroup's
 constexpr int kMostRows = 256;                       // up to here its long prefixes are shared out among several (one row on each CU)
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
@@ -33,7 +33,7 @@ constexpr int kGather = 8192;                        // entries of the second li
 constexpr int kSmall = 4096;                         // vocabularies up to here are one list
 // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
 constexpr int kGroups = 3, kListed = 64 << (kGroups - 1);   // and the largest top_k that lists are made for
-constexpr int kInFlight = 4;                         // 16-byte pieces a lane asks for at once
+constexpr int kInFlight = 2;                         // 16-byte pieces a lane asks for at once
 constexpr u64 kNoEntry = ~0ull;
 
 // order of logits as whole numbers; -0 and +0 are equal
@@ -159,13 +159,23 @@ struct RowView {
     }
     // f(piece, values) for pieces `from`, from + step, .. below `end`, kInFlight of them loaded at once; pieces at `end` and behind it come as -infinity (f is called by whole
     // waves, whose lanes hold consecutive pieces).  The row has a piece that lies inside.
-    template <typename F>
+    template <bool AHEAD = false, typename F>
     __device__ __forceinline__ void each(int from, int step, int end, F f) const {
         const int lane = threadIdx.x & 63, in0 = off ? 1 : 0, in1 = (V + off) / VEC;   // pieces in0 .. in1 - 1 lie inside
-        for (int c = from; c - lane < end; c += kInFlight * step) {
-            u32x4_t w[kInFlight];
+        u32x4_t w[kInFlight], next[kInFlight];
+        auto ask = [&](int c, u32x4_t (&w)[kInFlight]) {
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) w[u] = raw(min(max(c + u * step, in0), in1 - 1));
+        };
+        if (AHEAD) ask(from, next);
+        for (int c = from; c - lane < end; c += kInFlight * step) {
+            if (AHEAD) {
+#pragma unroll
+                for (int u = 0; u < kInFlight; ++u) w[u] = next[u];
+                ask(c + kInFlight * step, next);   // (held inside the row)
+            } else {
+                ask(c, w);
+            }
             if (c - lane < in0 || c - lane + (kInFlight - 1) * step + 63 >= min(end, in1)) {   // (uniform over the wave)
                 const int behind = in1 * VEC < V + off ? in1 : -1;   // the piece behind the last whole one
                 u32x4_t part = {};
@@ -406,11 +416,16 @@ struct PickGeo {
     int rows_per_seq;
 };
 
-// The workgroup that is the last of `total` of a row to come here sees what all of them wrote (every wave waits for its stores, then one thread releases them).
+// What one workgroup of a row leaves for another of the same launch goes past the caches of an XCD, both ways, so that nothing has to be written back or dropped where they meet.
+template <typename V>
+__device__ __forceinline__ void leave(V* to, V v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V>
+__device__ __forceinline__ V left(const V* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// The workgroup that is the last of `total` of a row to come here sees what all of them left (every wave waits until its stores are done, then one thread counts).
 __device__ __forceinline__ bool last_here(uint32_t* seen, int total, int* flag) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(seen, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)total - 1u;
+    if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(seen, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)total - 1u;
     __syncthreads();
     return *flag != 0;
 }
@@ -671,7 +686,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     uint32_t kept_n = 0;
     u64* listing = local + wave * kWaveList;   // the wave's own list: no counter is shared while the segment is read
     uint32_t listed = 0;
-    row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
+    row.template each<true>(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
         double weight[VEC];
         if (weigh_all) {
 #pragma unroll
@@ -710,26 +725,32 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         }
     });
     whole = block_sum<NT>(whole, tmp);
-    if (tid == 0) ws.whole[lr * geo.segs + g] = whole;
+    if (tid == 0) leave(ws.whole + lr * geo.segs + g, whole);
     if (!prefix) {
         kept = wave_sum_d(kept);
         for (int o = 32; o > 0; o >>= 1) kept_n += __shfl_xor(kept_n, o, 64);
-        if (lane == 0) ws.part[(lr * geo.segs + g) * 8 + wave] = kept, ws.part_n[(lr * geo.segs + g) * 8 + wave] = kept_n;
+        if (lane == 0) leave(ws.part + (lr * geo.segs + g) * 8 + wave, kept), leave(ws.part_n + (lr * geo.segs + g) * 8 + wave, kept_n);
     } else {
         uint32_t base = 0;
         if (lane == 0) base = atomicAdd(&pr->list_n, listed > (uint32_t)kWaveList ? 1u << 20 : listed);
         base = __builtin_amdgcn_readfirstlane(base);
         listed = min(listed, (uint32_t)kWaveList);
         for (uint32_t i = lane; i < listed; i += 64)
-            if (base + i < (uint32_t)kList) ws.list[(int64_t)lr * kList + base + i] = listing[i];
+            if (base + i < (uint32_t)kList) leave(ws.list + (int64_t)lr * kList + base + i, listing[i]);
         __syncthreads();   // (the bins)
         if (use_bins)
-            for (int i = tid; i < kBins; i += NT) ws.bins[((int64_t)lr * geo.segs + g) * kBins + i] = lds.bins[i];
+            for (int i = tid; i < kBins; i += NT) leave(ws.bins + ((int64_t)lr * geo.segs + g) * kBins + i, lds.bins[i]);
     }
     if (!last_here(&pr->seen_weigh, geo.segs, &flag)) return;
 
-    // ---- the row's last workgroup
-    whole = wave_sum_d(lane < geo.segs ? ws.whole[lr * geo.segs + lane] : 0.0);
+    // ---- the row's last workgroup.  (The list's beginning is asked for together with its length.)
+    constexpr int kEarly = 8;
+    u64 early[kEarly];
+    if (prefix) {
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) early[i] = left(ws.list + (int64_t)lr * kList + i * NT + tid);
+    }
+    whole = wave_sum_d(lane < geo.segs ? left(ws.whole + lr * geo.segs + lane) : 0.0);
     if (tid == 0) pr->whole = whole;
     FindLds& find = lds.find;
     if (!prefix) {
@@ -738,8 +759,8 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         // the wave's range that holds the draw
         static_assert(kSegsMost * 8 <= NT, "a range per thread");
         const bool is = tid < geo.segs * 8 && (tid & 7) < NW;
-        const double mine = is ? ws.part[lr * geo.segs * 8 + tid] : 0.0;
-        const double S = block_sum<NT>(mine, tmp), count = block_sum<NT>(is ? (double)ws.part_n[lr * geo.segs * 8 + tid] : 0.0, tmp);
+        const double mine = is ? left(ws.part + lr * geo.segs * 8 + tid) : 0.0;
+        const double S = block_sum<NT>(mine, tmp), count = block_sum<NT>(is ? (double)left(ws.part_n + lr * geo.segs * 8 + tid) : 0.0, tmp);
         if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
         const double aim = aim_of(out.u[r], S);
         double base;
@@ -750,15 +771,17 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
         return;
     }
-    const uint32_t n = pr->list_n;
+    const uint32_t n = left(&pr->list_n);
     if (n > 0 && n <= (uint32_t)kList) {
         double* stored = n <= kList / 2 ? (double*)(local + kList / 2) : nullptr;
-#pragma unroll 4
-        for (uint32_t i = tid; i < n; i += NT) {
-            const u64 e = ws.list[(int64_t)lr * kList + i];
-            local[i] = e;
-            if (stored) stored[i] = w(entry_logit(e));
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) {
+            if ((uint32_t)(i * NT + tid) < n) local[i * NT + tid] = early[i];
+            if (stored && (uint32_t)(i * NT + tid) < n) stored[i * NT + tid] = w(entry_logit(early[i]));
         }
+        static_assert(kList <= 2 * kEarly * NT, "weights are stored for early ones alone");
+#pragma unroll 4
+        for (uint32_t i = kEarly * NT + tid; i < n; i += NT) local[i] = left(ws.list + (int64_t)lr * kList + i);
         __syncthreads();
         const TokenList l{local, stored, w, (int)n};
         const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
@@ -782,7 +805,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     for (int i = 0; i < geo.segs; ++i) {
         const u64* from_seg = ws.bins + ((int64_t)lr * geo.segs + i) * kBins + OWN * tid;
 #pragma unroll
-        for (int k = 0; k < OWN; ++k) own[k] += from_seg[k];
+        for (int k = 0; k < OWN; ++k) own[k] += left(from_seg + k);
     }
     double mine = 0.0;
 #pragma unroll
@@ -937,7 +960,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         if (tid == 0) local_n = 0;
         __syncthreads();
         SparseSum above{sparse[wave], ask.least};
-        row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
+        row.template each<true>(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const int b = bin_of(w, x[e], per_logit);
@@ -949,15 +972,15 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         });
         above.finish(w);
         const double kept = wave_sum_d(above.sum), kept_n = wave_sum_d((double)above.count);
-        if (lane == 0) ws.part[lr * ranges + g * 8 + wave] = kept, ws.part_n[lr * ranges + g * 8 + wave] = (uint32_t)kept_n;
+        if (lane == 0) leave(ws.part + lr * ranges + g * 8 + wave, kept), leave(ws.part_n + lr * ranges + g * 8 + wave, (uint32_t)kept_n);
         __syncthreads();
         if (tid == 0) base_n = atomicAdd(&pr->gather_n, local_n > (uint32_t)kGather ? 1u << 20 : local_n);
         __syncthreads();
         const uint32_t mine_n = min(local_n, (uint32_t)kGather), at = base_n;
         for (uint32_t i = tid; i < mine_n; i += NT)
-            if (at + i < (uint32_t)kGather) ws.gather[(int64_t)lr * kGather + at + i] = local[i];
+            if (at + i < (uint32_t)kGather) leave(ws.gather + (int64_t)lr * kGather + at + i, local[i]);
         if (!last_here(&pr->seen_gather, geo.segs, &flag)) return;
-        const uint32_t n = pr->gather_n;
+        const uint32_t n = left(&pr->gather_n);
         if (n > 0 && n <= (uint32_t)kGather) {
             if (tid == 0) find.bins[0] = kNoEntry, find.bins[1] = 0;
             __syncthreads();
@@ -965,7 +988,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
             u64 first = kNoEntry, last = 0;
 #pragma unroll 4
             for (uint32_t i = tid; i < n; i += NT) {
-                const u64 e = ws.gather[(int64_t)lr * kGather + i];
+                const u64 e = left(ws.gather + (int64_t)lr * kGather + i);
                 local[i] = e;
                 if (stored) stored[i] = w(entry_logit(e));
                 first = min(first, e), last = max(last, e);
@@ -990,8 +1013,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
                 }
                 // the listed ones join the sums of their ranges
                 static_assert(kSegsMost * 8 <= NT, "a range per thread");
-                if (tid < ranges) part[tid] = ws.part[lr * ranges + tid];
-                double count = tid < ranges ? (double)ws.part_n[lr * ranges + tid] : 0.0;
+                if (tid < ranges) part[tid] = left(ws.part + lr * ranges + tid);
+                double count = tid < ranges ? (double)left(ws.part_n + lr * ranges + tid) : 0.0;
                 __syncthreads();
                 for (uint32_t i = tid; i < n; i += NT)
                     if (local[i] <= end && l.weight(i) >= ask.least) {

@@ -110,6 +110,8 @@ class Engine:
         the target-only sampling rule (the drafter's top-k tree stays as it is); asked (a SampleFilter of B sequences, with
         `sample` only) reduces the target's distribution to what top-k, top-p and min-p keep of it at the temperature: its own, which is
         that of `sample`.  Tokens then follow the reduced distribution; the logits kept are the reduced ones."""
+        if asked is not None and sample is None:
+            raise ValueError("asked: a greedy step has no distribution to reduce")
         B = self.B
         pool = topk + (depth - 1) * topk * topk if depth >= 1 else 0
         n = min(n_verify, 1 + pool)
@@ -184,7 +186,8 @@ class Engine:
         key = ("reduce", n)
         if key not in self._trees:
             self._trees[key] = tlt.sample_workspace(self.B * n, self.cfg.vocab)
-        tlt.sample_filter(tlt.TLT_F32, logits, asked, logits, None, self._trees[key])
+        rows = logits.view(self.B, n, self.cfg.vocab)
+        tlt.sample_filter(tlt.TLT_F32, rows, asked, rows, None, self._trees[key])
 
     def _read_result(self):
         """(accept_len [B], out_tokens [B, stride]) as numpy arrays, in the step's one synchronisation; raises when a kernel saw

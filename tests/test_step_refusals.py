@@ -97,7 +97,7 @@ def mask(**over):
 
 @pytest.mark.parametrize("call", [sample, mask])
 def test_sampling(call):
-    for over in (dict(dtype=2), dict(rows=0), dict(rows=1 << 23, per=1), dict(per=0), dict(per=4), dict(V=0), dict(V=(1 << 20) + 1, step=1 << 25), dict(logits=None), dict(logits=P + 2), dict(step=999), dict(f=None),
+    for over in (dict(dtype=2), dict(rows=0), dict(rows=1 << 22, per=1), dict(per=0), dict(per=4), dict(V=0), dict(V=(1 << 20) + 1, step=1 << 25), dict(logits=None), dict(logits=P + 2), dict(step=999), dict(f=None),
                  dict(ws=None), dict(ws=P + 16)):
         assert call(**over) == -1, over
     assert call(bytes=16) == -2
@@ -109,5 +109,11 @@ def test_sampling_outputs():
     assert mask(out=None) == mask(out_step=999) == mask(out=2 * P + 2) == -1
     assert mask(out=P, step=1004, out_step=1000) == -1                                   # in place, but with other rows
     size = tlt.load().tlt_sample_workspace_bytes
-    assert size(0, 10) == size(10, 0) == size(1 << 23, 10) == size(1, (1 << 20) + 1) == 0
-    assert size(1, 1) > 0 and size(1536, 152064) > 0 and size((1 << 23) - 1, 1 << 20) > 0
+    assert size(0, 10) == size(10, 0) == size(1 << 22, 10) == size(1, (1 << 20) + 1) == 0
+    assert size(1, 1) > 0 and size(1536, 152064) > 0 and size((1 << 22) - 1, 1 << 20) > 0
+
+
+def test_a_greedy_engine_step_takes_no_filter():
+    from paper_2511_16665_amd.engine import Engine
+    with pytest.raises(ValueError):
+        Engine.step(None, 4, 4, 8, asked=object())
