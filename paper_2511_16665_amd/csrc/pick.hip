@@ -23,8 +23,7 @@ typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
-constexpr int kManyRows = 129;                       // from here on a row is one workgroup's
-constexpr int kMostRows = 256;                       // up to here its long prefixes are shared out among several (one row on each CU)
+constexpr int kFewRows = 256;                         // up to here a row is cut into segments; more rows are a workgroup's each
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
@@ -430,13 +429,14 @@ __device__ __forceinline__ bool last_here(uint32_t* seen, int total, int* flag) 
     return *flag != 0;
 }
 
-// the bin of a logit, for rows whose bins span `reach` (nats times tau); at or past kBins: below them
-__device__ __forceinline__ float bins_per_logit(const Asked& ask, int V) {
+// bins per logit, downwards from the largest one; at or past kBins a token is below them.  likely: how far down a thousand or two of the tokens reach.
+__device__ __forceinline__ float bins_per_logit(const Asked& ask, int V, float likely) {
     // tokens whose weight is below (1 - p) 2^32 / V cannot be in the shortest prefix of weight p S, as S >= 2^32 and together they are less than (1 - p) S; otherwise
-    // down to where weights are 0
-    double reach = 23.0;
-    if (ask.top_k == 0) reach = fmin(reach, 0.01 + log((double)V / fmax(1.0 - (double)ask.top_p * 0x1p-31, 1e-10)));
-    return (float)fmin((double)kBins / (reach * ask.tau), 1e30);
+    // down to where weights are 0, and for a number of tokens, which may be many of those, to where most tokens are (four times as far as the likely ones, in a bell)
+    double reach = 23.0 * ask.tau;
+    if (ask.top_k == 0) reach = fmin(reach, ask.tau * (0.01 + log((double)V / fmax(1.0 - (double)ask.top_p * 0x1p-31, 1e-10))));
+    else if (likely > 0.f) reach = fmax(reach, 4.0 * (double)likely);
+    return (float)fmin((double)kBins / reach, 1e30);
 }
 __device__ __forceinline__ int bin_of(const Weigh& w, float x, float per_logit) { return (int)fminf(w.distance(x) * per_logit, 1e6f); }
 
@@ -633,8 +633,9 @@ __device__ __forceinline__ Asked asked_of_row(const PickGeo& geo, const PickWs& 
 }
 
 // A logit that at least `rank` tokens reach, by the groups that fit what is asked for.
-__device__ __forceinline__ float reached(const PickGeo& geo, const PickWs& ws, int lr, const Asked& ask, int& rank) {
-    const int lane = threadIdx.x & 63, at = (lr * geo.segs + lane) * kGroups + (ask.top_k <= 64 ? 0 : ask.top_k <= 128 ? 1 : 2);
+__device__ __forceinline__ int level_of(const Asked& ask) { return ask.top_k <= 64 ? 0 : ask.top_k <= 128 ? 1 : 2; }
+__device__ __forceinline__ float reached(const PickGeo& geo, const PickWs& ws, int lr, int level, int& rank) {
+    const int lane = threadIdx.x & 63, at = (lr * geo.segs + lane) * kGroups + level;
     const float least = lane < geo.segs ? ws.reach[at] : INFINITY;
     rank = (int)wave_sum(lane < geo.segs ? (float)ws.groups[at] : 0.f);
     return fmaxf(-wave_max(-least), -FLT_MAX);
@@ -668,10 +669,10 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     const bool prefix = ask.prefix();
     // tokens from `from` on go to the list
     int rank = 0;
-    float from = prefix ? reached(geo, ws, lr, ask, rank) : INFINITY;
+    float from = prefix ? reached(geo, ws, lr, level_of(ask), rank) : INFINITY;
     const bool count_bins = ask.top_k > min(rank, kListed), use_bins = prefix && (count_bins || ask.top_k == 0);
+    const float per_logit = use_bins ? bins_per_logit(ask, geo.V, w.distance(from)) : 0.f;
     if (count_bins) from = INFINITY;   // (no list reaches that far)
-    const float per_logit = use_bins ? bins_per_logit(ask, geo.V) : 0.f;
     const bool weigh_all = out.token ? !prefix || use_bins || out.logprob : use_bins;
     if (!prefix && !weigh_all) {   // (a filtered row without a prefix: what it keeps is known)
         if (g == 0 && tid == 0) pr->state = kDone, pr->cut = kKeyNothing, pr->last = -1;
@@ -954,7 +955,8 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     const double whole = pr->whole;
     const int wper = (geo.per + NW - 1) / NW, ranges = geo.segs * 8;
     if (state != kStepwise) {
-        const float per_logit = bins_per_logit(ask, geo.V);
+        int rank;
+        const float per_logit = bins_per_logit(ask, geo.V, w.distance(reached(geo, ws, lr, level_of(ask), rank)));
         const int lo = pr->bin_lo, hi = pr->bin_hi;
         const int seg_end = min(row.pieces(), (g + 1) * geo.per), c0 = min(seg_end, g * geo.per + wave * wper), c1 = min(seg_end, c0 + wper);
         if (tid == 0) local_n = 0;
@@ -980,28 +982,32 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         for (uint32_t i = tid; i < mine_n; i += NT)
             if (at + i < (uint32_t)kGather) leave(ws.gather + (int64_t)lr * kGather + at + i, local[i]);
         if (!last_here(&pr->seen_gather, geo.segs, &flag)) return;
+        constexpr int kEarly = 2;   // (asked for together with the list's length)
+        u64 early[kEarly];
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) early[i] = left(ws.gather + (int64_t)lr * kGather + i * NT + tid);
         const uint32_t n = left(&pr->gather_n);
         if (n > 0 && n <= (uint32_t)kGather) {
-            if (tid == 0) find.bins[0] = kNoEntry, find.bins[1] = 0;
-            __syncthreads();
             double* stored = n <= kGather / 2 ? (double*)(local + kGather / 2) : nullptr;
-            u64 first = kNoEntry, last = 0;
+#pragma unroll
+            for (int i = 0; i < kEarly; ++i)
+                if ((uint32_t)(i * NT + tid) < n) {
+                    local[i * NT + tid] = early[i];
+                    if (stored) stored[i * NT + tid] = w(entry_logit(early[i]));
+                }
 #pragma unroll 4
-            for (uint32_t i = tid; i < n; i += NT) {
+            for (uint32_t i = kEarly * NT + tid; i < n; i += NT) {
                 const u64 e = left(ws.gather + (int64_t)lr * kGather + i);
                 local[i] = e;
                 if (stored) stored[i] = w(entry_logit(e));
-                first = min(first, e), last = max(last, e);
             }
-            if (last) atomicMin(&find.bins[0], first), atomicMax(&find.bins[1], last);
-            __syncthreads();
-            first = find.bins[0], last = find.bins[1];
             __syncthreads();
             const TokenList l{local, stored, w, (int)n};
             if (state == kByNumber) ask.top_p = 1u << 31;
             if (state == kAllDownTo && ask.top_k > (int)n) ask.top_k = 0;   // (tokens without weight fill it up)
             const double before = pr->before;
-            const u64 end = end_in_list<NT>(l, (int)n, ask, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, entry_logit(first), entry_logit(last), find, tmp);
+            const u64 end = end_in_list<NT>(l, (int)n, ask, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit,
+                                            find, tmp);
             if (end != kNoEntry) {
                 const Kept in{~(uint32_t)(end >> 32), (int)(uint32_t)end, ask.least};
                 if (tid == 0) pr->cut = in.cut, pr->last = in.last;
@@ -1122,10 +1128,9 @@ __device__ __attribute__((noinline)) u64 cut_stepwise_apart(const RowView<T> row
 }
 __device__ __attribute__((noinline)) void put_token_apart(int32_t* token, float* logprob, const Weigh w, const Drawn& d, double whole) { put_token(token, logprob, w, d, whole); }
 
-// ---- many rows: a workgroup each, which does everything without meeting another one.  segs > 0: but for rows whose prefix the list does not hold, which are left to
-// pick_gather_k, with what it needs to know in ws.
+// ---- many rows: a workgroup each, which does everything without meeting another one.
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out, int segs, PickWs ws) {
+__global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kRowThreads, NW = NT / 64, kWaveList = kGather / NW;
     __shared__ u64 list[kGather];         // waves' lists of likely tokens, put together; then the bin's tokens
     __shared__ u64 bins[kBins];
@@ -1168,8 +1173,6 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
 #pragma unroll
     for (int v = 1; v < NW; ++v) top = top != top || wave_top[v] != wave_top[v] ? NAN : fmaxf(top, wave_top[v]), tokens += wave_n[v];
     T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
-    PickRow* pr = ws.row + r;
-    if (segs && tid == 0) pr->state = kDone, pr->gather_n = pr->seen_gather = 0;
     if (top != top || top == -INFINITY) {   // (uniform)
         if (o && o != row.row) mask_row<T>(row, o, tid, NT, pieces, Weigh(0.f, 1.0), Kept{0, 0, 0.0}, true);
         if (tid == 0) put_nothing(out, r, top != top);
@@ -1184,15 +1187,15 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
     bool by_ranges = !prefix;              // the draw goes by the sums over the waves' ranges
     double kept = 0.0, count = 0.0;
     if (prefix) {
-        const int level = ask.top_k <= 64 ? 0 : ask.top_k <= 128 ? 1 : 2;
+        const int level = level_of(ask);
         int rank = 0;
         float from = INFINITY;
 #pragma unroll
         for (int v = 0; v < NW; ++v) rank += wave_groups[level][v], from = fminf(from, wave_reach[level][v]);
         from = fmaxf(from, -FLT_MAX);
         const bool count_bins = ask.top_k > min(rank, kListed), use_bins = count_bins || ask.top_k == 0;
+        const float per_logit = use_bins ? bins_per_logit(ask, V, w.distance(from)) : 0.f;
         if (count_bins) from = INFINITY;
-        const float per_logit = use_bins ? bins_per_logit(ask, V) : 0.f;
         const bool weigh_all = use_bins || out.logprob;
         if (use_bins)
             for (int i = tid; i < kBins; i += NT) bins[i] = 0;
@@ -1268,11 +1271,6 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                 before = 0.0, lo = 0, hi = found ? hi : kBins - 1;
             }
             __syncthreads();
-        }
-        if (segs && state != kDone) {
-            if (tid < segs) ws.top[r * segs + tid] = top, ws.tokens[r * segs + tid] = tid == 0 ? tokens : 0;
-            if (tid == 0) pr->state = state, pr->bin_lo = lo, pr->bin_hi = hi, pr->before = before, pr->whole = whole;
-            return;
         }
         if (state == kByNumber || state == kByWeight || state == kAllDownTo) {
             if (tid == 0) count_n = 0;
@@ -1437,15 +1435,14 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 
 // ---- host
 static int pick_segs(int rows, int vocab) {
-    if (rows >= kManyRows) return std::max(1, std::min(8, 1 << (31 - __builtin_clz(std::max(1, vocab / 4096)))));   // (of the second list)
     // some 512 workgroups (each costs some 10 us of beginning, meeting and end: 64 x 152064 96 us with 1024, 86 with 512, 92 with 256), of 4096 tokens at least (so that each of a segment's threads has some)
-    const int most = std::max(1, std::min(512 / rows, vocab / 4096));
+    const int most = std::max(1, std::min(1024 / rows, vocab / 4096));
     int segs = 1;
     while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
     return segs;
 }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
-    if (vocab <= kSmall || rows > kMostRows) return 256;
+    if (vocab <= kSmall || rows > kFewRows) return 256;
     const size_t R = (size_t)rows, S = (size_t)pick_segs(rows, vocab);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -1476,6 +1473,10 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
         hipLaunchKernelGGL(pick_small_k<T>, dim3(rows), dim3(kGatherThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
         return;
     }
+    if (rows > kFewRows) {
+        hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
+        return;
+    }
     PickWs ws;
     pick_carve(rows, vocab, base, &ws);
     PickGeo geo;
@@ -1484,12 +1485,6 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
     constexpr int VEC = RowView<T>::VEC;
     geo.per = ((vocab + 2 * VEC - 2) / VEC + geo.segs - 1) / geo.segs;
     geo.rows_per_seq = rows_per_seq;
-    if (rows >= kManyRows) {
-        const int segs = out.token && rows <= kMostRows ? geo.segs : 0;
-        hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out, segs, ws);
-        if (segs) hipLaunchKernelGGL(pick_gather_k<T>, dim3((unsigned)(rows * geo.segs)), dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
-        return;
-    }
     const dim3 grid((unsigned)(rows * geo.segs));
     hipLaunchKernelGGL(pick_max_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, ws, out);
     hipLaunchKernelGGL(pick_weigh_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);

@@ -129,15 +129,30 @@ def test_batches_and_trees(B, n, V):
 
 @pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("rows,V", [(112, 5003), (280, 4099), (28, 33000), (3, 33001)])
+@pytest.mark.parametrize("rows,V", [(112, 5003), (280, 4099), (280, 9001), (28, 33000), (3, 33001)])
 def test_rows_by_one_or_several_workgroups(code, kind, rows, V):
-    """Few rows are cut into segments, more of them are a workgroup's, the longest prefixes of up to 256 such rows are cut up again; every setting on every kind of row."""
+    """Few rows are cut into segments, more of them are a workgroup's; every setting on every kind of row."""
     rng = np.random.default_rng(rows + len(kind))
     x = logits_of(kind, rows, V, rng)
     u = rng.integers(0, 2 ** 32, rows)
     asked = asks(rng, 28) * 10
     values, *got = run(code, x, asked[:rows], 1, u, pad=V % 4)
     check_rows(values, asked[:rows], 1, u, *got)
+
+
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+@pytest.mark.parametrize("rows", [8, 264])
+def test_more_tokens_asked_for_than_weigh_anything(code, rows):
+    """At a low temperature most of the first top_k tokens weigh nothing: they are kept all the same, but never drawn."""
+    rng = np.random.default_rng(rows)
+    V = 20011
+    x = logits_of("peaks", rows, V, rng)
+    u = rng.integers(0, 2 ** 32, rows)
+    u[:2] = 0, 2 ** 32 - 1
+    asked = [dict(tau=0.05, top_k=4000), dict(tau=0.05, top_k=4000, top_p=0.9), dict(tau=0.02, top_k=15000, min_p=1e-6), dict(tau=0.1, top_k=19999), dict(tau=0.05, top_k=300),
+             dict(tau=0.3, top_k=9000, top_p=0.999999), dict(tau=1e-3, top_k=20010), dict(tau=2.5, top_k=12000, top_p=0.95)] * (rows // 8)
+    values, *got = run(code, x, asked, 1, u)
+    check_rows(values, asked, 1, u, *got)
 
 
 def test_values_at_the_ends():
