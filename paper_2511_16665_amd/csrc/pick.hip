@@ -23,7 +23,8 @@ typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
-constexpr int kFewRows = 256;                         // up to here a row is cut into segments; more rows are a workgroup's each
+constexpr int kPassRows = 1024;                      // rows that the segments' kernels take at a time
+constexpr int kFewRows = 256;                        // from there on filtered rows are a workgroup's each
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
@@ -412,7 +413,7 @@ struct PickWs {
 };
 struct PickGeo {
     int V, segs, per;         // per: pieces of a segment
-    int rows_per_seq;
+    int rows_per_seq, row0;   // row0: first row of this launch
 };
 
 // What one workgroup of a row leaves for another of the same launch goes past the caches of an XCD, both ways, so that nothing has to be written back or dropped where they meet.
@@ -566,8 +567,8 @@ __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T
     constexpr int VEC = RowView<T>::VEC, NW = kWeighThreads / 64;
     __shared__ float wave_top[NW], wave_reach[kGroups][NW];
     __shared__ uint32_t wave_groups[kGroups][NW], wave_tokens[NW];
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, wave = tid >> 6;
-    const RowView<T> row(logits + (int64_t)lr * row_stride, geo.V);
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, wave = tid >> 6, r = geo.row0 + lr;
+    const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     float top = -INFINITY;
     bool nan = false;
     uint32_t tokens = 0;
@@ -613,7 +614,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_max_k(PickGeo geo, const T
         if (g == 0) {
             PickRow z{};
             ws.row[lr] = z;
-            if (out.rows && out.kept) out.kept[lr] = 0;
+            if (out.rows && out.kept) out.kept[r] = 0;
         }
     }
 }
@@ -626,7 +627,7 @@ __device__ __forceinline__ float row_top(const PickGeo& geo, const PickWs& ws, i
 }
 
 __device__ __forceinline__ Asked asked_of_row(const PickGeo& geo, const PickWs& ws, int lr, const PickFilter& filter) {
-    const Wish wish(filter, (lr) / geo.rows_per_seq);
+    const Wish wish(filter, (geo.row0 + lr) / geo.rows_per_seq);
     const int lane = threadIdx.x & 63;
     const float n = wave_sum(lane < geo.segs ? (float)ws.tokens[lr * geo.segs + lane] : 0.f);   // (2^20 at most: exact)
     return wish.asked((int)n);
@@ -653,7 +654,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     __shared__ double tmp[16];
     __shared__ Drawn drawn;
     __shared__ int flag;
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     PickRow* pr = ws.row + lr;
     const float top = row_top(geo, ws, lr);
@@ -944,7 +945,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     __shared__ float sparse[NW][128];
     __shared__ uint32_t local_n, base_n;
     __shared__ int flag;
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = geo.row0 + lr;
     PickRow* pr = ws.row + lr;
     const int state = pr->state;
     if (state == kDone || (state == kStepwise && g != 0)) return;
@@ -1096,7 +1097,7 @@ template <typename T>
 __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const T* logits, int64_t row_stride, PickFilter filter, PickWs ws, PickOut out) {
     constexpr int NT = kWeighThreads;
     __shared__ double tmp[16];
-    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, r = lr;
+    const int lr = blockIdx.x / geo.segs, g = blockIdx.x - lr * geo.segs, r = geo.row0 + lr;
     const RowView<T> row(logits + (int64_t)r * row_stride, geo.V);
     const Asked ask = Wish(filter, r / geo.rows_per_seq).asked(geo.V);   // (its least weight)
     const PickRow& pr = ws.row[lr];
@@ -1108,43 +1109,32 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
     if (threadIdx.x == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
 }
 
-// The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (filtered rows 32 x 48 770 us, 975 with them inlined; the kernels with fewer threads are better
+// The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (32 x 48 rows of 152064 770 us, 975 with them inlined; the kernels with fewer threads are better
 // off inlined).
 template <int NT>
 __device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
     return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, s, tmp);
 }
-template <int NT>
-__device__ __attribute__((noinline)) void draw_from_list_apart(const TokenList l, u64 end, double least, int V, FindLds& s, double* tmp, int32_t* kept, uint32_t u, Drawn* drawn) {
-    draw_from_list<NT>(l, end, least, V, s, tmp, kept, u, drawn);
-}
-template <int NT, typename T>
-__device__ __attribute__((noinline)) void draw_from_apart(const RowView<T> row, int c0, int c1, const Weigh w, const Kept kept, double base, double S, uint32_t u, double* tmp, Drawn* drawn) {
-    draw_from<NT, T>(row, c0, c1, w, kept, base, S, u, tmp, drawn);
-}
 template <int NT, typename T>
 __device__ __attribute__((noinline)) u64 cut_stepwise_apart(const RowView<T> row, const Asked ask, const Weigh w, u64* lds, double* tmp) {
     return cut_stepwise<NT, T>(row, ask, w, lds, tmp);
 }
-__device__ __attribute__((noinline)) void put_token_apart(int32_t* token, float* logprob, const Weigh w, const Drawn& d, double whole) { put_token(token, logprob, w, d, whole); }
 
-// ---- many rows: a workgroup each, which does everything without meeting another one.
+// Many rows: a workgroup each, which does everything without meeting another one.
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kRowThreads, NW = NT / 64, kWaveList = kGather / NW;
     __shared__ u64 list[kGather];         // waves' lists of likely tokens, put together; then the bin's tokens
     __shared__ u64 bins[kBins];
     __shared__ FindLds find;
-    __shared__ double tmp[16], part[16];
-    __shared__ float sparse[NW][128];
+    __shared__ double tmp[16];
     __shared__ float wave_top[NW], wave_reach[kGroups][NW];
     __shared__ uint32_t wave_groups[kGroups][NW], wave_n[NW], count_n;
-    __shared__ Drawn drawn;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const RowView<T> row(logits + (int64_t)r * row_stride, V);
+    T* o = (T*)out.rows + (int64_t)r * out.rows_stride;
     const int pieces = row.pieces();
     const Wish wish(filter, r / rows_per_seq);
-    const uint32_t u = out.token ? out.u[r] : 0u;
     // the largest logit, the number of tokens, and how far the likely ones reach
     float top = -INFINITY;
     bool nan = false;
@@ -1172,37 +1162,30 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
     top = wave_top[0], tokens = wave_n[0];
 #pragma unroll
     for (int v = 1; v < NW; ++v) top = top != top || wave_top[v] != wave_top[v] ? NAN : fmaxf(top, wave_top[v]), tokens += wave_n[v];
-    T* o = out.rows ? (T*)out.rows + (int64_t)r * out.rows_stride : nullptr;
     if (top != top || top == -INFINITY) {   // (uniform)
-        if (o && o != row.row) mask_row<T>(row, o, tid, NT, pieces, Weigh(0.f, 1.0), Kept{0, 0, 0.0}, true);
+        if (o != row.row) mask_row<T>(row, o, tid, NT, pieces, Weigh(0.f, 1.0), Kept{0, 0, 0.0}, true);
         if (tid == 0) put_nothing(out, r, top != top);
         return;
     }
     const Asked ask = wish.asked((int)tokens);
     const Weigh w(top, ask.tau);
-    const bool prefix = ask.prefix();
     Kept in{kKeyNothing, -1, ask.least};   // (all, unless a prefix is asked for)
-    const int wper = (pieces + NW - 1) / NW, c0 = min(pieces, wave * wper), c1 = min(pieces, c0 + wper);   // a wave's range, where ranges matter
-    double whole = 0.0;
-    bool by_ranges = !prefix;              // the draw goes by the sums over the waves' ranges
-    double kept = 0.0, count = 0.0;
-    if (prefix) {
+    if (ask.prefix()) {
         const int level = level_of(ask);
         int rank = 0;
         float from = INFINITY;
 #pragma unroll
         for (int v = 0; v < NW; ++v) rank += wave_groups[level][v], from = fminf(from, wave_reach[level][v]);
         from = fmaxf(from, -FLT_MAX);
-        const bool count_bins = ask.top_k > min(rank, kListed), use_bins = count_bins || ask.top_k == 0;
+        const bool count_bins = ask.top_k > min(rank, kListed), use_bins = count_bins || ask.top_k == 0, weigh_all = ask.top_k == 0;
         const float per_logit = use_bins ? bins_per_logit(ask, V, w.distance(from)) : 0.f;
         if (count_bins) from = INFINITY;
-        const bool weigh_all = use_bins || out.logprob;
         if (use_bins)
             for (int i = tid; i < kBins; i += NT) bins[i] = 0;
-        if (tid == 0) count_n = 0;
         __syncthreads();
         u64* listing = list + wave * kWaveList;
         uint32_t listed = 0;
+        double whole = 0.0;
         row.each(tid, NT, pieces, [&](int c, const float (&x)[VEC]) {   // (waves take turns, so that neighbouring tokens go to several lists)
             double weight[VEC];
             if (weigh_all) {
@@ -1251,117 +1234,51 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
         TokenList l{list, nullptr, w, (int)n};
         u64 end = kNoEntry;
         if (n > 0 && n <= (uint32_t)kGather) end = end_in_list_apart<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
-        int lo = 0, hi = 0;
-        double before = 0.0;
-        int state = end != kNoEntry ? kDone : kStepwise;
-        if (state != kDone && use_bins) {
+        if (end == kNoEntry && use_bins) {
             // the bin that the end lies in
             static_assert(kBins <= NT, "a bin per thread");
             const double mine = tid < kBins ? (double)bins[tid] : 0.0;
             const double all = block_sum<NT>(mine, tmp), aim = count_bins ? (double)ask.top_k : share_of(ask.top_p, whole), run = block_excl_d<NT>(mine, tmp);
-            if (tid == 0) find.bin = -1;
+            if (tid == 0) find.bin = -1, count_n = 0;
             __syncthreads();
             if (run < aim && aim <= run + mine) find.bin = tid, find.base = run, find.value[0] = run + mine;
             __syncthreads();
-            const bool found = find.bin >= 0;
-            lo = hi = find.bin, before = find.base;
-            if (found) state = count_bins ? kByNumber : kByWeight;
-            if (count_bins && ask.by_p()) {
-                state = (found ? find.value[0] : all) <= (double)kGather ? kAllDownTo : kStepwise;
-                before = 0.0, lo = 0, hi = found ? hi : kBins - 1;
-            }
-            __syncthreads();
-        }
-        if (state == kByNumber || state == kByWeight || state == kAllDownTo) {
-            if (tid == 0) count_n = 0;
-            __syncthreads();
-            SparseSum above{sparse[wave], ask.least};
-            row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
+            // two limits: all tokens down to the bin of the first, if a list holds them (all that weigh anything, if they are fewer than top_k)
+            const bool found = find.bin >= 0, down_to = count_bins && ask.by_p();
+            const int lo = down_to ? 0 : find.bin, hi = found ? find.bin : kBins - 1;
+            const double before = down_to ? 0.0 : find.base;
+            if (down_to ? (found ? find.value[0] : all) <= (double)kGather : found) {   // (uniform)
+                row.each(tid, NT, pieces, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const int b = bin_of(w, x[e], per_logit);
-                    if (out.token) above.add(w, b < lo, x[e]);
-                    const bool is = b >= lo && b <= hi;
-                    const uint32_t at = place(is, &count_n);
-                    if (is && at < (uint32_t)kGather) list[at] = entry_of(x[e], row.first(c) + e);
+                    for (int e = 0; e < VEC; ++e) {
+                        const int b = bin_of(w, x[e], per_logit);
+                        const bool is = b >= lo && b <= hi;
+                        const uint32_t to = place(is, &count_n);
+                        if (is && to < (uint32_t)kGather) list[to] = entry_of(x[e], row.first(c) + e);
+                    }
+                });
+                __syncthreads();
+                n = count_n;
+                if (n > 0 && n <= (uint32_t)kGather) {
+                    l.n = (int)n;
+                    Asked one = ask;
+                    if (count_bins && !down_to) one.top_p = 1u << 31;
+                    if (down_to && one.top_k > (int)n) one.top_k = 0;   // (tokens without weight fill it up)
+                    end = end_in_list_apart<NT>(l, (int)n, one, count_bins ? 0.0 : before, count_bins ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit, find, tmp);
                 }
-            });
-            above.finish(w);
-            kept = above.sum, count = (double)above.count;
-            __syncthreads();
-            n = count_n;
-            if (n > 0 && n <= (uint32_t)kGather) {
-                l.n = (int)n;
-                Asked one = ask;
-                if (state == kByNumber) one.top_p = 1u << 31;
-                if (state == kAllDownTo && one.top_k > (int)n) one.top_k = 0;   // (tokens without weight fill it up)
-                end = end_in_list_apart<NT>(l, (int)n, one, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit,
-                                      find, tmp);
             }
-            if (end == kNoEntry) state = kStepwise;
         }
-        if (state == kStepwise) {
+        if (end != kNoEntry) {
+            in.cut = ~(uint32_t)(end >> 32), in.last = (int)(uint32_t)end;
+        } else {
             __syncthreads();
             const u64 cut = cut_stepwise_apart<NT, T>(row, ask, w, list, tmp);
             in.cut = (uint32_t)(cut >> 32), in.last = (int)(uint32_t)cut;
-            by_ranges = true;
-        } else {
-            in.cut = ~(uint32_t)(end >> 32), in.last = (int)(uint32_t)end;
-        }
-        if (out.token && (state == kDone || state == kAllDownTo)) {
-            draw_from_list_apart<NT>(l, end, ask.least, V, find, tmp, out.kept ? out.kept + r : nullptr, u, &drawn);
-            if (tid == 0) put_token_apart(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
-            return;
-        }
-        if (out.token && !by_ranges) {
-            // what the bin's list keeps joins the sums of its ranges
-            kept = wave_sum_d(kept);
-            if (lane == 0) part[wave] = kept;
-            __syncthreads();
-            for (uint32_t i = tid; i < n; i += NT) {
-                const double x = list[i] <= end ? l.weight((int)i) : -1.0;
-                if (x >= ask.least && x >= 0.0) {
-                    atomicAdd(&part[(((int)(uint32_t)list[i] + row.off) / VEC) / wper], x);
-                    count += 1.0;
-                }
-            }
-            __syncthreads();
         }
     }
-    if (!out.token) {
-        const uint32_t mine = mask_row<T>(row, o, tid, NT, pieces, w, in, false);
-        const double all = block_sum<NT>((double)mine, tmp);
-        if (tid == 0 && out.kept) out.kept[r] = (int32_t)all;
-        return;
-    }
-    if (by_ranges) {
-        // sums over the waves' ranges; without a prefix they are those of all weights too
-        count = 0.0, kept = 0.0;
-        double all = 0.0;
-        uint32_t kept_n = 0;
-        row.each(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const double weight = w(x[e]);
-                const bool is = in(w, row.first(c) + e, x[e]) && x[e] > -INFINITY;
-                all += weight, kept += is ? weight : 0.0, kept_n += is;
-            }
-        });
-        whole = block_sum<NT>(all, tmp);
-        count = (double)kept_n;
-        kept = wave_sum_d(kept);
-        if (lane == 0) part[wave] = kept;
-        __syncthreads();
-    }
-    count = block_sum<NT>(count, tmp);
-    if (tid == 0 && out.kept) out.kept[r] = (int32_t)count;
-    const double mine = tid < NW ? part[tid] : 0.0, S = block_sum<NT>(mine, tmp), aim = aim_of(u, S);
-    double base;
-    const int range = range_of<NT>(mine, aim, base, find, tmp);
-    if (range < 0) return;   // (cannot be)
-    const int p0 = min(pieces, range * wper), p1 = min(pieces, p0 + wper);
-    draw_from_apart<NT, T>(row, p0, p1, w, in, base, S, u, tmp, &drawn);
-    if (tid == 0) put_token_apart(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
+    const uint32_t mine = mask_row<T>(row, o, tid, NT, pieces, w, in, false);
+    const double all = block_sum<NT>((double)mine, tmp);
+    if (tid == 0 && out.kept) out.kept[r] = (int32_t)all;
 }
 
 // ---- small vocabularies: a row is one list, and one workgroup does everything
@@ -1435,14 +1352,15 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 
 // ---- host
 static int pick_segs(int rows, int vocab) {
-    // some 512 workgroups (each costs some 10 us of beginning, meeting and end: 64 x 152064 96 us with 1024, 86 with 512, 92 with 256), of 4096 tokens at least (so that each of a segment's threads has some)
+    // some 1024 workgroups, of 4096 tokens at least (so that each of a segment's threads has some)
     const int most = std::max(1, std::min(1024 / rows, vocab / 4096));
     int segs = 1;
     while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
     return segs;
 }
+static int pick_pass(int rows) { return (rows + (rows + kPassRows - 1) / kPassRows - 1) / ((rows + kPassRows - 1) / kPassRows); }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
-    if (vocab <= kSmall || rows > kFewRows) return 256;
+    if (vocab <= kSmall) return 256;
     const size_t R = (size_t)rows, S = (size_t)pick_segs(rows, vocab);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -1465,7 +1383,7 @@ static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
     if (ws) *ws = w;
     return at;
 }
-size_t pick_workspace_bytes(int rows, int vocab) { return pick_carve(rows, vocab, nullptr, nullptr); }
+size_t pick_workspace_bytes(int rows, int vocab) { return pick_carve(pick_pass(rows), vocab, nullptr, nullptr); }
 
 template <typename T>
 static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, const T* logits, int64_t row_stride, const PickFilter& filter, const PickOut& out, char* base) {
@@ -1473,23 +1391,26 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
         hipLaunchKernelGGL(pick_small_k<T>, dim3(rows), dim3(kGatherThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
         return;
     }
-    if (rows > kFewRows) {
+    if (out.rows && rows > kFewRows) {
         hipLaunchKernelGGL(pick_row_k<T>, dim3(rows), dim3(kRowThreads), 0, s, vocab, rows_per_seq, logits, row_stride, filter, out);
         return;
     }
+    const int pass = pick_pass(rows);
     PickWs ws;
-    pick_carve(rows, vocab, base, &ws);
+    pick_carve(pass, vocab, base, &ws);
     PickGeo geo;
     geo.V = vocab;
-    geo.segs = pick_segs(rows, vocab);
+    geo.segs = pick_segs(pass, vocab);
     constexpr int VEC = RowView<T>::VEC;
     geo.per = ((vocab + 2 * VEC - 2) / VEC + geo.segs - 1) / geo.segs;
     geo.rows_per_seq = rows_per_seq;
-    const dim3 grid((unsigned)(rows * geo.segs));
-    hipLaunchKernelGGL(pick_max_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, ws, out);
-    hipLaunchKernelGGL(pick_weigh_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
-    hipLaunchKernelGGL(pick_gather_k<T>, grid, dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
-    if (out.rows) hipLaunchKernelGGL(pick_mask_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+    for (geo.row0 = 0; geo.row0 < rows; geo.row0 += pass) {
+        const dim3 grid((unsigned)(std::min(pass, rows - geo.row0) * geo.segs));
+        hipLaunchKernelGGL(pick_max_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, ws, out);
+        hipLaunchKernelGGL(pick_weigh_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+        hipLaunchKernelGGL(pick_gather_k<T>, grid, dim3(kGatherThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+        if (out.rows) hipLaunchKernelGGL(pick_mask_k<T>, grid, dim3(kWeighThreads), 0, s, geo, logits, row_stride, filter, ws, out);
+    }
 }
 
 hipError_t pick(hipStream_t s, int dtype, int rows, int rows_per_seq, int vocab, const void* logits, int64_t row_stride, const PickFilter& filter,
