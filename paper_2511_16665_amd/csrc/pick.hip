@@ -307,13 +307,21 @@ __device__ __forceinline__ double block_excl_d(double v, double* tmp) {
     return base + incl - v;
 }
 
-// ---- tokens in a list in LDS: entry_of, and the weights where there is room for them (they are formed when they are asked for otherwise)
+// ---- tokens in a list in LDS: entry_of, and the weights where there is room for them (they are formed when they are asked for otherwise): S double, or uint32_t, which holds half as many bytes, all
+// weights but the largest two, and costs a comparison
+template <typename S>
 struct TokenList {
     const u64* e;
-    const double* stored;
+    const S* stored;
     Weigh w;
     int n;
-    __device__ __forceinline__ double weight(int i) const { return stored ? stored[i] : w(entry_logit(e[i])); }
+    static constexpr uint32_t kFull = 0xffffffffu;   // this, or the one weight above it
+    __device__ __forceinline__ double weight(int i) const {
+        if constexpr (std::is_same<S, double>::value) return stored ? stored[i] : w(entry_logit(e[i]));
+        const uint32_t x = stored ? (uint32_t)stored[i] : kFull;
+        return x != kFull ? (double)x : w(entry_logit(e[i]));
+    }
+    static __device__ __forceinline__ S held(double weight) { return std::is_same<S, double>::value ? (S)weight : (S)fmin(weight, 4294967295.0); }
 };
 struct FindLds {
     u64 bins[kFindBins], order[kFindFew];
@@ -507,8 +515,8 @@ __device__ __forceinline__ void draw_from(const RowView<T> row, int c0, int c1, 
 
 // Where the prefix ends in a list whose tokens follow on before_n others of weight before_w: its last token, or kNoEntry if it ends behind them.  n of the list's entries are
 // tokens, nearly all between the logits `best` and `least`.  S: the weight that top_p is a share of, for rows without top_k.
-template <int NT>
-__device__ __forceinline__ u64 end_in_list(const TokenList l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
+template <int NT, typename L>
+__device__ __forceinline__ u64 end_in_list(const L l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
     u64 end = kNoEntry - 1;   // (above every entry)
     auto order = [&](int i) { return l.e[i]; };
     // evenly over the distances from `best`
@@ -529,8 +537,8 @@ __device__ __forceinline__ u64 end_in_list(const TokenList l, int n, const Asked
 }
 
 // Draws from the list's tokens up to `end`, which are all that is kept but for `least`.
-template <int NT>
-__device__ __forceinline__ void draw_from_list(const TokenList l, u64 end, double least, int V, FindLds& s, double* tmp, int32_t* kept, uint32_t u, Drawn* drawn) {
+template <int NT, typename L>
+__device__ __forceinline__ void draw_from_list(const L l, u64 end, double least, int V, FindLds& s, double* tmp, int32_t* kept, uint32_t u, Drawn* drawn) {
     auto in = [&](int i) { return l.e[i] <= end && l.weight(i) >= least; };
     double S = 0.0, count = 0.0;
     for (int i = threadIdx.x; i < l.n; i += NT) {
@@ -785,7 +793,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
 #pragma unroll 4
         for (uint32_t i = kEarly * NT + tid; i < n; i += NT) local[i] = left(ws.list + (int64_t)lr * kList + i);
         __syncthreads();
-        const TokenList l{local, stored, w, (int)n};
+        const TokenList<double> l{local, stored, w, (int)n};
         const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
         if (end != kNoEntry) {
             if (tid == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
@@ -989,21 +997,21 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         for (int i = 0; i < kEarly; ++i) early[i] = left(ws.gather + (int64_t)lr * kGather + i * NT + tid);
         const uint32_t n = left(&pr->gather_n);
         if (n > 0 && n <= (uint32_t)kGather) {
-            double* stored = n <= kGather / 2 ? (double*)(local + kGather / 2) : nullptr;
+            uint32_t* stored = n <= kGather / 3 * 2 ? (uint32_t*)(local + kGather / 3 * 2) : nullptr;   // (8 and 4 bytes a token)
 #pragma unroll
             for (int i = 0; i < kEarly; ++i)
                 if ((uint32_t)(i * NT + tid) < n) {
                     local[i * NT + tid] = early[i];
-                    if (stored) stored[i * NT + tid] = w(entry_logit(early[i]));
+                    if (stored) stored[i * NT + tid] = TokenList<uint32_t>::held(w(entry_logit(early[i])));
                 }
 #pragma unroll 4
             for (uint32_t i = kEarly * NT + tid; i < n; i += NT) {
                 const u64 e = left(ws.gather + (int64_t)lr * kGather + i);
                 local[i] = e;
-                if (stored) stored[i] = w(entry_logit(e));
+                if (stored) stored[i] = TokenList<uint32_t>::held(w(entry_logit(e)));
             }
             __syncthreads();
-            const TokenList l{local, stored, w, (int)n};
+            const TokenList<uint32_t> l{local, stored, w, (int)n};
             if (state == kByNumber) ask.top_p = 1u << 31;
             if (state == kAllDownTo && ask.top_k > (int)n) ask.top_k = 0;   // (tokens without weight fill it up)
             const double before = pr->before;
@@ -1112,7 +1120,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
 // The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (32 x 48 rows of 152064 770 us, 975 with them inlined; the kernels with fewer threads are better
 // off inlined).
 template <int NT>
-__device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
+__device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList<double> l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
     return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, s, tmp);
 }
 template <int NT, typename T>
@@ -1231,7 +1239,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                 if ((uint32_t)(i * 64 + lane) < listed) list[at + i * 64 + lane] = held[i];
             __syncthreads();
         }
-        TokenList l{list, nullptr, w, (int)n};
+        TokenList<double> l{list, nullptr, w, (int)n};
         u64 end = kNoEntry;
         if (n > 0 && n <= (uint32_t)kGather) end = end_in_list_apart<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
         if (end == kNoEntry && use_bins) {
@@ -1332,7 +1340,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
         weight[j] = x, whole += x;
     }
     whole = block_sum<NT>(whole, tmp);   // (and all of both lists is there)
-    const TokenList l{entry, weight, w, V};
+    const TokenList<double> l{entry, weight, w, V};
     const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, top, least, find, tmp);
     if (out.token) {
         draw_from_list<NT>(l, end, ask.least, V, find, tmp, out.kept ? out.kept + r : nullptr, u, &drawn);
@@ -1352,11 +1360,11 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 
 // ---- host
 static int pick_segs(int rows, int vocab) {
-    // some 1024 workgroups, of 4096 tokens at least (so that each of a segment's threads has some)
-    const int most = std::max(1, std::min(1024 / rows, vocab / 4096));
+    // 1024 workgroups (four on each CU), or up to 1448 where the next fewer would be half of that, of 4096 tokens at least (so that each of a segment's threads has some)
+    const int most = std::min(kSegsMost, std::max(1, vocab / 4096));
     int segs = 1;
-    while (2 * segs <= std::min(most, kSegsMost)) segs *= 2;
-    return segs;
+    while (2 * segs <= std::min(most, 1024 / rows)) segs *= 2;
+    return segs < 8 && 2 * segs <= std::min(most, 1448 / rows) ? 2 * segs : segs;
 }
 static int pick_pass(int rows) { return (rows + (rows + kPassRows - 1) / kPassRows - 1) / ((rows + kPassRows - 1) / kPassRows); }
 static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
