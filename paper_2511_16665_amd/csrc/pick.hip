@@ -33,7 +33,7 @@ constexpr int kGather = 8192;                        // entries of the second li
 constexpr int kSmall = 4096;                         // vocabularies up to here are one list
 // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
 constexpr int kGroups = 3, kListed = 64 << (kGroups - 1);   // and the largest top_k that lists are made for
-constexpr int kInFlight = 2;                         // 16-byte pieces a lane asks for at once
+constexpr int kInFlight = 4, kAhead = 2;             // 16-byte pieces a lane asks for at once
 constexpr u64 kNoEntry = ~0ull;
 
 // order of logits as whole numbers; -0 and +0 are equal
@@ -157,35 +157,36 @@ struct RowView {
             for (int e = 0; e < VEC; ++e) x[e] = j + e >= 0 && j + e < V ? to_float(row[j + e]) : -INFINITY;
         }
     }
-    // f(piece, values) for pieces `from`, from + step, .. below `end`, kInFlight of them loaded at once; pieces at `end` and behind it come as -infinity (f is called by whole
+    // f(piece, values) for pieces `from`, from + step, .. below `end`, N of them loaded at once (AHEAD: before the ones in front of them are worked on); pieces at `end` and behind it come as -infinity (f is called by whole
     // waves, whose lanes hold consecutive pieces).  The row has a piece that lies inside.
     template <bool AHEAD = false, typename F>
     __device__ __forceinline__ void each(int from, int step, int end, F f) const {
+        constexpr int N = AHEAD ? kAhead : kInFlight;
         const int lane = threadIdx.x & 63, in0 = off ? 1 : 0, in1 = (V + off) / VEC;   // pieces in0 .. in1 - 1 lie inside
-        u32x4_t w[kInFlight], next[kInFlight];
-        auto ask = [&](int c, u32x4_t (&w)[kInFlight]) {
+        u32x4_t w[N], next[N];
+        auto ask = [&](int c, u32x4_t (&w)[N]) {
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) w[u] = raw(min(max(c + u * step, in0), in1 - 1));
+            for (int u = 0; u < N; ++u) w[u] = raw(min(max(c + u * step, in0), in1 - 1));
         };
         if (AHEAD) ask(from, next);
-        for (int c = from; c - lane < end; c += kInFlight * step) {
+        for (int c = from; c - lane < end; c += N * step) {
             if (AHEAD) {
 #pragma unroll
-                for (int u = 0; u < kInFlight; ++u) w[u] = next[u];
-                ask(c + kInFlight * step, next);   // (held inside the row)
+                for (int u = 0; u < N; ++u) w[u] = next[u];
+                ask(c + N * step, next);   // (held inside the row)
             } else {
                 ask(c, w);
             }
-            if (c - lane < in0 || c - lane + (kInFlight - 1) * step + 63 >= min(end, in1)) {   // (uniform over the wave)
+            if (c - lane < in0 || c - lane + (N - 1) * step + 63 >= min(end, in1)) {   // (uniform over the wave)
                 const int behind = in1 * VEC < V + off ? in1 : -1;   // the piece behind the last whole one
                 u32x4_t part = {};
                 if (c == 0 && in0) w[0] = partly(0);
                 bool is = false;
 #pragma unroll
-                for (int u = 0; u < kInFlight; ++u) is |= c + u * step == behind;
+                for (int u = 0; u < N; ++u) is |= c + u * step == behind;
                 if (is) part = partly(behind);
 #pragma unroll
-                for (int u = 0; u < kInFlight; ++u) {
+                for (int u = 0; u < N; ++u) {
                     const int at = c + u * step;
                     const bool in = at < end && (at < in1 || at == behind);
                     float x[VEC];
@@ -196,7 +197,7 @@ struct RowView {
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
+            for (int u = 0; u < N; ++u) {
                 float x[VEC];
                 values(w[u], x);
                 f(c + u * step, x);
