@@ -66,8 +66,8 @@ __device__ __forceinline__ int above(const int32_t* v, int n, int32_t x) {
     return lo;
 }
 
-// `done`: the only workgroup, which also moves the stack's end and the counts; otherwise pages_grow_end_k does, after all have read them.  32 sequences of 48 rows: 5.3 us, a launch and four
-// dependent loads (lengths, page, stack); 256 sequences with 180000 rows and 11000 pages 7.3 us on 180 workgroups.
+// `done`: the only workgroup, which also moves the stack's end and the counts; otherwise pages_grow_end_k does, after all have read them.  Bound by the chain lengths, sums, page, stack of
+// dependent loads: 32 sequences of 48 rows 6.5 us, 256 sequences with 180000 rows and 11000 pages 7.5 us on 180 workgroups (and 2.6 for the counts).
 __global__ __launch_bounds__(kPageThreads) void pages_grow_k(int B, int max_rows, int done, const int32_t* __restrict__ seq_len, const int32_t* __restrict__ n_new,
                                                              PageState pg, GrowOut out) {
     extern __shared__ int32_t page_lds[];
@@ -189,7 +189,8 @@ __device__ __forceinline__ int gives(const PageState& pg, const int32_t* keep_le
     return held >= 0 && held <= pg.max_pages && (uint32_t)held > keep ? held - (int)keep : 0;
 }
 
-// Pushed in the reverse of the order in which growing pops: page q of those given back, counted by sequence and table entry, goes to n_free + total - 1 - q.  32 sequences: 3.2 us.
+// Pushed in the reverse of the order in which growing pops: page q of those given back, counted by sequence and table entry, goes to n_free + total - 1 - q.  32 sequences 3.2 us,
+// 256 sequences with 11000 pages 9.2.
 __global__ __launch_bounds__(kPageThreads) void pages_release_k(int B, int done, const int32_t* __restrict__ keep_len, PageState pg) {
     extern __shared__ int32_t page_lds[];
     __shared__ int64_t tmp[2][kPageWaves];
@@ -243,8 +244,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_release_end_k(int B, const
     if (tid == 0) *pg.n_free = (int32_t)(n_free + all);
 }
 
-// One workgroup does everything in one launch; where there may be much to do, several and a launch for the counts.  Rows: 16384 in one workgroup 12 us, with a second launch 9.  Pages given back: what the
-// call cannot know is how many of them there are, a step's are few, and a workgroup moves 4096 in about a microsecond and a half.
+// One workgroup does everything in one launch; where there may be much to do, several and a launch for the counts.  Growing and giving back, 4096 rows 11.6 us in one workgroup, 17.4 in two launches; 8192 rows 15.1
+// and 17.4, 16384 rows 24.7 and 17.3.  Pages given back: what the call cannot know is how many of a pool's pages they are.  A step's are few: taken and given back, 1024 of a pool of 131072 are 10.8 us in
+// one launch, 13.1 in two; 4096 pages 12.1 and 12.9, all of them 171 and 108.
 constexpr int64_t kRowsOfOne = 8 * kPageThreads, kPagesOfOne = 128 * kPageThreads;
 
 hipError_t pages_grow(hipStream_t s, int B, const PageState& pg, const int32_t* seq_len, const int32_t* n_new, const int32_t* depth, int max_rows,

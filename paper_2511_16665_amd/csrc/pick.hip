@@ -10,6 +10,9 @@
 //                  prefix's end.  The last workgroup of a row finds that end in the list, or the histogram's bin that holds it
 //   pick_gather_k  only where the list did not reach: the tokens of that bin (or all down to it) go to a list, what is above is summed up
 //   pick_mask_k    for filtered rows
+// What has to be read and written once would take 35 us for 256 rows of 152064 in fp32 (156 MB); here they take 31 us for the maximum (5.0 TB/s), 70 for the weights (some 30 operations in double
+// or of the same length per element, and a histogram in LDS), 41 for the second list.  One row is a chain of about 25 us: three launches, in the second 2.5 us of sums over the segments, 5 of reading, 2 of
+// meeting, 9 of searches in LDS.  Many filtered rows (pick_row_k) and vocabularies up to 4096 (pick_small_k) have kernels of their own.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -23,17 +26,22 @@ typedef unsigned long long u64;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
-constexpr int kPassRows = 1024;                      // rows that the segments' kernels take at a time
-constexpr int kFewRows = 256;                        // from there on filtered rows are a workgroup's each
+// Rows that the segments' kernels take at a time, for which the workspace has room (0.1 MB a row).  1024 rows of 152064 with top-p: 437 us at once, 474 in two halves, 549 in quarters; a workgroup per row 528.
+constexpr int kPassRows = 1024;
+// From there on filtered rows are a workgroup's each: a row is read again while it is near.  96 rows of 152064 86 us by segments, 154 by a workgroup each; 192 rows 150 and 176, 256 rows 181 and 191, 384 rows
+// 274 and 266, 1536 rows 852 and 712.
+constexpr int kFewRows = 256;
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other
 constexpr int kList = 4096, kWaveList = 1024;        // entries of a row's list of likely tokens, and of what a wave may add (4096 in all: the row's list lies in their place)
 constexpr int kGather = 8192;                        // entries of the second list
-constexpr int kSmall = 4096;                         // vocabularies up to here are one list
+// vocabularies up to here are one list: one row of 4096 15.7 us, 20.9 by segments; 256 rows 22.5 and 38.3; of 1025 10.1 and 18.4, 12.0 and 34.0
+constexpr int kSmall = 4096;
 // numbers of groups whose largest logits show how far the likely tokens reach: 64 << k
 constexpr int kGroups = 3, kListed = 64 << (kGroups - 1);   // and the largest top_k that lists are made for
-constexpr int kInFlight = 4, kAhead = 2;             // 16-byte pieces a lane asks for at once
+// 16-byte pieces a lane asks for at once: in kernels that mostly move data (filtered rows 32 x 48 712 us, 740 with 2), and in those that compute, where they are asked for ahead (64 rows of 152064 62 us, 66 with 4)
+constexpr int kInFlight = 4, kAhead = 2;
 constexpr u64 kNoEntry = ~0ull;
 
 // order of logits as whole numbers; -0 and +0 are equal
@@ -425,7 +433,8 @@ struct PickGeo {
     int rows_per_seq, row0;   // row0: first row of this launch
 };
 
-// What one workgroup of a row leaves for another of the same launch goes past the caches of an XCD, both ways, so that nothing has to be written back or dropped where they meet.
+// What one workgroup of a row leaves for another of the same launch goes past the caches of an XCD, both ways, so that nothing has to be written back or dropped where they meet: a meeting takes 0.7 us of the
+// last workgroup, 4.1 with ordinary stores and a release that writes the cache back, and its list is there after 1.3 us instead of 5.8 (64 rows of 152064).
 template <typename V>
 __device__ __forceinline__ void leave(V* to, V v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename V>
@@ -844,7 +853,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
     }
 }
 
-// ---- rows that neither list nor bins settle: digit by digit over the keys, one workgroup, every step a pass over the row
+// ---- rows that neither list nor bins settle (thousands of equal logits, or a great top_k far down): digit by digit over the keys, one workgroup, every step a pass over the row; 280 us for a row of 152064
 template <int NT, typename T>
 __device__ __forceinline__ u64 cut_stepwise(const RowView<T> row, const Asked ask, const Weigh w, u64* lds, double* tmp) {
     uint32_t cut;
@@ -1074,7 +1083,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
     if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);
 }
 
-// ---- filtered rows
+// ---- filtered rows: read and written once, bound by memory (256 rows of 152064 in 55 us, 5.7 TB/s)
 // Pieces first, first + step, .. of a row below `end`, with what is not kept at -infinity (copy: as they are); returns this thread's number of kept tokens.
 template <typename T>
 __device__ __forceinline__ uint32_t mask_row(const RowView<T>& row, T* o, int first, int step, int end, const Weigh& w, const Kept& in, bool copy) {
@@ -1118,8 +1127,8 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
     if (threadIdx.x == 0 && all > 0.0) atomicAdd(&out.kept[r], (int32_t)all);
 }
 
-// The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (32 x 48 rows of 152064 770 us, 975 with them inlined; the kernels with fewer threads are better
-// off inlined).
+// The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (32 x 48 rows of 152064 770 us when it was first measured, 975
+// with them inlined; the kernels with fewer threads are better off inlined).
 template <int NT>
 __device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList<double> l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
     return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, s, tmp);
@@ -1129,7 +1138,8 @@ __device__ __attribute__((noinline)) u64 cut_stepwise_apart(const RowView<T> row
     return cut_stepwise<NT, T>(row, ask, w, lds, tmp);
 }
 
-// Many rows: a workgroup each, which does everything without meeting another one.
+// Many rows: a workgroup each, which does everything without meeting another one.  Rows are read three times and written once: 1536 rows of 152064 (0.93 GB each
+// time) in 712 us, 5.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
     constexpr int VEC = RowView<T>::VEC, NT = kRowThreads, NW = NT / 64, kWaveList = kGather / NW;
@@ -1290,7 +1300,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
     if (tid == 0 && out.kept) out.kept[r] = (int32_t)all;
 }
 
-// ---- small vocabularies: a row is one list, and one workgroup does everything
+// ---- small vocabularies: a row is one list, and one workgroup does everything.  2 x 1024 in 10 us, a chain: the row, its weights, two or three searches of about 2 us in LDS.
 template <typename T>
 __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_per_seq, const T* logits, int64_t row_stride, PickFilter filter, PickOut out) {
     constexpr int NT = kGatherThreads;
@@ -1361,7 +1371,9 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 
 // ---- host
 static int pick_segs(int rows, int vocab) {
-    // 1024 workgroups (four on each CU), or up to 1448 where the next fewer would be half of that, of 4096 tokens at least (so that each of a segment's threads has some)
+    // 1024 workgroups (four on each CU), or up to 1448 where the next fewer would be half of that, of 4096 tokens at least (so that each of a segment's threads has some).  With top-p over 152064 tokens
+    // 1024, 512 and 2048 workgroups: 64 rows 69, 76 and 83 us, 90 rows 84, 103 and 81, 32 rows 60, 58 and 60.  The rounding: 320 rows as 1280 workgroups 167 us, as 640 193; 700 rows as 1400 305, as 700 368; but 45 rows as
+    // 1440 63, as 720 56.
     const int most = std::min(kSegsMost, std::max(1, vocab / 4096));
     int segs = 1;
     while (2 * segs <= std::min(most, 1024 / rows)) segs *= 2;

@@ -28,11 +28,26 @@ __device__ __forceinline__ u32x4_t packed(const float (&x)[VEC]) {
     return w;
 }
 
-// cos and sin of position * freq: the product in double, in turns, of which the fraction is exact, so the angle is good to fp32 at any position
+// amplitude times cos and sin of position * freq.  The product in double, in turns, of which the fraction is exact; an eighth of a turn at most from a quarter turn, where Taylor's series to the 12th and 11th
+// power are 2^-37 off: so both are right to half a unit of fp32's last place but for one in a thousand.  (sincospif of the fraction in fp32 is up to 2^-23 off: rows of an 8-bit cache then differed from angles in
+// double by 1.7e-5, root mean square, as some values round the other way, now by 6.5e-7; it takes as long.)
 __device__ __forceinline__ void turn(int position, double freq, float amplitude, float& c, float& s) {
     const double t = (double)position * (freq * 0.15915494309189533577);   // 1 / 2 pi
-    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
-    c *= amplitude, s *= amplitude;
+    const double f = t - rint(t), q = rint(4.0 * f), x = (f - 0.25 * q) * 6.2831853071795864769, z = x * x;
+    double u = fma(z, -1.0 / 39916800, 1.0 / 362880);
+    u = fma(z, u, -1.0 / 5040);
+    u = fma(z, u, 1.0 / 120);
+    u = fma(z, u, -1.0 / 6);
+    u = fma(z * x, u, x);
+    double v = fma(z, 1.0 / 479001600, -1.0 / 3628800);
+    v = fma(z, v, 1.0 / 40320);
+    v = fma(z, v, -1.0 / 720);
+    v = fma(z, v, 1.0 / 24);
+    v = fma(z, v, -0.5);
+    v = fma(z, v, 1.0);
+    const int quarter = (int)q;   // -2 .. 2
+    const double a = (double)amplitude, cs = quarter & 1 ? u : v, sn = quarter & 1 ? v : u;
+    c = (float)(a * ((quarter + 1) & 2 ? -cs : cs)), s = (float)(a * (quarter & 2 ? -sn : sn));
 }
 
 // One wave per row and head, lane l holding elements of pairs l and l + 64: any layout, any even head_dim up to 256, any alignment.
@@ -108,8 +123,9 @@ __global__ __launch_bounds__(256) void rope_any_k(int rows, int n_q_heads, RopeI
 }
 
 // A workgroup per row and 2 x 16 bytes of a head per thread, the two pieces holding whole pairs: with pairs (j, j + rot_dim / 2) a piece of either half of the turned part (or two
-// pieces behind it), with pairs (2j, 2j + 1) two pieces side by side.  The row's angles are formed once and shared through LDS; its elements are asked for before that.  Memory moves what has to be moved
-// once: bound by memory for many rows, by the chain position - angle - LDS - store for few.
+// pieces behind it), with pairs (2j, 2j + 1) two pieces side by side.  The row's angles are formed once and shared through LDS; its elements are asked for before that.
+// Bound by memory for many rows: 8190 rows of 64 + 8 + 8 heads of 128 (336 MB) in 62 us, 5.4 TB/s; rope_any_k, which forms a head's angles for itself, 208.  Few rows are a chain, position, angle, LDS, store: one row
+// 2.6 us, 1536 rows of 28 + 4 + 4 heads into 8 bits 9.5 (a wave per head 24).
 template <typename T, bool INTERLEAVED, bool E8>
 __global__ __launch_bounds__(1024) void rope_row_k(int n_q_heads, int lanes_log2, RopeIn in, RopeOut out) {
     constexpr int VEC = 16 / sizeof(T);
