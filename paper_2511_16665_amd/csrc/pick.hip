@@ -28,9 +28,9 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 constexpr int kWeighThreads = 256, kGatherThreads = 512, kRowThreads = 1024;
 // Rows that the segments' kernels take at a time, for which the workspace has room (0.1 MB a row).  1024 rows of 152064 with top-p: 437 us at once, 474 in two halves, 549 in quarters; a workgroup per row 528.
 constexpr int kPassRows = 1024;
-// From there on filtered rows are a workgroup's each: a row is read again while it is near.  96 rows of 152064 86 us by segments, 154 by a workgroup each; 192 rows 150 and 176, 256 rows 181 and 191, 384 rows
-// 274 and 266, 1536 rows 852 and 712.
-constexpr int kFewRows = 256;
+// From there on filtered rows are a workgroup's each: a row is read again while it is near.  Of 152064 tokens, by segments and by a workgroup each: 128 rows with top-k and top-p 80 and 73 us, with top-p 100 and
+// 124, of mixed settings 98 and 156; 192 rows 115 and 99, 147 and 146, 150 and 175; 256 rows 149 and 129, 186 and 164, 182 and 190; 1536 rows of mixed settings 852 and 712.
+constexpr int kFewRows = 192;
 constexpr int kSegsMost = 32;                        // (a power of two)
 constexpr int kBins = 512;                           // of a row's histogram
 constexpr int kFindBins = 256, kFindFew = 64;        // of a search in a list, and tokens that are compared with each other

@@ -129,7 +129,7 @@ def test_batches_and_trees(B, n, V):
 
 @pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("rows,V", [(112, 5003), (280, 4099), (280, 9001), (28, 33000), (3, 33001)])
+@pytest.mark.parametrize("rows,V", [(112, 5003), (196, 4500), (280, 4099), (280, 9001), (28, 33000), (3, 33001)])
 def test_rows_by_one_or_several_workgroups(code, kind, rows, V):
     """Few rows are cut into segments, more of them are a workgroup's; every setting on every kind of row."""
     rng = np.random.default_rng(rows + len(kind))
