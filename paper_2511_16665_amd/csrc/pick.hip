@@ -457,7 +457,7 @@ __device__ __forceinline__ float bins_per_logit(const Asked& ask, int V, float l
     else if (likely > 0.f) reach = fmax(reach, 4.0 * (double)likely);
     return (float)fmin((double)kBins / reach, 1e30);
 }
-__device__ __forceinline__ int bin_of(const Weigh& w, float x, float per_logit) { return (int)fminf(w.distance(x) * per_logit, 1e6f); }
+__device__ __forceinline__ float bin_of(const Weigh& w, float x, float per_logit) { return w.distance(x) * per_logit; }   // (its whole part; NaN: below them)
 
 // ---- outputs
 __device__ __forceinline__ void put_nothing(const PickOut& out, int r, bool nan) {
@@ -731,6 +731,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
             for (int e = 0; e < VEC; ++e) {
                 const bool in = x[e] >= from;
                 const uint64_t all = __ballot(in);
+                if (all == 0) continue;
                 const uint32_t at = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
                 if (in && at < (uint32_t)kWaveList) listing[at] = entry_of(x[e], row.first(c) + e);
                 listed += (uint32_t)__popcll(all);
@@ -739,8 +740,8 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         if (use_bins) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const int b = bin_of(w, x[e], per_logit);
-                if (b < kBins) atomicAdd(&lds.bins[b], count_bins ? 1ull : w.whole(weight[e]));
+                const float b = bin_of(w, x[e], per_logit);
+                if (b < (float)kBins) atomicAdd(&lds.bins[(int)b], count_bins ? 1ull : w.whole(weight[e]));
             }
         }
     });
@@ -984,9 +985,9 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
         row.template each<true>(c0 + lane, 64, c1, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const int b = bin_of(w, x[e], per_logit);
-                if (out.token) above.add(w, b < lo, x[e]);
-                const bool is = b >= lo && b <= hi;
+                const float b = bin_of(w, x[e], per_logit);
+                if (out.token) above.add(w, b < (float)lo, x[e]);
+                const bool is = b >= (float)lo && b < (float)(hi + 1);
                 const uint32_t at = place(is, &local_n);
                 if (is && at < (uint32_t)kGather) local[at] = entry_of(x[e], row.first(c) + e);
             }
@@ -1222,6 +1223,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                 for (int e = 0; e < VEC; ++e) {
                     const bool is = x[e] >= from;
                     const uint64_t all = __ballot(is);
+                    if (all == 0) continue;
                     const uint32_t at = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
                     if (is && at < (uint32_t)kWaveList) listing[at] = entry_of(x[e], row.first(c) + e);
                     listed += (uint32_t)__popcll(all);
@@ -1230,8 +1232,8 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
             if (use_bins) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const int b = bin_of(w, x[e], per_logit);
-                    if (b < kBins) atomicAdd(&bins[b], count_bins ? 1ull : w.whole(weight[e]));
+                    const float b = bin_of(w, x[e], per_logit);
+                    if (b < (float)kBins) atomicAdd(&bins[(int)b], count_bins ? 1ull : w.whole(weight[e]));
                 }
             }
         });
@@ -1270,8 +1272,8 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                 row.each(tid, NT, pieces, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const int b = bin_of(w, x[e], per_logit);
-                        const bool is = b >= lo && b <= hi;
+                        const float b = bin_of(w, x[e], per_logit);
+                        const bool is = b >= (float)lo && b < (float)(hi + 1);
                         const uint32_t to = place(is, &count_n);
                         if (is && to < (uint32_t)kGather) list[to] = entry_of(x[e], row.first(c) + e);
                     }
