@@ -10,8 +10,8 @@
 //                  prefix's end.  The last workgroup of a row finds that end in the list, or the histogram's bin that holds it
 //   pick_gather_k  only where the list did not reach: the tokens of that bin (or all down to it) go to a list, what is above is summed up
 //   pick_mask_k    for filtered rows
-// What has to be read and written once would take 35 us for 256 rows of 152064 in fp32 (156 MB); here they take 31 us for the maximum (5.0 TB/s), 70 for the weights (some 30 operations in double
-// or of the same length per element, and a histogram in LDS), 41 for the second list.  One row is a chain of about 25 us: three launches, in the second 2.5 us of sums over the segments, 5 of reading, 2 of
+// What has to be read and written once would take 35 us for 256 rows of 152064 in fp32 (156 MB); here they take 31 us for the maximum (5.0 TB/s), 66 for the weights (42 vector instructions per
+// element, half of them in double, 83 % of the cycles; 16 instructions an element take as long as reading it), 41 for the second list.  One row is a chain of about 25 us: three launches, in the second 2.5 us of sums over the segments, 5 of reading, 2 of
 // meeting, 9 of searches in LDS.  Many filtered rows (pick_row_k) and vocabularies up to 4096 (pick_small_k) have kernels of their own.
 #include <algorithm>
 #include <cfloat>

@@ -117,7 +117,7 @@ def test_a_large_vocabulary(code, kind):
     check_rows(values, asked, 1, u, *got)
 
 
-@pytest.mark.parametrize("B,n,V", [(1, 1, 152064), (3, 7, 20000), (40, 8, 3001), (300, 1, 2048), (5, 64, 1024)])
+@pytest.mark.parametrize("B,n,V", [(1, 1, 152064), (3, 7, 20000), (40, 8, 3001), (300, 1, 2048), (5, 64, 1024), (11, 100, 4500)])
 def test_batches_and_trees(B, n, V):
     rng = np.random.default_rng(B)
     x = np.concatenate([logits_of("peaks", B * n - B * n // 2, V, rng), logits_of("bell", B * n // 2, V, rng)])
