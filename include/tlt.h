@@ -478,7 +478,7 @@ int tlt_rope_write(void *stream, int dtype, int rows, int n_q_heads, int n_kv_he
  * A temperature that is not positive keeps the first token of the order alone, weights as at temperature 1.  A row with a NaN, or with
  * nothing above -infinity, keeps nothing; +infinity is a largest value like any other.  Logits of dtype TLT_F32 or TLT_BF16, rows `row_stride` elements apart (>= vocab); row r belongs
  * to sequence r / rows_per_seq (the nodes of a tree lie side by side).  vocab <= 2^20, rows < 2^22.
- * ws: DEVICE scratch (256-byte aligned) of tlt_sample_workspace_bytes(rows, vocab) bytes; it need not be cleared, and calls that may overlap in
+ * ws: DEVICE scratch (256-byte aligned) of tlt_sample_workspace_bytes(rows, vocab) bytes (some 0.1 MB a row up to 1024 rows, no more behind them; never less for more rows or a larger vocabulary); it need not be cleared, and calls that may overlap in
  * time need one each.  The function returns 0 for sizes that the calls refuse. */
 typedef struct tlt_filter {
     const float *temperature;

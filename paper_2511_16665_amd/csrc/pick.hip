@@ -1372,19 +1372,20 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
 }
 
 // ---- host
+constexpr int kMostGroups = 1448;   // segments of all rows, or one of each
+static int pick_most_segs(int vocab) { return std::min(kSegsMost, std::max(1, vocab / 4096)); }
 static int pick_segs(int rows, int vocab) {
     // 1024 workgroups (four on each CU), or up to 1448 where the next fewer would be half of that, of 4096 tokens at least (so that each of a segment's threads has some).  With top-p over 152064 tokens
     // 1024, 512 and 2048 workgroups: 64 rows 69, 76 and 83 us, 90 rows 84, 103 and 81, 32 rows 60, 58 and 60.  The rounding: 320 rows as 1280 workgroups 167 us, as 640 193; 700 rows as 1400 305, as 700 368; but 45 rows as
     // 1440 63, as 720 56.
-    const int most = std::min(kSegsMost, std::max(1, vocab / 4096));
+    const int most = pick_most_segs(vocab);
     int segs = 1;
     while (2 * segs <= std::min(most, 1024 / rows)) segs *= 2;
-    return segs < 8 && 2 * segs <= std::min(most, 1448 / rows) ? 2 * segs : segs;
+    return segs < 8 && 2 * segs <= std::min(most, kMostGroups / rows) ? 2 * segs : segs;
 }
 static int pick_pass(int rows) { return (rows + (rows + kPassRows - 1) / kPassRows - 1) / ((rows + kPassRows - 1) / kPassRows); }
-static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
-    if (vocab <= kSmall) return 256;
-    const size_t R = (size_t)rows, S = (size_t)pick_segs(rows, vocab);
+// R rows with RS segments
+static size_t pick_carve(size_t R, size_t RS, char* base, PickWs* ws) {
     size_t at = 0;
     auto take = [&](size_t bytes) {
         char* p = base + at;
@@ -1393,20 +1394,25 @@ static size_t pick_carve(int rows, int vocab, char* base, PickWs* ws) {
     };
     PickWs w;
     w.row = (PickRow*)take(R * sizeof(PickRow));
-    w.top = (float*)take(R * S * 4);
-    w.reach = (float*)take(R * S * kGroups * 4);
-    w.groups = (uint32_t*)take(R * S * kGroups * 4);
-    w.tokens = (uint32_t*)take(R * S * 4);
-    w.whole = (double*)take(R * S * 8);
-    w.part = (double*)take(R * S * 64);
-    w.part_n = (uint32_t*)take(R * S * 32);
+    w.top = (float*)take(RS * 4);
+    w.reach = (float*)take(RS * kGroups * 4);
+    w.groups = (uint32_t*)take(RS * kGroups * 4);
+    w.tokens = (uint32_t*)take(RS * 4);
+    w.whole = (double*)take(RS * 8);
+    w.part = (double*)take(RS * 64);
+    w.part_n = (uint32_t*)take(RS * 32);
     w.list = (u64*)take(R * kList * 8);
     w.gather = (u64*)take(R * kGather * 8);
-    w.bins = (u64*)take(R * S * kBins * 8);
+    w.bins = (u64*)take(RS * kBins * 8);
     if (ws) *ws = w;
     return at;
 }
-size_t pick_workspace_bytes(int rows, int vocab) { return pick_carve(pick_pass(rows), vocab, nullptr, nullptr); }
+// (no smaller for more rows or a larger vocabulary: a caller sizes it once, for the largest call)
+size_t pick_workspace_bytes(int rows, int vocab) {
+    if (vocab <= kSmall) return 256;
+    const size_t R = (size_t)std::min(rows, kPassRows);
+    return pick_carve(R, std::max(R, std::min((size_t)kMostGroups, R * pick_most_segs(vocab))), nullptr, nullptr);
+}
 
 template <typename T>
 static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, const T* logits, int64_t row_stride, const PickFilter& filter, const PickOut& out, char* base) {
@@ -1420,10 +1426,10 @@ static void pick_rounds(hipStream_t s, int rows, int rows_per_seq, int vocab, co
     }
     const int pass = pick_pass(rows);
     PickWs ws;
-    pick_carve(pass, vocab, base, &ws);
     PickGeo geo;
     geo.V = vocab;
     geo.segs = pick_segs(pass, vocab);
+    pick_carve((size_t)pass, (size_t)pass * geo.segs, base, &ws);
     constexpr int VEC = RowView<T>::VEC;
     geo.per = ((vocab + 2 * VEC - 2) / VEC + geo.segs - 1) / geo.segs;
     geo.rows_per_seq = rows_per_seq;

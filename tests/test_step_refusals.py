@@ -117,3 +117,13 @@ def test_a_greedy_engine_step_takes_no_filter():
     from paper_2511_16665_amd.engine import Engine
     with pytest.raises(ValueError):
         Engine.step(None, 4, 4, 8, asked=object())
+
+
+def test_a_sampling_workspace_for_the_largest_call_serves_smaller_ones():
+    size = tlt.load().tlt_sample_workspace_bytes
+    for V in (4096, 4097, 8192, 9001, 50000, 152064, 1 << 20):
+        sizes = [size(r, V) for r in [*range(1, 1500), 2047, 2048, 2049, 5000, (1 << 22) - 1]]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    for r in (1, 33, 363, 1024, 5000):
+        sizes = [size(r, V) for V in (1, 4096, 4097, 8191, 8192, 16383, 16384, 40000, 152064, 1 << 20)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:]))
