@@ -400,7 +400,7 @@ __device__ u64 locate(int n, O order, A active, F value, G bin, double aim, Find
             const u64 o = order(i);
             if (o >= lo && o <= hi && active(i) && bin_at(i, o) == at) first = min(first, o), last = max(last, o);
         }
-        if (last) atomicMin(&s.order[0], first), atomicMax(&s.order[1], last);
+        if (first != kNoEntry) atomicMin(&s.order[0], first), atomicMax(&s.order[1], last);   // (not `last`: in the order of indices token 0 is 0)
         together<NT>();
         lo = s.order[0], hi = s.order[1];
         per = (double)kFindBins / ((double)(hi - lo) + 1.0) * (1.0 - 0x1p-40);
@@ -557,7 +557,10 @@ __device__ __forceinline__ void draw_from_list(const L l, u64 end, double least,
     }
     S = block_sum<NT>(S, tmp);
     count = block_sum<NT>(count, tmp);
-    if (threadIdx.x == 0 && kept) *kept = (int32_t)count;
+    if (threadIdx.x == 0) {
+        if (kept) *kept = (int32_t)count;
+        drawn->S = 1.0, drawn->token = -1, drawn->logit = -INFINITY;   // (a search that finds nothing draws nothing)
+    }
     const double per = (double)kFindBins / ((double)V + 1.0);
     const u64 token = locate<NT>(l.n, [&](int i) { return l.e[i] & 0xffffffffull; }, in, [&](int i) { return l.weight(i); }, [&](int i) { return (int)((double)(uint32_t)l.e[i] * per); },
                                  aim_of(u, S) + 1.0, s, tmp);

@@ -1,0 +1,39 @@
+"""tlt_sample and tlt_sample_filter where their searches in lists and bins refine, run short, or join many segments; against the model in whole numbers."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import pick_model as pm
+from paper_2511_16665_amd import binding as tlt
+from test_gpu_sample import check_rows, run
+
+pytestmark = pytest.mark.gpu
+
+
+def as_stored(x, code):
+    """The values that a row of this type holds, as fp32."""
+    return torch.from_numpy(x.astype(np.float32)).to(tlt.torch_dtype(code)).float().numpy()
+
+
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+@pytest.mark.parametrize("V,likely,ask", [(152064, 200, dict(top_k=200)), (152064, 300, dict(top_k=2000, top_p=0.97)), (152064, 150, dict(top_k=150, top_p=0.999, tau=0.9)),
+                                          (50001, 180, dict(top_k=180)), (152064, 120, dict(top_k=120, min_p=1e-6))])
+def test_draws_among_many_tokens_of_low_index(code, V, likely, ask):
+    """The kept tokens are 0 .. likely - 1, of which token 0 weighs most: far more of them in one 256th of the vocabulary than a search compares with each other.  The uniforms reach into
+    token 0's share, both sides of its end (2^13 of 2^32, hundreds of times what a unit in every weight could move it), the rest, and the last of it."""
+    rng = np.random.default_rng(likely)
+    row = rng.normal(-25.0, 2.0, V)
+    row[:likely] = 5.0 + rng.random(likely)
+    row[0] = 9.0
+    row = as_stored(row, code)
+    kept, _, W = pm.choose(row, **ask)
+    assert 0 in kept and len(kept) > 100 and kept.max() < likely
+    share = int(W[0]) * 2 ** 32 // int(W[kept].sum())
+    assert 2 ** 28 < share < 2 ** 31
+    u = np.array([0, 1, share // 2, share - 2 ** 13, share + 2 ** 13, 2 ** 31, 3 * 2 ** 30, 2 ** 32 - 1, *rng.integers(0, 2 ** 32, 4)])
+    x = np.tile(row, (len(u), 1))
+    values, *got = run(code, x, [ask] * len(u), 1, u)
+    check_rows(values, [ask] * len(u), 1, u, *got)
+    assert got[0][:4].tolist() == [0] * 4 and (got[0][4:8] > 0).all()
