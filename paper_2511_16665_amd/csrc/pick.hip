@@ -457,6 +457,8 @@ __device__ __forceinline__ float bins_per_logit(const Asked& ask, int V, float l
     else if (likely > 0.f) reach = fmax(reach, 4.0 * (double)likely);
     return (float)fmin((double)kBins / reach, 1e30);
 }
+// Is every token that weighs anything in a bin?  (In front of which the bins end where weights are 0; a difference that fp32 does not hold is in none, and at such a temperature it may weigh.)
+__device__ __forceinline__ bool bins_hold_all(const Asked& ask) { return 23.0 * ask.tau <= (double)FLT_MAX; }
 __device__ __forceinline__ float bin_of(const Weigh& w, float x, float per_logit) { return w.distance(x) * per_logit; }   // (its whole part; NaN: below them)
 
 // ---- outputs
@@ -850,7 +852,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         pr->bin_lo = pr->bin_hi = find.bin, pr->before = find.base;
         // two limits: all tokens down to the bin of the first, if a list holds them (all that weigh anything, if they are fewer than top_k)
         if (count_bins && ask.by_p()) {
-            state = (found ? find.value[0] : all) <= (double)kGather ? kAllDownTo : kStepwise;
+            state = (found || bins_hold_all(ask)) && (found ? find.value[0] : all) <= (double)kGather ? kAllDownTo : kStepwise;
             pr->before = 0.0, pr->bin_lo = 0, pr->bin_hi = found ? find.bin : kBins - 1;
         }
         pr->state = state;
@@ -1271,7 +1273,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
             const bool found = find.bin >= 0, down_to = count_bins && ask.by_p();
             const int lo = down_to ? 0 : find.bin, hi = found ? find.bin : kBins - 1;
             const double before = down_to ? 0.0 : find.base;
-            if (down_to ? (found ? find.value[0] : all) <= (double)kGather : found) {   // (uniform)
+            if (down_to ? (found || bins_hold_all(ask)) && (found ? find.value[0] : all) <= (double)kGather : found) {   // (uniform)
                 row.each(tid, NT, pieces, [&](int c, const float (&x)[VEC]) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {

@@ -37,3 +37,29 @@ def test_draws_among_many_tokens_of_low_index(code, V, likely, ask):
     values, *got = run(code, x, [ask] * len(u), 1, u)
     check_rows(values, [ask] * len(u), 1, u, *got)
     assert got[0][:4].tolist() == [0] * 4 and (got[0][4:8] > 0).all()
+
+
+def both_sides(x, asked, code, rng):
+    """Eight rows, which segments take, against the model; and 33 times as many, which are a workgroup's each: the same."""
+    u = rng.integers(0, 2 ** 32, 8)
+    values, *few = run(code, x, asked, 1, u)
+    check_rows(values, asked, 1, u, *few)
+    _, *many = run(code, np.tile(x, (33, 1)), asked * 33, 1, np.tile(u, 33))
+    for a, b in zip(few, many):
+        np.testing.assert_array_equal(b.reshape(33, *a.shape), np.broadcast_to(a, (33, *a.shape)))
+
+
+def shuffled(x, rng):
+    return np.stack([row[rng.permutation(len(row))] for row in x]).astype(np.float32)
+
+
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+@pytest.mark.parametrize("V", [20000, 70001])
+def test_differences_that_fp32_does_not_hold(code, V):
+    """Logits at both ends of the type, and temperatures at which they weigh all the same: 400 tokens are within fp32's range of the largest, the first top_k reach behind them."""
+    rng = np.random.default_rng(V)
+    x = np.full((8, V), -math.inf)
+    x[:, :400], x[:, 400:1400] = 3e38, -3e38
+    asked = [dict(top_k=k, top_p=p, tau=tau) for k, p, tau in ((1000, 0.99, math.inf), (1300, 0.5, 1e38), (1399, 0.9, 3e38), (600, 0.9, 2e37), (1000, 0.3, math.inf), (1399, 0.2, math.inf), (700, 0.999, 2e38),
+                                                               (500, 0.9, 1e38))]
+    both_sides(shuffled(x, rng), asked, code, rng)
