@@ -526,9 +526,10 @@ __device__ __forceinline__ void draw_from(const RowView<T> row, int c0, int c1, 
 }
 
 // Where the prefix ends in a list whose tokens follow on before_n others of weight before_w: its last token, or kNoEntry if it ends behind them.  n of the list's entries are
-// tokens, nearly all between the logits `best` and `least`.  S: the weight that top_p is a share of, for rows without top_k.
+// tokens, nearly all between the logits `best` and `least`.  S: the weight that top_p is a share of, for rows without top_k.  all: what is not in the list weighs nothing (a
+// top_k that reaches behind it, with top_p, then leaves the share of the whole list).
 template <int NT, typename L>
-__device__ __forceinline__ u64 end_in_list(const L l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
+__device__ __forceinline__ u64 end_in_list(const L l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, bool all, FindLds& s, double* tmp) {
     u64 end = kNoEntry - 1;   // (above every entry)
     auto order = [&](int i) { return l.e[i]; };
     // evenly over the distances from `best`
@@ -536,8 +537,8 @@ __device__ __forceinline__ u64 end_in_list(const L l, int n, const Asked ask, do
     auto bin = [&](int i) { return min((int)fminf(fmaxf(l.w.distance(entry_logit(l.e[i])) - near, 0.f) * per, 1e6f), kFindBins - 1); };
     if (ask.top_k > 0) {
         const double aim = (double)ask.top_k - before_n;
-        if (aim > (double)n) return kNoEntry;
-        end = locate<NT>(l.n, order, [](int) { return true; }, [](int) { return 1.0; }, bin, aim, s, tmp);
+        if (aim <= (double)n) end = locate<NT>(l.n, order, [](int) { return true; }, [](int) { return 1.0; }, bin, aim, s, tmp);
+        else if (!all) return kNoEntry;
         if (ask.by_p()) {
             double mine = 0.0;
             for (int i = threadIdx.x; i < l.n; i += NT) mine += l.e[i] <= end ? l.weight(i) : 0.0;
@@ -810,7 +811,7 @@ __global__ __launch_bounds__(kWeighThreads) void pick_weigh_k(PickGeo geo, const
         for (uint32_t i = kEarly * NT + tid; i < n; i += NT) local[i] = left(ws.list + (int64_t)lr * kList + i);
         __syncthreads();
         const TokenList<double> l{local, stored, w, (int)n};
-        const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
+        const u64 end = end_in_list<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, false, find, tmp);
         if (end != kNoEntry) {
             if (tid == 0) pr->state = kDone, pr->cut = ~(uint32_t)(end >> 32), pr->last = (int32_t)(uint32_t)end;
             if (out.token) {
@@ -1029,10 +1030,9 @@ __global__ __launch_bounds__(kGatherThreads) void pick_gather_k(PickGeo geo, con
             __syncthreads();
             const TokenList<uint32_t> l{local, stored, w, (int)n};
             if (state == kByNumber) ask.top_p = 1u << 31;
-            if (state == kAllDownTo && ask.top_k > (int)n) ask.top_k = 0;   // (tokens without weight fill it up)
             const double before = pr->before;
             const u64 end = end_in_list<NT>(l, (int)n, ask, state == kByWeight ? before : 0.0, state == kByNumber ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit,
-                                            find, tmp);
+                                            state == kAllDownTo, find, tmp);
             if (end != kNoEntry) {
                 const Kept in{~(uint32_t)(end >> 32), (int)(uint32_t)end, ask.least};
                 if (tid == 0) pr->cut = in.cut, pr->last = in.last;
@@ -1136,8 +1136,9 @@ __global__ __launch_bounds__(kWeighThreads) void pick_mask_k(PickGeo geo, const 
 // The same, as functions of their own: inlined they would cost pick_row_k's loops their registers (32 x 48 rows of 152064 770 us when it was first measured, 975
 // with them inlined; the kernels with fewer threads are better off inlined).
 template <int NT>
-__device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList<double> l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, FindLds& s, double* tmp) {
-    return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, s, tmp);
+__device__ __attribute__((noinline)) u64 end_in_list_apart(const TokenList<double> l, int n, const Asked ask, double before_w, double before_n, double S, float best, float least, bool all,
+                                                             FindLds& s, double* tmp) {
+    return end_in_list<NT>(l, n, ask, before_w, before_n, S, best, least, all, s, tmp);
 }
 template <int NT, typename T>
 __device__ __attribute__((noinline)) u64 cut_stepwise_apart(const RowView<T> row, const Asked ask, const Weigh w, u64* lds, double* tmp) {
@@ -1259,7 +1260,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
         }
         TokenList<double> l{list, nullptr, w, (int)n};
         u64 end = kNoEntry;
-        if (n > 0 && n <= (uint32_t)kGather) end = end_in_list_apart<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, find, tmp);
+        if (n > 0 && n <= (uint32_t)kGather) end = end_in_list_apart<NT>(l, (int)n, ask, 0.0, 0.0, whole, top, from, false, find, tmp);
         if (end == kNoEntry && use_bins) {
             // the bin that the end lies in
             static_assert(kBins <= NT, "a bin per thread");
@@ -1289,8 +1290,7 @@ __global__ __launch_bounds__(kRowThreads) void pick_row_k(int V, int rows_per_se
                     l.n = (int)n;
                     Asked one = ask;
                     if (count_bins && !down_to) one.top_p = 1u << 31;
-                    if (down_to && one.top_k > (int)n) one.top_k = 0;   // (tokens without weight fill it up)
-                    end = end_in_list_apart<NT>(l, (int)n, one, count_bins ? 0.0 : before, count_bins ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit, find, tmp);
+                    end = end_in_list_apart<NT>(l, (int)n, one, count_bins ? 0.0 : before, count_bins ? before : 0.0, whole, top - (float)lo / per_logit, top - (float)(hi + 1) / per_logit, down_to, find, tmp);
                 }
             }
         }
@@ -1359,7 +1359,7 @@ __global__ __launch_bounds__(kGatherThreads) void pick_small_k(int V, int rows_p
     }
     whole = block_sum<NT>(whole, tmp);   // (and all of both lists is there)
     const TokenList<double> l{entry, weight, w, V};
-    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, top, least, find, tmp);
+    const u64 end = end_in_list<NT>(l, (int)tokens, ask, 0.0, 0.0, whole, top, least, true, find, tmp);
     if (out.token) {
         draw_from_list<NT>(l, end, ask.least, V, find, tmp, out.kept ? out.kept + r : nullptr, u, &drawn);
         if (tid == 0) put_token(out.token + r, out.logprob ? out.logprob + 2 * r : nullptr, w, drawn, whole);

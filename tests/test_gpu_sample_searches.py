@@ -63,3 +63,24 @@ def test_differences_that_fp32_does_not_hold(code, V):
     asked = [dict(top_k=k, top_p=p, tau=tau) for k, p, tau in ((1000, 0.99, math.inf), (1300, 0.5, 1e38), (1399, 0.9, 3e38), (600, 0.9, 2e37), (1000, 0.3, math.inf), (1399, 0.2, math.inf), (700, 0.999, 2e38),
                                                                (500, 0.9, 1e38))]
     both_sides(shuffled(x, rng), asked, code, rng)
+
+
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+@pytest.mark.parametrize("kind", ["mask", "lowest", "two bells", "ends"])
+@pytest.mark.parametrize("V", [20000, 70001])
+def test_top_k_past_the_tokens_that_weigh_anything_with_top_p(code, kind, V):
+    """The share of top_p is that of the first top_k tokens, of which most weigh nothing."""
+    rng = np.random.default_rng(V + len(kind))
+    x = rng.normal(0.0, 2.0, (8, V))
+    if kind == "mask":            # a finite mask instead of -infinity
+        x[:, 3000:] = -1e4
+    if kind == "lowest":          # the lowest values of fp16 and fp32 as masks (in bf16 the latter is -infinity)
+        x[:4, 4000:], x[4:, 4000:] = -65504.0, float(np.finfo(np.float32).min)
+    if kind == "two bells":
+        x[:, :3000] *= 0.5
+        x[:, 3000:] = rng.normal(-40.0, 0.5, (8, V - 3000))
+    if kind == "ends":            # differences that fp32 does not hold
+        x[:, :400], x[:, 400:] = 3e38, -3e38
+    asked = [dict(top_k=k, top_p=p, tau=tau) for k, p, tau in ((5000, 0.9, 1.0), (5000, 0.95, 0.8), (4500, 0.9, 0.7), (7000, 0.5, 0.3), (4001, 0.999, 1.0), (19000, 0.9, 0.6), (5000, 1e-9, 1.0),
+                                                               (8100, 1.0 - 2.0 ** -24, 0.5))]
+    both_sides(shuffled(x, rng), asked, code, rng)
