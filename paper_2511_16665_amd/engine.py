@@ -108,8 +108,9 @@ class Engine:
         back and the bounds advance by the largest possible accept length.
         sample = (temperature, u_accept [B, n], u_final [B]) switches the acceptance from greedy to
         the target-only sampling rule (the drafter's top-k tree stays as it is); asked (a SampleFilter of B sequences, with
-        `sample` only) reduces the target's distribution to what top-k, top-p and min-p keep of it at the temperature: its own, which is
-        that of `sample`.  Tokens then follow the reduced distribution; the logits kept are the reduced ones."""
+        `sample` only) reduces the target's distribution to what top-k, top-p and min-p keep of it.  What that is goes by the
+        temperature of `sample`, at which tokens are drawn, unless asked has temperatures of its own (0: the sequence is decoded
+        greedily).  Tokens then follow the reduced distribution; the logits kept are the reduced ones."""
         if asked is not None and sample is None:
             raise ValueError("asked: a greedy step has no distribution to reduce")
         B = self.B
@@ -132,7 +133,7 @@ class Engine:
             temperature, u_accept, u_final = sample
             logits = logits_out if logits_out is not None else self.logits(n)
             self.ctx.verify_forward(B, t, self.kv, out_logits=logits, out_argmax=None, out_hidden=hid)
-            self._reduce(logits, n, asked)
+            self._reduce(logits, n, asked, temperature)
             self.ctx.accept(B, 2, temperature, t, logits, None, None, u_accept, u_final, self.stride, self.accept_len,
                             self.path_idx, self.out_tokens, self.n_out)
         self.ctx.kv_commit(B, self.kv, self.accept_len, self.path_idx, self.stride)
@@ -167,7 +168,7 @@ class Engine:
                                   u_draw, t, q)
         hid = self._buf("hid", n)
         self.ctx.verify_forward(B, t, self.kv, out_logits=logits, out_argmax=None, out_hidden=hid)
-        self._reduce(logits, n, asked)
+        self._reduce(logits, n, asked, temperature)
         self.ctx.accept(B, 1, temperature, t, logits, None, q, u_accept, u_final, self.stride, self.accept_len,
                         self.path_idx, self.out_tokens, self.n_out)
         self.ctx.kv_commit(B, self.kv, self.accept_len, self.path_idx, self.stride)
@@ -179,15 +180,23 @@ class Engine:
         self.pending_max_new = inc
         return al, out
 
-    def _reduce(self, logits, n, asked):
-        """What is not kept of the target's logits [B, n, V] becomes -infinity, in place."""
+    def _reduce(self, logits, n, asked, temperature):
+        """What is not kept of the target's logits [B, n, V] becomes -infinity, in place; at the step's temperature, unless the request has its own."""
         if asked is None:
             return
+        if asked.temperature is None:
+            asked = tlt.SampleFilter(self._buf_temperature(temperature), asked.top_k, asked.top_p, asked.min_p)
         key = ("reduce", n)
         if key not in self._trees:
             self._trees[key] = tlt.sample_workspace(self.B * n, self.cfg.vocab)
         rows = logits.view(self.B, n, self.cfg.vocab)
         tlt.sample_filter(tlt.TLT_F32, rows, asked, rows, None, self._trees[key])
+
+    def _buf_temperature(self, temperature):
+        """[B] fp32 with the step's temperature."""
+        if "temperature" not in self._trees:
+            self._trees["temperature"] = torch.empty((self.B,), dtype=torch.float32, device="cuda")
+        return self._trees["temperature"].fill_(temperature)
 
     def _read_result(self):
         """(accept_len [B], out_tokens [B, stride]) as numpy arrays, in the step's one synchronisation; raises when a kernel saw

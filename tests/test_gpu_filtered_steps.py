@@ -91,3 +91,28 @@ def test_one_token_kept_is_greedy_decoding():
     for b in range(B):
         m = min(len(greedy[b]), len(got[b]))
         assert m >= 6 and greedy[b][:m] == got[b][:m]
+
+
+@pytest.mark.parametrize("target_only", [False, True])
+def test_a_filter_without_a_temperature_takes_the_step_s(target_only):
+    """The same steps as with that temperature given for every sequence, and not those of temperature 1; one that is given as 0 leaves its sequence greedy."""
+    tau, n = 0.4, N if target_only else len(osd.static_template(K, D, N)[0])
+    top_p = torch.full((B,), 0.7).cuda()
+    given = [None, torch.full((B,), tau).cuda(), torch.ones((B,)).cuda(), torch.tensor([0.0] + [tau] * (B - 1)).cuda()]
+    runs = []
+    for temperature in given:
+        filt, rng, kept = tlt.SampleFilter(temperature, None, top_p), np.random.default_rng(6), []
+        e, _ = engine(5)
+        for _ in range(4):
+            draws = [dev(u32(rng, B, n)) for _ in range(2)] + [dev(u32(rng, B))]
+            al, out = e.step(K, D, N, sample=(tau, *draws[1:]), asked=filt) if target_only else e.step_sampled(K, D, N, tau, *draws, asked=filt)
+            kept.append((al.copy(), out.copy(), e.logits(n).cpu().numpy()))
+        assert filt.temperature is temperature
+        e.ctx.close()
+        runs.append(kept)
+    for a, b in zip(runs[0], runs[1]):
+        for x, y in zip(a, b):
+            np.testing.assert_array_equal(x, y)
+    counts = [np.isfinite(r[0][2]).sum(-1) for r in runs]         # of the first step, whose tree is the same
+    assert (counts[0] <= counts[2]).all() and (counts[0] < counts[2]).any()
+    assert (counts[3][0] == 1).all() and (counts[3][1:] == counts[0][1:]).all()
