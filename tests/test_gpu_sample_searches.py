@@ -7,7 +7,7 @@ import torch
 
 import pick_model as pm
 from paper_2511_16665_amd import binding as tlt
-from test_gpu_sample import check_rows, run
+from test_gpu_sample import KINDS, asks, check_rows, filter_of, logits_of, run
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +84,36 @@ def test_top_k_past_the_tokens_that_weigh_anything_with_top_p(code, kind, V):
     asked = [dict(top_k=k, top_p=p, tau=tau) for k, p, tau in ((5000, 0.9, 1.0), (5000, 0.95, 0.8), (4500, 0.9, 0.7), (7000, 0.5, 0.3), (4001, 0.999, 1.0), (19000, 0.9, 0.6), (5000, 1e-9, 1.0),
                                                                (8100, 1.0 - 2.0 ** -24, 0.5))]
     both_sides(shuffled(x, rng), asked, code, rng)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("code,V", [(tlt.TLT_F32, 152064), (tlt.TLT_BF16, 131073), (tlt.TLT_F32, 70001), (tlt.TLT_BF16, 65536)])
+def test_every_setting_on_rows_of_16_and_32_segments(code, V, kind):
+    """Rows at the vocabularies of models (16 segments from 65536 tokens on, 32 from 131072): every setting, 28 rows at a time and three, which have as many segments."""
+    rng = np.random.default_rng(V + len(kind))
+    x = logits_of(kind, 28, V, rng)
+    u = rng.integers(0, 2 ** 32, 28)
+    asked = asks(rng, 28)
+    values, *got = run(code, x, asked, 1, u, pad=V % 4)
+    check_rows(values, asked, 1, u, *got)
+    for r in range(0, 28, 3):
+        _, *three = run(code, x[r:r + 3], asked[r:r + 3], 1, u[r:r + 3])
+        for a, b in zip(three, got):
+            np.testing.assert_array_equal(a, b[r:r + 3])
+
+
+@pytest.mark.parametrize("code", [tlt.TLT_F32, tlt.TLT_BF16])
+def test_rows_of_several_segments_in_two_passes(code):
+    """More rows than are taken at a time: every pass finds its counters cleared, whatever the one before left."""
+    rng = np.random.default_rng(13)
+    V, rows = 8200, 1100                     # (two passes of 550 rows, of two segments each)
+    x = np.concatenate([logits_of(kind, 25, V, rng) for kind in KINDS] * 6)[:rows]
+    u = rng.integers(0, 2 ** 32, rows)
+    asked = (asks(rng, 27) * 41)[:rows]
+    dt = tlt.torch_dtype(code)
+    logits = torch.from_numpy(x).cuda().to(dt)
+    token, kept = (torch.full((rows,), 9, dtype=torch.int32, device="cuda") for _ in range(2))
+    logprob, ws = torch.zeros((rows, 2), device="cuda"), tlt.sample_workspace(rows, V)
+    ws.fill_(255)
+    tlt.sample(code, logits, filter_of(asked), torch.from_numpy(u.astype(np.uint32).view(np.int32)).cuda(), token, logprob, kept, ws)
+    check_rows(logits.double().cpu().numpy(), asked, 1, u, token.cpu().numpy(), logprob.cpu().numpy(), kept.cpu().numpy())
