@@ -460,7 +460,8 @@ int tlt_rope_freqs(int kind, int rot_dim, double theta, double factor, double or
  *   not written,
  *   keys and values to kv_out, rows of 2*Hkv*d elements kv_stride apart (NULL: nowhere).
  * kv and kv8: one at most, with slot; at least one output.  q_out may be qkv with its stride, kv_out may be qkv + Hq*d with its stride; other
- * overlaps, and two rows with one slot, are caller errors (such rows then hold a mixture).  head_dim even, <= 256; any page size; rows < 2^23; pointers and
+ * overlaps, and two rows with one slot, are caller errors (such rows then hold a mixture).  head_dim even, <= 256; any page size; rows < 2^23 and
+ * rows * (Hq + 2Hkv) < 2^26 - 4; pointers and
  * strides in whole elements (kv8's pools 16-byte aligned); 16-byte aligned rows of heads in whole 16-byte pieces are the fast case.  Sums and rotations are fp32, one rounding to dtype. */
 int tlt_rope_write(void *stream, int dtype, int rows, int n_q_heads, int n_kv_heads, int head_dim, int page_size, const tlt_rope *rope, const void *qkv,
                    int64_t qkv_stride, const void *bqkv, const int32_t *position, const int64_t *slot, const tlt_kv *kv, const tlt_kv8 *kv8, void *q_out,
@@ -470,8 +471,10 @@ int tlt_rope_write(void *stream, int dtype, int rows, int n_q_heads, int n_kv_he
  * What every request asks for, DEVICE arrays with an entry per sequence, each NULL for none: temperature (NULL: 1), top_k (<= 0: off), top_p
  * (off unless < 1), min_p (off unless > 0).
  *
- * A row of logits l gives whole-number weights W_j = floor(exp(l_j / temperature - max / temperature) * 2^32) (exp in double: tlt_accept's), so every sum
- * is exact.  Tokens are ordered by falling logit, equal ones by rising index; tokens at -infinity are never kept.  Kept are
+ * A row of logits l gives whole-number weights W_j = floor(exp(l_j / temperature - max / temperature) * 2^32), so every sum
+ * is exact.  exp is a polynomial in double of (l_j - max) / temperature, good to 2^-50; tlt_accept subtracts rounded quotients and calls the
+ * library's function, so some weights, a few in a million at most, differ from its by one, and a draw that close to a token's border by one kept
+ * token.  Tokens are ordered by falling logit, equal ones by rising index; tokens at -infinity are never kept.  Kept are
  *   the first top_k of the order, weight S_k together;
  *   of these the ones before which less than top_p * S_k lies (top_p in units of 2^-31, rounded down; the first one always);
  *   of these the ones with W_j >= min_p * 2^32 (rounded down; the first one always).
@@ -488,7 +491,7 @@ typedef struct tlt_filter {
 size_t tlt_sample_workspace_bytes(int rows, int vocab);
 
 /* One token per row: the first, by index, whose running sum of kept weights exceeds (u[r] * S) >> 32, S their whole sum and u (DEVICE [rows])
- * the caller's 32-bit uniforms: the final draw of tlt_accept.  out_token [rows] (-1 where nothing is kept); out_logprob [rows][2] fp32, may be NULL: the
+ * the caller's 32-bit uniforms: the final draw of tlt_accept (but for the weights' last unit).  out_token [rows] (-1 where nothing is kept); out_logprob [rows][2] fp32, may be NULL: the
  * token's log-probability in the distribution it was drawn from and in the row's whole one, l / temperature - max / temperature - ln(S 2^-32) with S
  * the kept or the whole sum (-infinity where nothing is kept, NaN with a NaN in the row); out_kept [rows], may be NULL: number of tokens kept. */
 int tlt_sample(void *stream, int dtype, int rows, int rows_per_seq, int vocab, const void *logits, int64_t row_stride, const tlt_filter *filter,

@@ -1,8 +1,8 @@
 // Sampling from rows of logits behind top-k, top-p and min-p: one token per row, or the row with all other tokens at -infinity.
 //
-// Weights are the acceptance rules' whole numbers W = floor(exp(l / tau - max / tau) * 2^32), so sums do not depend on their order; they are held as doubles, which are exact
-// up to 2^53 (2^20 tokens, 2^52).  What is kept is a prefix of the order (logit falling, index rising), given by the logit it ends in and the last index kept of those equal to it
-// (cut, last below), and of that what weighs enough.  Equal logits have equal weights.
+// Weights are whole numbers W = floor(exp(l / tau - max / tau) * 2^32), so sums do not depend on their order; they are held as doubles, which are exact up to 2^53 (2^20 tokens,
+// 2^52).  (The acceptance rules form them by another formula; a few in a million at most differ by one.)  What is kept is a prefix of the order (logit falling, index rising), given by the logit it ends in
+// and the last index kept of those equal to it (cut, last below), and of that what weighs enough.  Equal logits have equal weights.
 //
 // A row is cut into segments, a workgroup each, and read two or three times:
 //   pick_max_k     the largest logit, and how far down the most likely few hundred tokens reach
